@@ -25,7 +25,9 @@ EXPORTS = ["muxq_version", "muxq_status_string", "muxq_k_pad", "muxq_wq_bytes",
            "muxq_mlp", "muxq_mlp_workspace_bytes",
            "muxq_quantize_weight_smooth", "muxq_smooth_absmax",
            "muxq_probe_mfma_rate", "muxq_gemm_kernel", "muxq_code_kernel", "muxq_static_bytes", "muxq_static_layout_of",
-           "muxq_prepare_static", "muxq_linear_static", "muxq_gelu_absmax"]
+           "muxq_prepare_static", "muxq_linear_static", "muxq_gelu_absmax",
+           "muxq_kv_append", "muxq_kv_gather", "muxq_paged_attention", "muxq_paged_attention_workspace_bytes",
+           "muxq_lora", "muxq_norm", "muxq_norm_slabs", "muxq_norm_scratch_bytes"]
 
 
 class MuxqError(RuntimeError):
@@ -46,6 +48,12 @@ class StaticLayout(C.Structure):
 class ActOpts(C.Structure):
     _fields_ = [("x_gran", C.c_int32), ("ia_bits", C.c_int32), ("absmax_ready", C.c_int32),
                 ("aux_own_scale", C.c_int32), ("absmax_slabs", C.c_int32)]
+
+
+class KvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("type", "n_blocks", "block_size", "n_kv_heads", "head_dim", "reserved")] + \
+               [(n, C.c_int64) for n in ("ld_block", "ld_head", "ld_token")]
 
 
 X_PER_TENSOR, X_PER_TOKEN = 0, 1
@@ -137,6 +145,23 @@ def lib():
         L.muxq_linear_gelu.restype = i
         L.muxq_linear_gelu.argtypes = [vp, i, i, i, vp, vp, i, i, vp, f, i, i, vp, i, vp, sz, vp,
                                        C.POINTER(ActOpts), vp]
+        kv = C.POINTER(KvCache)
+        L.muxq_kv_append.restype = i
+        L.muxq_kv_append.argtypes = [vp, vp, i, i, i, vp, i, i, vp, i, vp, vp, vp, i, i, i, kv, vp]
+        L.muxq_kv_gather.restype = i
+        L.muxq_kv_gather.argtypes = [vp, i, kv, vp, i, vp, i, vp]
+        L.muxq_paged_attention_workspace_bytes.restype = sz
+        L.muxq_paged_attention_workspace_bytes.argtypes = [i, i, i, i, i]
+        L.muxq_paged_attention.restype = i
+        L.muxq_paged_attention.argtypes = [vp, i, i, i, kv, vp, i, vp, i, f, vp, i, vp, sz, vp]
+        L.muxq_lora.restype = i
+        L.muxq_lora.argtypes = [vp, i, i, i, vp, vp, vp, i, i, vp, vp, i, vp, i, i, vp, i, vp]
+        L.muxq_norm_slabs.restype = i
+        L.muxq_norm_slabs.argtypes = [i, i]
+        L.muxq_norm_scratch_bytes.restype = sz
+        L.muxq_norm_scratch_bytes.argtypes = [i, i]
+        L.muxq_norm.restype = i
+        L.muxq_norm.argtypes = [vp, i, i, i, vp, i, f, vp, vp, vp, i, vp, vp, i, f, vp, i, vp, i, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -525,3 +550,206 @@ def muxq_probe_mfma_rate(a_codes, b_codes, iters=4000, n_workgroups=512):
     ops = n_workgroups * 4 * iters * 8 * 65536.0
     c = clocks.cpu().tolist()
     return ops / (start.elapsed_time(stop) * 1e-3) / 1e12, (c[0] / (c[1] * 10.0) if c[1] else 0.0)
+
+
+# ---- what stands between the projections of a block (include/muxq_block.h) --------------------
+
+NORM_LAYER, NORM_RMS = 0, 1
+_NORM = {"layer": NORM_LAYER, "rms": NORM_RMS, NORM_LAYER: NORM_LAYER, NORM_RMS: NORM_RMS}
+
+
+def _want(ok, what):
+    if not ok:
+        raise MuxqError(what)
+
+
+def _rows(t, name, dtype=torch.float16):
+    """t: [rows, heads, d] or [rows, width] of fp16 whose rows are contiguous; returns its row stride."""
+    st = t.stride()
+    _want(t.dtype == dtype and t.is_cuda and st[-1] == 1 and (t.dim() == 2 or (t.dim() == 3 and (st[1] == t.shape[2] or t.shape[1] == 1))),
+          f"{name}: a GPU tensor of {dtype} with contiguous rows is expected")
+    return st[0]
+
+
+def _ints(t, n, name):
+    _want(t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and t.numel() >= n,
+          f"{name}: a contiguous int32 GPU tensor of at least {n} entries is expected")
+    return t.data_ptr()
+
+
+def _vector(t, n, name, dtype=torch.float16):
+    if t is None:
+        return None
+    _want(t.dtype == dtype and t.is_cuda and t.is_contiguous() and t.numel() == n,
+          f"{name}: a contiguous GPU tensor of {n} {dtype} is expected")
+    return t.data_ptr()
+
+
+def _kv(k_cache, v_cache, k_scale, v_scale):
+    """The descriptor of a cache given as tensors [pages, heads, tokens of a page, d]: views of any
+    strides with contiguous d (transpose a [pages, tokens, heads, d] tensor), fp16 or int8, the latter with scales
+    [pages, heads, tokens of a page]."""
+    n, heads, block, d = k_cache.shape
+    lb, lh, lt, one = k_cache.stride()
+    _want(one == 1 and k_cache.is_cuda and v_cache.is_cuda and v_cache.shape == k_cache.shape and
+          v_cache.stride() == k_cache.stride() and v_cache.dtype == k_cache.dtype,
+          "cache: keys and values are GPU tensors of one shape, type and order, with contiguous head dimensions")
+    c = KvCache(k_cache.data_ptr(), v_cache.data_ptr(), None, None, 0, n, block, heads, d, 0, lb, lh, lt)
+    if k_cache.dtype == torch.int8:
+        _want(k_scale is not None and v_scale is not None, "cache: 8-bit codes come with k_scale and v_scale")
+        c.type = 1
+        c.k_scale = _vector(k_scale, n * heads * block, "k_scale", torch.float32)
+        c.v_scale = _vector(v_scale, n * heads * block, "v_scale", torch.float32)
+    else:
+        _want(k_cache.dtype == torch.float16 and k_scale is None and v_scale is None,
+              "cache: fp16 without scales, or int8 with them")
+    # a dimension of one element may carry any stride
+    if heads == 1:
+        c.ld_head = (lt * block + 15) // 16 * 16
+    if n == 1:
+        c.ld_block = max(lb, (block - 1) * lt + (heads - 1) * c.ld_head + d + 15) // 16 * 16
+    return c
+
+
+def alloc_kv_cache(n_blocks, block_size, n_kv_heads, head_dim, dtype=torch.float16, device="cuda"):
+    """(k_cache, v_cache, k_scale, v_scale): empty pages, heads before tokens; scales are None for fp16."""
+    k, v = (torch.empty((n_blocks, n_kv_heads, block_size, head_dim), dtype=dtype, device=device) for _ in "kv")
+    if dtype != torch.int8:
+        return k, v, None, None
+    ks, vs = (torch.empty((n_blocks, n_kv_heads, block_size), dtype=torch.float32, device=device) for _ in "kv")
+    return k, v, ks, vs
+
+
+def muxq_kv_append(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, q=None, q_out=None, positions=None,
+                   cos_sin=None, interleaved=False):
+    """Keys and values [M, n_kv_heads, d] of new tokens to their slots (int32 [M], page * block_size + place,
+    -1: nowhere) of the cache; with cos_sin (float [positions, rot_dim]: cosines, then sines) and positions
+    (int32 [M]) rotated on the way, and the queries q [M, n_heads, d] with them.  q, k, v may be column
+    ranges of one tensor.  Returns q_out (made when not given; None without q)."""
+    M, heads, d = k.shape
+    c = _kv(k_cache, v_cache, k_scale, v_scale)
+    _want(v.shape == k.shape and heads == c.n_kv_heads and d == c.head_dim, "muxq_kv_append: k, v and the cache differ in heads")
+    n_heads = ldq = ldqo = 0
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
+        n_heads = q.shape[1]
+        _want(q.shape == (M, n_heads, d) and q_out.shape == q.shape, "muxq_kv_append: q and k differ in tokens or head size")
+        ldq, ldqo = _rows(q, "q"), _rows(q_out, "q_out")
+    n_pos = rot = 0
+    if cos_sin is not None:
+        n_pos, rot = cos_sin.shape
+        _want(positions is not None, "muxq_kv_append: cos_sin comes with positions")
+    _check(lib().muxq_kv_append(_p(k), _p(v), M, _rows(k, "k"), _rows(v, "v"), _p(q), n_heads, ldq, _p(q_out), ldqo,
+                                _ints(slots, M, "slots"), None if positions is None else _ints(positions, M, "positions"),
+                                _vector(cos_sin, n_pos * rot, "cos_sin", torch.float32), n_pos, rot,
+                                int(interleaved), C.byref(c), _stream()), "muxq_kv_append")
+    return q_out
+
+
+def muxq_kv_gather(slots, k_cache, v_cache, k_scale=None, v_scale=None, k_out=None, v_out=None):
+    """Keys and values of the cache's slots (int32 [M]) as fp16 [M, n_kv_heads, d]; zeros for slots outside."""
+    c = _kv(k_cache, v_cache, k_scale, v_scale)
+    shape = (slots.numel(), c.n_kv_heads, c.head_dim)
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=torch.float16, device=k_cache.device)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=torch.float16, device=k_cache.device)
+    _want(k_out.shape == shape and v_out.shape == shape, f"muxq_kv_gather: outputs of shape {shape} are expected")
+    _check(lib().muxq_kv_gather(_ints(slots, shape[0], "slots"), shape[0], C.byref(c), _p(k_out), _rows(k_out, "k_out"),
+                                _p(v_out), _rows(v_out, "v_out"), _stream()), "muxq_kv_gather")
+    return k_out, v_out
+
+
+def attention_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_length) -> int:
+    return lib().muxq_paged_attention_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_length)
+
+
+def alloc_attention_workspace(S, n_heads, n_kv_heads, head_dim, max_length, device="cuda"):
+    """Workspace of muxq_paged_attention (also good for a smaller S or max_length); None where none is needed."""
+    n = attention_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_length)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def muxq_paged_attention(q, k_cache, v_cache, block_table, lengths, max_length, scale=None, k_scale=None, v_scale=None,
+                         out=None, workspace=None):
+    """Attention of one new token of each sequence, q [S, n_heads, d], over the cache's pages that
+    block_table (int32 [S, pages]) lists, the first lengths[s] tokens (int32 [S]) of each sequence;
+    max_length: a bound on lengths known on the host.  scale: 1 / sqrt(d) when not given."""
+    S, n_heads, d = q.shape
+    c = _kv(k_cache, v_cache, k_scale, v_scale)
+    if out is None:
+        out = torch.empty((S, n_heads, d), dtype=torch.float16, device=q.device)
+    _want(d == c.head_dim and out.shape == q.shape, "muxq_paged_attention: q, out and the cache differ in head size")
+    _want(block_table.dtype == torch.int32 and block_table.is_cuda and block_table.shape[0] == S and block_table.stride(1) == 1,
+          "muxq_paged_attention: block_table is an int32 GPU tensor [S, pages] with contiguous rows")
+    if workspace is None:
+        workspace = alloc_attention_workspace(S, n_heads, c.n_kv_heads, d, max_length, q.device)
+    _want(max_length <= block_table.shape[1] * c.block_size, "muxq_paged_attention: max_length goes beyond the block table")
+    _check(lib().muxq_paged_attention(_p(q), S, n_heads, _rows(q, "q"), C.byref(c), _p(block_table),
+                                      block_table.stride(0) if S > 1 else block_table.shape[1], _ints(lengths, S, "lengths"),
+                                      max_length, d ** -0.5 if scale is None else scale, _p(out), _rows(out, "out"),
+                                      _p(workspace), 0 if workspace is None else workspace.numel(), _stream()),
+           "muxq_paged_attention")
+    return out
+
+
+def muxq_lora(X, A, B, scales, starts, adapters, Y, out=None):
+    """out = Y + scales[i] (X A_i^T) B_i^T for rows starts[q]..starts[q + 1] of request q with adapter i =
+    adapters[q] (-1: none).  X [M, K], Y [M, N] fp16; A [n, r, K], B [n, N, r] fp16; scales float [n]; starts int32
+    [requests + 1], adapters int32 [requests].  out may be Y."""
+    M, K = X.shape
+    n, r, k = A.shape
+    N = Y.shape[1]
+    requests = adapters.numel()
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.float16, device=X.device)
+    _want(k == K and B.shape == (n, N, r) and Y.shape[0] == M and out.shape == (M, N), "muxq_lora: shapes of X, A, B, Y and out do not fit")
+    _check(lib().muxq_lora(_p(X), M, K, _rows(X, "X"), _vector(A, n * r * K, "A"), _vector(B, n * N * r, "B"),
+                           _vector(scales, n, "scales", torch.float32), n, r, _ints(starts, requests + 1, "starts"),
+                           _ints(adapters, requests, "adapters"), requests, _p(Y), _rows(Y, "Y"), N, _p(out),
+                           _rows(out, "out"), _stream()), "muxq_lora")
+    return out
+
+
+def norm_slabs(M: int, K: int) -> int:
+    """Rows of column maxima that muxq_norm leaves for M tokens (absmax_slabs of the next layer)."""
+    return lib().muxq_norm_slabs(M, K)
+
+
+def alloc_norm_scratch(M, K, device="cuda"):
+    """Scratch of a muxq_norm call that hands maxima over; None where none is needed."""
+    n = lib().muxq_norm_scratch_bytes(M, K)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def muxq_norm(x, weight, bias=None, residual=None, residual_scale=1.0, post_weight=None, post_bias=None, gate=None,
+              kind="layer", eps=1e-5, out=None, residual_out=None, slabs=None, scratch=None):
+    """r = residual_scale * residual + gate * post-norm(x) (each part optional), y = norm(r) with kind "layer" or "rms".
+    gate: [K], or [M, K] for one per token.  slabs: the absmax_partial region of the next layer's workspace
+    (workspace[layout.absmax_partial:]), which then runs with absmax_ready=True, absmax_slabs=norm_slabs(M, K).
+    Returns (y, r); r is made when there is something to add or scale, else None."""
+    M, K = x.shape
+    if out is None:
+        out = torch.empty((M, K), dtype=torch.float16, device=x.device)
+    if residual_out is None and (residual is not None or gate is not None or post_weight is not None):
+        residual_out = torch.empty((M, K), dtype=torch.float16, device=x.device)
+    if slabs is not None:
+        _want(slabs.is_cuda and slabs.is_contiguous() and
+              slabs.numel() * slabs.element_size() >= norm_slabs(M, K) * k_pad(K) * 2, "muxq_norm: slabs are too small")
+        if scratch is None:
+            scratch = alloc_norm_scratch(M, K, x.device)
+    for t, name in ((residual, "residual"), (out, "out"), (residual_out, "residual_out")):
+        _want(t is None or t.shape == x.shape, f"muxq_norm: {name} and x differ in shape")
+    ldg = 0
+    if gate is not None and gate.dim() == 2:
+        _want(gate.shape == x.shape, "muxq_norm: gate is [K] or [M, K]")
+        ldg = _rows(gate, "gate") if M > 1 else K
+    elif gate is not None:
+        _vector(gate, K, "gate")
+    _check(lib().muxq_norm(_p(x), M, K, _rows(x, "x"), _p(residual), 0 if residual is None else _rows(residual, "residual"),
+                           residual_scale, _vector(post_weight, K, "post_weight"), _vector(post_bias, K, "post_bias"), _p(gate), ldg,
+                           _vector(weight, K, "weight"), _vector(bias, K, "bias"), _NORM[kind], eps, _p(residual_out),
+                           0 if residual_out is None else _rows(residual_out, "residual_out"), _p(out), _rows(out, "out"),
+                           _p(slabs), _p(scratch), 0 if scratch is None else scratch.numel(), _stream()), "muxq_norm")
+    return out, residual_out
