@@ -41,7 +41,7 @@ int check_cache(const muxq_kv_cache *c, muxq::KvView *view)
         c->ld_token < (c->n_kv_heads - 1) * c->ld_head + c->head_dim)
         return MUXQ_ERR_SHAPE;
     if (!aligned(c->k, 16) || !aligned(c->v, 16)) return MUXQ_ERR_ALIGN;
-    if (c->type == MUXQ_KV_INT8 && (!aligned(c->k_scale, 4) || !aligned(c->v_scale, 4))) return MUXQ_ERR_ALIGN;
+    if (c->type == MUXQ_KV_INT8 && (!aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))) return MUXQ_ERR_ALIGN;
     view->k = (char *)c->k;
     view->v = (char *)c->v;
     view->k_scale = c->k_scale;
@@ -62,6 +62,7 @@ constexpr int kMaxRows = 1 << 24, kMaxCols = 1 << 21;
 int check_attend(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
 {
     if (S < 1 || S > 65535 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || max_length < 1 ||
+        max_length > 65535ll * muxq::kAttendMaxChunk ||
         head_dim < 16 || head_dim > 256 || head_dim % 16 != 0 || n_heads > kMaxCols / head_dim)
         return MUXQ_ERR_SHAPE;
     return MUXQ_OK;
