@@ -1,82 +1,215 @@
 // The norms around the residual stream, with the column maxima for the next quantised layer.
+//
+// Each element is read once and written once: X and R in, the stream and Y out, 8 bytes a channel and token.  A
+// row stays in the registers of its W waves in binary32 from the first load to the last store, both means of
+// both norms taken from there (the mean first, then the squares of what is left: no cancellation).  Prompts:
+// a wave a row.  Few rows: four waves
+// a row, and 16 beyond 8192 channels, so that a lane has few elements and its loads go out together.
+// Column maxima: every wave keeps those of the rows it writes; a workgroup's go to the scratch and a second launch folds
+// them (half of what the abs-max pass over Y would read is not even written).  Up to 64 rows their magnitudes are
+// the maxima, and there is one launch.
 #include "muxq_block_kernels.h"
 
 namespace muxq {
 namespace {
 
-__device__ float block_sum(float v, float *sh)
+constexpr int kMaxGroups = 512;             // workgroups that leave maxima
+
+template <int W>
+__device__ __forceinline__ float row_sum(float v, float *sh, int &turn)
 {
     for (int x = 1; x < 64; x <<= 1) v += __shfl_xor(v, x, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (sh[0] + sh[1]) + (sh[2] + sh[3]);
-}
-
-// One workgroup to a row, a thread every 256th channel; the row stays in LDS in binary32.
-template <bool kRms>
-__device__ void norm_row(float *row, int K, const _Float16 *w, const _Float16 *b, float eps, float *sh)
-{
-    float mean = 0.0f;
-    if (!kRms) {
-        float s = 0.0f;
-        for (int k = threadIdx.x; k < K; k += 256) s += row[k];
-        mean = block_sum(s, sh) / K;
+    if constexpr (W > 1) {                  // two buffers in turn: one barrier a sum
+        float *const s = sh + (turn ^= W);
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) v += s[w];
     }
-    float q = 0.0f;
-    for (int k = threadIdx.x; k < K; k += 256) q += (row[k] - mean) * (row[k] - mean);
-    const float inv = 1.0f / sqrtf(block_sum(q, sh) / K + eps);
-    for (int k = threadIdx.x; k < K; k += 256) row[k] = (row[k] - mean) * inv * (float)w[k] + (b ? (float)b[k] : 0.0f);
+    return v;
 }
 
-template <bool kRms>
-__global__ __launch_bounds__(256) void k_norm(NormArgs n)
+// W waves to a row, C runs of 8 channels to a lane; a workgroup of kWaves waves has kWaves / W rows at a time.
+template <int W, int C, bool kRms>
+__global__ __launch_bounds__(64 * (W == 1 ? 8 : W)) void k_norm(NormArgs n, uint16_t *maxima)
 {
-    extern __shared__ float row[];
-    __shared__ float sh[4];
-    const int m = blockIdx.x;
-    for (int k = threadIdx.x; k < n.K; k += 256) row[k] = (float)n.x[(long long)m * n.ldx + k];
-    if (n.post_w) norm_row<kRms>(row, n.K, n.post_w, n.post_b, n.eps, sh);
-    for (int k = threadIdx.x; k < n.K; k += 256) {
-        float t = row[k];
-        if (n.gate) t *= (float)n.gate[(long long)m * n.ldg + k];
-        if (n.res) t = n.r_scale * (float)n.res[(long long)m * n.ldr + k] + t;
-        row[k] = t;
+    constexpr int kWaves = W == 1 ? 8 : W, kRows = kWaves / W;
+    __shared__ float sh[2 * W];
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, t = W == 1 ? tid & 63 : tid;
+    const float by_k = 1.0f / (float)n.K;
+    int turn = 0;
+    bool there[C];
+    int at[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        at[c] = (c * 64 * W + t) * 8;
+        there[c] = at[c] < n.K;
     }
-    if (n.r_out)
-        for (int k = threadIdx.x; k < n.K; k += 256) n.r_out[(long long)m * n.ldro + k] = (_Float16)row[k];
-    norm_row<kRms>(row, n.K, n.w, n.b, n.eps, sh);
-    for (int k = threadIdx.x; k < n.K; k += 256) n.y[(long long)m * n.ldy + k] = (_Float16)row[k];
+    uint4 most[C] = {};
+    float v[C][8];
+
+    // (the vectors of weights come from L1 for each row: in registers they cost more waves than they save loads)
+    auto normed = [&](const _Float16 *w, const _Float16 *b) {
+        f16x8 ww[C], bb[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            ww[c] = bb[c] = f16x8{};
+            if (there[c]) {
+                ww[c] = *(const f16x8 *)(w + at[c]);
+                if (b) bb[c] = *(const f16x8 *)(b + at[c]);
+            }
+        }
+        float mean = 0.0f;
+        if (!kRms) {
+            float s = 0.0f;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s += v[c][i];
+            mean = row_sum<W>(s, sh, turn) * by_k;
+        }
+        float q = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[c][i] = there[c] ? v[c][i] - mean : 0.0f;
+                q = __builtin_fmaf(v[c][i], v[c][i], q);
+            }
+        const float inv = 1.0f / sqrtf(row_sum<W>(q, sh, turn) * by_k + n.eps);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] = __builtin_fmaf(v[c][i] * inv, (float)ww[c][i], (float)bb[c][i]);
+    };
+
+    const int step = gridDim.x * kRows;
+    for (int m = blockIdx.x * kRows + (W == 1 ? tid >> 6 : 0); m < n.M; m += step) {
+        f16x8 r[C], gate[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            f16x8 x = {};
+            r[c] = gate[c] = f16x8{};
+            if (there[c]) {
+                x = *(const f16x8 *)(n.x + (long long)m * n.ldx + at[c]);
+                if (n.res) r[c] = *(const f16x8 *)(n.res + (long long)m * n.ldr + at[c]);
+                if (n.gate) gate[c] = *(const f16x8 *)(n.gate + (long long)m * n.ldg + at[c]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] = (float)x[i];
+        }
+        if (n.post_w) normed(n.post_w, n.post_b);
+        if (n.gate) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] *= (float)gate[c][i];
+        }
+        if (n.res) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] = __builtin_fmaf(n.r_scale, (float)r[c][i], v[c][i]);
+        }
+        if (n.r_out) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                f16x8 o;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = (_Float16)v[c][i];
+                if (there[c]) *(f16x8 *)(n.r_out + (long long)m * n.ldro + at[c]) = o;
+            }
+        }
+        normed(n.w, n.b);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            f16x8 o;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = (_Float16)v[c][i];
+            const uint4 bits = __builtin_bit_cast(uint4, o);
+            if (there[c]) {
+                *(uint4 *)(n.y + (long long)m * n.ldy + at[c]) = bits;
+                most[c] = absmax_step(most[c], bits);
+            }
+            if (n.slabs != nullptr && maxima == nullptr && at[c] < n.k_pad)       // few rows: each a row of maxima
+                *(uint4 *)(n.slabs + (long long)m * n.k_pad + at[c]) = there[c] ? absmax_step(uint4{0, 0, 0, 0}, bits) : uint4{0, 0, 0, 0};
+        }
+    }
+    if (maxima != nullptr) {
+        uint16_t *const row = maxima + (long long)blockIdx.x * n.k_pad;
+        if constexpr (W == 1) {
+            uint4 *const top = (uint4 *)lds;                     // [8 waves][64 C]
+#pragma unroll
+            for (int c = 0; c < C; ++c) top[(tid >> 6) * 64 * C + c * 64 + t] = most[c];
+            __syncthreads();
+            for (int i = tid; i < 64 * C && i * 8 < n.k_pad; i += 512) {
+                uint4 x = top[i];
+#pragma unroll
+                for (int y = 1; y < 8; ++y) x = absmax_step(x, top[y * 64 * C + i]);
+                *(uint4 *)(row + i * 8) = x;
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (at[c] < n.k_pad) *(uint4 *)(row + at[c]) = most[c];
+        }
+    }
 }
 
-__global__ __launch_bounds__(256) void k_maxima(const uint16_t *y, int rows, int K, int ldy, int k_pad, uint16_t *slabs)
+// Rows of maxima folded into one: 8 runs of 8 channels to a workgroup, 32 threads down each.
+__global__ __launch_bounds__(256) void k_norm_fold(const uint16_t *maxima, int rows, int k_pad, uint16_t *slab)
 {
-    const int k = blockIdx.x * 256 + threadIdx.x;
-    if (k >= k_pad) return;
-    uint16_t top = 0;
-    if (k < K)
-        for (int m = blockIdx.y * rows; m < (blockIdx.y + 1) * rows; ++m) top = max(top, (uint16_t)(y[(long long)m * ldy + k] & 0x7fff));
-    slabs[(long long)blockIdx.y * k_pad + k] = top;
+    __shared__ uint4 top[256];
+    const int c = (blockIdx.x * 8 + (threadIdx.x & 7)) * 8;
+    uint4 x = {0, 0, 0, 0};
+    if (c < k_pad)
+        for (int m = threadIdx.x >> 3; m < rows; m += 32) x = absmax_step(x, *(const uint4 *)(maxima + (long long)m * k_pad + c));
+    top[threadIdx.x] = x;
+    __syncthreads();
+    if (threadIdx.x < 8 && c < k_pad) {
+        for (int i = 1; i < 32; ++i) x = absmax_step(x, top[i * 8 + threadIdx.x]);
+        *(uint4 *)(slab + c) = x;
+    }
+}
+
+// Waves to a row.
+int waves_of(int M, int K) { return K > 8192 ? 16 : K > 2048 || M < 2048 ? 4 : 1; }
+
+int groups_of(int M, int K)
+{
+    const int rows = waves_of(M, K) == 1 ? 8 : 1, need = (M + rows - 1) / rows;
+    return need < kMaxGroups ? need : kMaxGroups;
+}
+
+template <int W, int C>
+hipError_t launch(const NormArgs &n, bool rms, uint16_t *maxima, hipStream_t s)
+{
+    const dim3 grid(maxima ? groups_of(n.M, n.K) : W == 1 ? (n.M + 7) / 8 : n.M), block(64 * (W == 1 ? 8 : W));
+    const size_t lds = W == 1 && maxima ? (size_t)8 * 64 * C * 16 : 0;
+    return rms ? launch_kernel(k_norm<W, C, true>, grid, block, lds, s, n, maxima) : launch_kernel(k_norm<W, C, false>, grid, block, lds, s, n, maxima);
 }
 
 }  // namespace
 
 int norm_slab_rows(int M) { return M <= 64 ? M : 1; }
 
-size_t norm_scratch_bytes(int, int, int) { return 0; }
+size_t norm_scratch_bytes(int M, int K, int k_pad) { return M <= 64 ? 0 : (size_t)groups_of(M, K) * k_pad * 2; }
 
 hipError_t launch_norm(const NormArgs &n, bool rms, hipStream_t s)
 {
-    const size_t lds = (size_t)n.K * 4;
+    uint16_t *const maxima = n.slabs && n.M > 64 ? n.scratch : nullptr;
+    const int W = waves_of(n.M, n.K), C = (n.k_pad + 512 * W - 1) / (512 * W);
     hipError_t e;
-    if (lds > 60 * 1024) {
-        if ((e = hipFuncSetAttribute((const void *)(rms ? k_norm<true> : k_norm<false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) != hipSuccess)
-            return e;
-    }
-    e = rms ? launch_kernel(k_norm<true>, dim3(n.M), dim3(256), lds, s, n) : launch_kernel(k_norm<false>, dim3(n.M), dim3(256), lds, s, n);
-    if (e != hipSuccess || n.slabs == nullptr) return e;
-    const int rows = norm_slab_rows(n.M);
-    return launch_kernel(k_maxima, dim3((n.k_pad + 255) / 256, rows), dim3(256), 0, s, (const uint16_t *)n.y, n.M / rows, n.K, n.ldy, n.k_pad, n.slabs);
+    if (W == 1)
+        e = C == 1 ? launch<1, 1>(n, rms, maxima, s) : C == 2 ? launch<1, 2>(n, rms, maxima, s) : C == 3 ? launch<1, 3>(n, rms, maxima, s) : launch<1, 4>(n, rms, maxima, s);
+    else if (W == 4)
+        e = C == 1 ? launch<4, 1>(n, rms, maxima, s) : C == 2 ? launch<4, 2>(n, rms, maxima, s) : C == 3 ? launch<4, 3>(n, rms, maxima, s) : launch<4, 4>(n, rms, maxima, s);
+    else
+        e = C <= 2 ? launch<16, 2>(n, rms, maxima, s) : launch<16, 4>(n, rms, maxima, s);
+    if (e != hipSuccess || maxima == nullptr) return e;
+    return launch_kernel(k_norm_fold, dim3((n.k_pad + 63) / 64), dim3(256), 0, s, maxima, groups_of(n.M, n.K), n.k_pad, n.slabs);
 }
 
 }  // namespace muxq
