@@ -85,7 +85,8 @@ int muxq_kv_gather(const int32_t *slots, int M, const muxq_kv_cache *cache, void
  * Arithmetic: products of fp16 (codes are exact in fp16) with binary32 sums; the softmax weights enter
  * the second product as two 16-bit parts (see the kernel).
  * workspace: muxq_paged_attention_workspace_bytes(...) bytes, 256-byte aligned, content undefined on
- * entry; NULL where that is 0.  Calls that share one must not overlap in time. */
+ * entry; enough for every call with S and max_length no larger; NULL where that is 0.  Calls that share one
+ * must not overlap in time. */
 size_t muxq_paged_attention_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_length);
 int muxq_paged_attention(const void *Q_fp16, int S, int n_heads, int ldq, const muxq_kv_cache *cache,
                          const int32_t *block_table, int ld_table, const int32_t *lengths, int max_length,

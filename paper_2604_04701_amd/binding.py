@@ -558,30 +558,33 @@ NORM_LAYER, NORM_RMS = 0, 1
 _NORM = {"layer": NORM_LAYER, "rms": NORM_RMS, NORM_LAYER: NORM_LAYER, NORM_RMS: NORM_RMS}
 
 
-def _want(ok, what):
-    if not ok:
-        raise MuxqError(what)
+_F16, _F32, _I8, _I32 = torch.float16, torch.float32, torch.int8, torch.int32
 
 
-def _rows(t, name, dtype=torch.float16):
+# (Messages are put together only where a check fails: a call of a few microseconds has a dozen checks.)
+def _refuse(what):
+    raise MuxqError(what)
+
+
+def _rows(t, name):
     """t: [rows, heads, d] or [rows, width] of fp16 whose rows are contiguous; returns its row stride."""
     st = t.stride()
-    _want(t.dtype == dtype and t.is_cuda and st[-1] == 1 and (t.dim() == 2 or (t.dim() == 3 and (st[1] == t.shape[2] or t.shape[1] == 1))),
-          f"{name}: a GPU tensor of {dtype} with contiguous rows is expected")
+    if t.dtype is not _F16 or not t.is_cuda or st[-1] != 1 or (len(st) == 3 and st[1] != t.shape[2] and t.shape[1] != 1):
+        _refuse(f"{name}: a GPU tensor of fp16 with contiguous rows is expected")
     return st[0]
 
 
 def _ints(t, n, name):
-    _want(t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and t.numel() >= n,
-          f"{name}: a contiguous int32 GPU tensor of at least {n} entries is expected")
+    if t.dtype is not _I32 or not t.is_cuda or t.numel() < n or not t.is_contiguous():
+        _refuse(f"{name}: a contiguous int32 GPU tensor of at least {n} entries is expected")
     return t.data_ptr()
 
 
-def _vector(t, n, name, dtype=torch.float16):
+def _vector(t, n, name, dtype=_F16):
     if t is None:
         return None
-    _want(t.dtype == dtype and t.is_cuda and t.is_contiguous() and t.numel() == n,
-          f"{name}: a contiguous GPU tensor of {n} {dtype} is expected")
+    if t.dtype is not dtype or not t.is_cuda or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{name}: a contiguous GPU tensor of {n} {dtype} is expected")
     return t.data_ptr()
 
 
@@ -589,26 +592,27 @@ def _kv(k_cache, v_cache, k_scale, v_scale):
     """The descriptor of a cache given as tensors [pages, heads, tokens of a page, d]: views of any
     strides with contiguous d (transpose a [pages, tokens, heads, d] tensor), fp16 or int8, the latter with scales
     [pages, heads, tokens of a page]."""
-    n, heads, block, d = k_cache.shape
-    lb, lh, lt, one = k_cache.stride()
-    _want(one == 1 and k_cache.is_cuda and v_cache.is_cuda and v_cache.shape == k_cache.shape and
-          v_cache.stride() == k_cache.stride() and v_cache.dtype == k_cache.dtype,
-          "cache: keys and values are GPU tensors of one shape, type and order, with contiguous head dimensions")
-    c = KvCache(k_cache.data_ptr(), v_cache.data_ptr(), None, None, 0, n, block, heads, d, 0, lb, lh, lt)
-    if k_cache.dtype == torch.int8:
-        _want(k_scale is not None and v_scale is not None, "cache: 8-bit codes come with k_scale and v_scale")
-        c.type = 1
-        c.k_scale = _vector(k_scale, n * heads * block, "k_scale", torch.float32)
-        c.v_scale = _vector(v_scale, n * heads * block, "v_scale", torch.float32)
-    else:
-        _want(k_cache.dtype == torch.float16 and k_scale is None and v_scale is None,
-              "cache: fp16 without scales, or int8 with them")
+    shape, strides, dtype = k_cache.shape, k_cache.stride(), k_cache.dtype
+    if v_cache.shape != shape or v_cache.stride() != strides or v_cache.dtype is not dtype or not k_cache.is_cuda or not v_cache.is_cuda:
+        _refuse("cache: keys and values are GPU tensors of one shape, type and order")
+    n, heads, block, d = shape
+    lb, lh, lt, one = strides
+    if one != 1:
+        _refuse("cache: head dimensions are contiguous")
     # a dimension of one element may carry any stride
     if heads == 1:
-        c.ld_head = (lt * block + 15) // 16 * 16
+        lh = (lt * block + 15) // 16 * 16
     if n == 1:
-        c.ld_block = max(lb, (block - 1) * lt + (heads - 1) * c.ld_head + d + 15) // 16 * 16
-    return c
+        lb = max(lb, (block - 1) * lt + (heads - 1) * lh + d + 15) // 16 * 16
+    if dtype is _I8:
+        if k_scale is None or v_scale is None:
+            _refuse("cache: 8-bit codes come with k_scale and v_scale")
+        scales = n * heads * block
+        return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), _vector(k_scale, scales, "k_scale", _F32),
+                       _vector(v_scale, scales, "v_scale", _F32), 1, n, block, heads, d, 0, lb, lh, lt)
+    if dtype is not _F16 or k_scale is not None or v_scale is not None:
+        _refuse("cache: fp16 without scales, or int8 with them")
+    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), None, None, 0, n, block, heads, d, 0, lb, lh, lt)
 
 
 def alloc_kv_cache(n_blocks, block_size, n_kv_heads, head_dim, dtype=torch.float16, device="cuda"):
@@ -628,18 +632,21 @@ def muxq_kv_append(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, q=
     ranges of one tensor.  Returns q_out (made when not given; None without q)."""
     M, heads, d = k.shape
     c = _kv(k_cache, v_cache, k_scale, v_scale)
-    _want(v.shape == k.shape and heads == c.n_kv_heads and d == c.head_dim, "muxq_kv_append: k, v and the cache differ in heads")
+    if not (v.shape == k.shape and heads == c.n_kv_heads and d == c.head_dim):
+        _refuse("muxq_kv_append: k, v and the cache differ in heads")
     n_heads = ldq = ldqo = 0
     if q is not None:
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
         n_heads = q.shape[1]
-        _want(q.shape == (M, n_heads, d) and q_out.shape == q.shape, "muxq_kv_append: q and k differ in tokens or head size")
+        if not (q.shape == (M, n_heads, d) and q_out.shape == q.shape):
+            _refuse("muxq_kv_append: q and k differ in tokens or head size")
         ldq, ldqo = _rows(q, "q"), _rows(q_out, "q_out")
     n_pos = rot = 0
     if cos_sin is not None:
         n_pos, rot = cos_sin.shape
-        _want(positions is not None, "muxq_kv_append: cos_sin comes with positions")
+        if not (positions is not None):
+            _refuse("muxq_kv_append: cos_sin comes with positions")
     _check(lib().muxq_kv_append(_p(k), _p(v), M, _rows(k, "k"), _rows(v, "v"), _p(q), n_heads, ldq, _p(q_out), ldqo,
                                 _ints(slots, M, "slots"), None if positions is None else _ints(positions, M, "positions"),
                                 _vector(cos_sin, n_pos * rot, "cos_sin", torch.float32), n_pos, rot,
@@ -655,7 +662,8 @@ def muxq_kv_gather(slots, k_cache, v_cache, k_scale=None, v_scale=None, k_out=No
         k_out = torch.empty(shape, dtype=torch.float16, device=k_cache.device)
     if v_out is None:
         v_out = torch.empty(shape, dtype=torch.float16, device=k_cache.device)
-    _want(k_out.shape == shape and v_out.shape == shape, f"muxq_kv_gather: outputs of shape {shape} are expected")
+    if not (k_out.shape == shape and v_out.shape == shape):
+        _refuse(f"muxq_kv_gather: outputs of shape {shape} are expected")
     _check(lib().muxq_kv_gather(_ints(slots, shape[0], "slots"), shape[0], C.byref(c), _p(k_out), _rows(k_out, "k_out"),
                                 _p(v_out), _rows(v_out, "v_out"), _stream()), "muxq_kv_gather")
     return k_out, v_out
@@ -680,12 +688,14 @@ def muxq_paged_attention(q, k_cache, v_cache, block_table, lengths, max_length, 
     c = _kv(k_cache, v_cache, k_scale, v_scale)
     if out is None:
         out = torch.empty((S, n_heads, d), dtype=torch.float16, device=q.device)
-    _want(d == c.head_dim and out.shape == q.shape, "muxq_paged_attention: q, out and the cache differ in head size")
-    _want(block_table.dtype == torch.int32 and block_table.is_cuda and block_table.shape[0] == S and block_table.stride(1) == 1,
-          "muxq_paged_attention: block_table is an int32 GPU tensor [S, pages] with contiguous rows")
+    if not (d == c.head_dim and out.shape == q.shape):
+        _refuse("muxq_paged_attention: q, out and the cache differ in head size")
+    if not (block_table.dtype == torch.int32 and block_table.is_cuda and block_table.shape[0] == S and block_table.stride(1) == 1):
+        _refuse("muxq_paged_attention: block_table is an int32 GPU tensor [S, pages] with contiguous rows")
     if workspace is None:
         workspace = alloc_attention_workspace(S, n_heads, c.n_kv_heads, d, max_length, q.device)
-    _want(max_length <= block_table.shape[1] * c.block_size, "muxq_paged_attention: max_length goes beyond the block table")
+    if not (max_length <= block_table.shape[1] * c.block_size):
+        _refuse("muxq_paged_attention: max_length goes beyond the block table")
     _check(lib().muxq_paged_attention(_p(q), S, n_heads, _rows(q, "q"), C.byref(c), _p(block_table),
                                       block_table.stride(0) if S > 1 else block_table.shape[1], _ints(lengths, S, "lengths"),
                                       max_length, d ** -0.5 if scale is None else scale, _p(out), _rows(out, "out"),
@@ -704,7 +714,8 @@ def muxq_lora(X, A, B, scales, starts, adapters, Y, out=None):
     requests = adapters.numel()
     if out is None:
         out = torch.empty((M, N), dtype=torch.float16, device=X.device)
-    _want(k == K and B.shape == (n, N, r) and Y.shape[0] == M and out.shape == (M, N), "muxq_lora: shapes of X, A, B, Y and out do not fit")
+    if not (k == K and B.shape == (n, N, r) and Y.shape[0] == M and out.shape == (M, N)):
+        _refuse("muxq_lora: shapes of X, A, B, Y and out do not fit")
     _check(lib().muxq_lora(_p(X), M, K, _rows(X, "X"), _vector(A, n * r * K, "A"), _vector(B, n * N * r, "B"),
                            _vector(scales, n, "scales", torch.float32), n, r, _ints(starts, requests + 1, "starts"),
                            _ints(adapters, requests, "adapters"), requests, _p(Y), _rows(Y, "Y"), N, _p(out),
@@ -735,15 +746,17 @@ def muxq_norm(x, weight, bias=None, residual=None, residual_scale=1.0, post_weig
     if residual_out is None and (residual is not None or gate is not None or post_weight is not None):
         residual_out = torch.empty((M, K), dtype=torch.float16, device=x.device)
     if slabs is not None:
-        _want(slabs.is_cuda and slabs.is_contiguous() and
-              slabs.numel() * slabs.element_size() >= norm_slabs(M, K) * k_pad(K) * 2, "muxq_norm: slabs are too small")
+        if not (slabs.is_cuda and slabs.is_contiguous() and slabs.numel() * slabs.element_size() >= norm_slabs(M, K) * k_pad(K) * 2):
+            _refuse("muxq_norm: slabs are too small")
         if scratch is None:
             scratch = alloc_norm_scratch(M, K, x.device)
     for t, name in ((residual, "residual"), (out, "out"), (residual_out, "residual_out")):
-        _want(t is None or t.shape == x.shape, f"muxq_norm: {name} and x differ in shape")
+        if not (t is None or t.shape == x.shape):
+            _refuse(f"muxq_norm: {name} and x differ in shape")
     ldg = 0
     if gate is not None and gate.dim() == 2:
-        _want(gate.shape == x.shape, "muxq_norm: gate is [K] or [M, K]")
+        if not (gate.shape == x.shape):
+            _refuse("muxq_norm: gate is [K] or [M, K]")
         ldg = _rows(gate, "gate") if M > 1 else K
     elif gate is not None:
         _vector(gate, K, "gate")

@@ -24,7 +24,8 @@ typedef __fp16 fp16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32;               // tokens of a wave's step
-constexpr int kMaxChunk = kAttendMaxChunk;
+constexpr int kMaxChunk = kAttendMaxChunk, kMinChunk = 512;
+constexpr int kWorkgroups = 1024;      // to fill the chip, four on a CU
 constexpr float kFloor = -__builtin_inff();
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -359,9 +360,9 @@ int chunk_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
 {
     const int group = n_heads / n_kv_heads, subs = (group + heads_of(head_dim) - 1) / heads_of(head_dim);
     const long long base = (long long)S * n_kv_heads * subs;
-    const long long want = (1024 + base - 1) / base;                    // splits that give four workgroups a CU
+    const long long want = (kWorkgroups + base - 1) / base;             // splits that give four workgroups a CU
     const long long chunk = ((max_length + want - 1) / want + 255) / 256 * 256;
-    return (int)(chunk < 512 ? 512 : chunk > kMaxChunk ? kMaxChunk : chunk);
+    return (int)(chunk < kMinChunk ? kMinChunk : chunk > kMaxChunk ? kMaxChunk : chunk);
 }
 
 Split split_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
@@ -373,6 +374,11 @@ Split split_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
 }
 
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+size_t parts_bytes(size_t splits, int n_heads, int head_dim)
+{
+    return up256(splits * n_heads * head_dim * 4) + up256(splits * n_heads * 8);
+}
 
 template <int kD>
 hipError_t launch_d(const AttendArgs &a, const Split &sp, bool int8, hipStream_t s)
@@ -392,12 +398,23 @@ hipError_t launch_d(const AttendArgs &a, const Split &sp, bool int8, hipStream_t
 
 }  // namespace
 
-size_t attend_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
+// Of this call.
+size_t attend_workspace_need(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
 {
     const Split sp = split_of(S, n_heads, n_kv_heads, head_dim, max_length);
-    if (sp.n == 1) return 0;
-    const size_t parts = (size_t)S * n_heads * sp.n;
-    return up256(parts * head_dim * 4) + up256(parts * 8);
+    return sp.n == 1 ? 0 : parts_bytes((size_t)S * sp.n, n_heads, head_dim);
+}
+
+// Of this call and every smaller one (S and max_length): there are ceil(max_length / chunk) splits, at most `want` of
+// them unless the longest chunk forces more, and S want < 1024 / heads + S.
+size_t attend_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
+{
+    if (max_length <= kMinChunk) return 0;
+    const int group = n_heads / n_kv_heads, subs = (group + heads_of(head_dim) - 1) / heads_of(head_dim);
+    const size_t forced = (size_t)S * ((max_length + kMaxChunk - 1) / kMaxChunk), shortest = (size_t)S * ((max_length + kMinChunk - 1) / kMinChunk);
+    const size_t wanted = (size_t)(kWorkgroups / (n_kv_heads * subs)) + S;
+    const size_t most = shortest < wanted ? shortest : wanted;
+    return parts_bytes(forced > most ? forced : most, n_heads, head_dim);
 }
 
 hipError_t launch_attend(const AttendArgs &a, bool int8, hipStream_t s)

@@ -150,7 +150,7 @@ int muxq_paged_attention(const void *Q, int S, int n_heads, int ldq, const muxq_
     if (!(fabsf(scale) <= 3.4e38f)) return MUXQ_ERR_PARAM;
     if (!aligned(Q, 16) || !aligned(O, 16) || !aligned(block_table, 4) || !aligned(lengths, 4)) return MUXQ_ERR_ALIGN;
     if ((Q != O || ldq != ldo) && share(Q, ldq, (long long)n_heads * d, O, ldo, (long long)n_heads * d, S)) return MUXQ_ERR_PARAM;
-    const size_t need = muxq::attend_workspace_bytes(S, n_heads, a.c.n_kv_heads, d, max_length);
+    const size_t need = muxq::attend_workspace_need(S, n_heads, a.c.n_kv_heads, d, max_length);
     if (need > 0) {
         if (!workspace) return MUXQ_ERR_NULL;
         if (!aligned(workspace, 256)) return MUXQ_ERR_ALIGN;
