@@ -21,6 +21,7 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __fp16 fp16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32;               // tokens of a wave's step
@@ -60,12 +61,13 @@ struct Split {
 template <int kD>
 constexpr int kHeads = kD == 256 ? 8 : 16;
 
-template <int kD, bool kInt8, bool kFull>
-__global__ __launch_bounds__(256) void k_attend(AttendArgs a, Split sp)
+template <int kD, bool kInt8, bool kFull, int kWaves>
+__global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
 {
-    constexpr int NS = kD / 32, VE = kD / 16, VW = VE / 2;
-    extern __shared__ char lds[];
-    __shared__ float sh_m[4][16], sh_l[4][16], sh_cap[4];
+    constexpr int NS = kD / 32, VE = kD / 16, kThreads = 64 * kWaves;
+    constexpr int KW = kInt8 ? NS / 2 : NS, VW = kInt8 ? VE / 4 : VE / 2;      // 16-byte pieces of a key row, words of a value row
+    extern __shared__ __align__(16) char lds[];
+    __shared__ float sh_m[kWaves][16], sh_l[kWaves][16], sh_cap[kWaves];
     __shared__ int sh_bad;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
     const int subs = (a.group + kHeads<kD> - 1) / kHeads<kD>;
@@ -76,16 +78,16 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a, Split sp)
     const int t0 = split * sp.chunk, t1 = min(len, t0 + sp.chunk);
     if (t0 >= len) {
         if (sp.n == 1)                       // an idle place
-            for (int i = tid; i < n_here * d; i += 256) a.o[(long long)s * a.ldo + (long long)head0 * d + i] = (_Float16)0.0f;
+            for (int i = tid; i < n_here * d; i += kThreads) a.o[(long long)s * a.ldo + (long long)head0 * d + i] = (_Float16)0.0f;
         return;
     }
 
-    // where the pages of the chunk stand, in elements; -1: not in the cache
+    // where the pages of the chunk stand, in elements (with codes: their numbers); -1: not in the cache
     long long *const sh_off = (long long *)lds;
-    const int first = t0 >> shift, pages = ((t1 - 1) >> shift) - first + 1, room = (pages + 4);
+    const int first = t0 >> shift, pages = ((t1 - 1) >> shift) - first + 1, room = pages + 4;
     if (tid == 0) sh_bad = 0;
     __syncthreads();
-    for (int i = tid; i < room; i += 256) {
+    for (int i = tid; i < room; i += kThreads) {
         long long at = -1;
         if (i < pages) {
             const int page = a.table[(long long)s * a.ld_table + first + i];
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a, Split sp)
         sh_off[i] = at;
     }
 
-    // queries: column `col` of the right operand, the dimensions of the left one's order
+    // queries: column `col` of the right operand, the dimensions in the left one's order
     f16x8 q[NS];
     const _Float16 *qrow = a.q + (long long)s * a.ldq + (long long)(head0 + min(col, n_here - 1)) * d;
 #pragma unroll
@@ -112,109 +114,121 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a, Split sp)
     const float c = a.scale * 1.44269504088896f;
     float m = kFloor, l = 0.0f, cap = 0.0f, cap_inv = 0.0f;
     f32x4 o[VE] = {};
+    // what is on its way: keys of tokens 16 t + col, values of tokens 16 t + 4 g + i, and their scales
+    uint4 k[2][KW];
+    uint32_t v[8][VW];
+    float4 ks[2], vs[2];
 
-    auto tile = [&](auto masked_c, const int tok) {
+    auto is_masked = [&](int tok) { return any_bad || tok + kTile > t1; };
+    auto load_k = [&](auto masked_c, int tok) {
         constexpr bool kMasked = decltype(masked_c)::value;
-        uint32_t v[8][VW];
-        float ks[8], vs[8];
-        f16x8 k[2][NS];
-        bool k_there[2][4];                 // of the tokens whose scores the lane will hold
-        long long vat[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            // keys: row `col` of the left operand is token 16 t + col
-            const int kt = tok + 16 * t + col, kp = (kt >> shift) - first;
-            long long at = sh_off[kp];
-            if (kInt8) at = (kMasked && at < 0) ? -1 : at * a.c.ld_block + kvh * a.c.ld_head;
+            const int kt = tok + 16 * t + col;
+            long long at = sh_off[(kt >> shift) - first];
             const bool there = !kMasked || (at >= 0 && kt < t1);
-            const long long krow = there ? at + (kt & mask) * a.c.ld_token : 0;
-            if constexpr (!kInt8) {
+            if (kInt8) at = at * a.c.ld_block + kvh * a.c.ld_head;
+            const long long row = there ? at + (kt & mask) * a.c.ld_token : 0;
 #pragma unroll
-                for (int st = 0; st < NS; ++st) {
-                    k[t][st] = f16x8{};
-                    if (kFull || 32 * st + 8 * g < d) k[t][st] = *(const f16x8 *)((const _Float16 *)a.c.k + krow + 32 * st + 8 * g);
-                }
-            } else {
-#pragma unroll
-                for (int u = 0; u < NS / 2; ++u) {
-                    uint4 w = {0, 0, 0, 0};
-                    if (kFull || 64 * u + 16 * g < d) w = *(const uint4 *)(a.c.k + krow + 64 * u + 16 * g);
-                    uint32_t h[8];
-                    codes_to_half(w.x, h[0], h[1]);
-                    codes_to_half(w.y, h[2], h[3]);
-                    codes_to_half(w.z, h[4], h[5]);
-                    codes_to_half(w.w, h[6], h[7]);
-                    k[t][2 * u] = half8(h[0], h[1], h[2], h[3]);
-                    k[t][2 * u + 1] = half8(h[4], h[5], h[6], h[7]);
-                }
+            for (int u = 0; u < KW; ++u) {
+                const int e = kInt8 ? 64 * u + 16 * g : 32 * u + 8 * g;
+                k[t][u] = uint4{0, 0, 0, 0};
+                if (kFull || e < d) k[t][u] = *(const uint4 *)(a.c.k + (row + e) * (kInt8 ? 1 : 2));
             }
-            // values and scores: the lane's tokens are 16 t + 4 g + 0..3, in one page
-            const int vt = tok + 16 * t + 4 * g, vp = (vt >> shift) - first;
-            const long long page = sh_off[vp];
-            vat[t] = kInt8 ? page * a.c.ld_block + kvh * a.c.ld_head : page;
+        }
+    };
+    auto load_v = [&](auto masked_c, int tok) {
+        constexpr bool kMasked = decltype(masked_c)::value;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) k_there[t][i] = !kMasked || (page >= 0 && vt + i < t1);
+        for (int t = 0; t < 2; ++t) {
+            // the lane's tokens are 16 t + 4 g + 0..3, in one page
+            const int vt = tok + 16 * t + 4 * g;
+            const long long page = sh_off[(vt >> shift) - first];
+            const long long at = kInt8 ? page * a.c.ld_block + kvh * a.c.ld_head : page;
             if constexpr (kInt8) {
                 const long long at_s = (kMasked && page < 0) ? 0 : ((page * a.c.n_kv_heads + kvh) << shift) + (vt & mask);
-                const float4 ks4 = *(const float4 *)(a.c.k_scale + at_s), vs4 = *(const float4 *)(a.c.v_scale + at_s);
-                const float kk[4] = {ks4.x, ks4.y, ks4.z, ks4.w}, vv[4] = {vs4.x, vs4.y, vs4.z, vs4.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ks[4 * t + i] = kk[i] * c, vs[4 * t + i] = k_there[t][i] ? vv[i] : 0.0f;
+                ks[t] = *(const float4 *)(a.c.k_scale + at_s);
+                vs[t] = *(const float4 *)(a.c.v_scale + at_s);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const long long row = k_there[t][i] ? vat[t] + ((vt & mask) + i) * a.c.ld_token + VE * col : 0;
+                const bool there = !kMasked || (page >= 0 && vt + i < t1);
+                const char *p = a.c.v + (there ? at + ((vt & mask) + i) * a.c.ld_token + VE * col : 0) * (kInt8 ? 1 : 2);
                 uint32_t *w = v[4 * t + i];
 #pragma unroll
                 for (int x = 0; x < VW; ++x) w[x] = 0;
                 if (kFull || VE * col < d) {
-                    if constexpr (!kInt8) {
-                        const _Float16 *p = (const _Float16 *)a.c.v + row;
-                        if constexpr (VE == 4) {
-                            const uint2 x = *(const uint2 *)p;
-                            w[0] = x.x, w[1] = x.y;
-                        } else {
-#pragma unroll
-                            for (int x = 0; x < VE / 8; ++x) {
-                                const uint4 y = *(const uint4 *)(p + 8 * x);
-                                w[4 * x] = y.x, w[4 * x + 1] = y.y, w[4 * x + 2] = y.z, w[4 * x + 3] = y.w;
-                            }
-                        }
+                    if constexpr (VW == 1) {
+                        w[0] = *(const uint32_t *)p;
+                    } else if constexpr (VW == 2) {
+                        const uint2 y = *(const uint2 *)p;
+                        w[0] = y.x, w[1] = y.y;
                     } else {
-                        const char *p = a.c.v + row;
-                        if constexpr (VE == 4) {
-                            codes_to_half(*(const uint32_t *)p, w[0], w[1]);
-                        } else if constexpr (VE == 8) {
-                            const uint2 x = *(const uint2 *)p;
-                            codes_to_half(x.x, w[0], w[1]);
-                            codes_to_half(x.y, w[2], w[3]);
-                        } else {
-                            const uint4 x = *(const uint4 *)p;
-                            codes_to_half(x.x, w[0], w[1]);
-                            codes_to_half(x.y, w[2], w[3]);
-                            codes_to_half(x.z, w[4], w[5]);
-                            codes_to_half(x.w, w[6], w[7]);
+#pragma unroll
+                        for (int x = 0; x < VW / 4; ++x) {
+                            const uint4 y = ((const uint4 *)p)[x];
+                            w[4 * x] = y.x, w[4 * x + 1] = y.y, w[4 * x + 2] = y.z, w[4 * x + 3] = y.w;
                         }
                     }
                 }
-                if (kMasked && !k_there[t][i]) {
+                if (kMasked && !there) {          // what stands there may be NaN: its weight of 0 does not clear it
 #pragma unroll
                     for (int x = 0; x < VW; ++x) w[x] = 0;
                 }
             }
         }
+    };
+    auto ask_k = [&](int tok) {
+        if (is_masked(tok)) load_k(std::true_type{}, tok); else load_k(std::false_type{}, tok);
+    };
+    auto ask_v = [&](int tok) {
+        if (is_masked(tok)) load_v(std::true_type{}, tok); else load_v(std::false_type{}, tok);
+    };
 
+    // The keys of the next step are requested when this step's are in the matrix pipes, its values when this step's are: the
+    // same registers, and something is always on its way.
+    int tok = t0 + wave * kTile;
+    if (tok < t1) {
+        ask_k(tok);
+        ask_v(tok);
+    }
+    for (; tok < t1; tok += kWaves * kTile) {
+        const int next = tok + kWaves * kTile;
         f32x4 acc[2] = {};
 #pragma unroll
-        for (int st = 0; st < NS; ++st) {
-            acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[0][st], q[st], acc[0], 0, 0, 0);
-            acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[1][st], q[st], acc[1], 0, 0, 0);
-        }
-        float p[8];
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            p[j] = acc[j >> 2][j & 3] * (kInt8 ? ks[j] : c);
-            if (kMasked && !k_there[j >> 2][j & 3]) p[j] = kFloor;
+            for (int u = 0; u < KW; ++u) {
+                if constexpr (!kInt8) {
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, k[t][u]), q[u], acc[t], 0, 0, 0);
+                } else {
+                    uint32_t h[8];
+                    codes_to_half(k[t][u].x, h[0], h[1]);
+                    codes_to_half(k[t][u].y, h[2], h[3]);
+                    codes_to_half(k[t][u].z, h[4], h[5]);
+                    codes_to_half(k[t][u].w, h[6], h[7]);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(h[0], h[1], h[2], h[3]), q[2 * u], acc[t], 0, 0, 0);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(h[4], h[5], h[6], h[7]), q[2 * u + 1], acc[t], 0, 0, 0);
+                }
+            }
+        if (next < t1) ask_k(next);
+
+        float p[8], w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = acc[j >> 2][j & 3] * c;
+        if constexpr (kInt8) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                p[4 * t] *= ks[t].x, p[4 * t + 1] *= ks[t].y, p[4 * t + 2] *= ks[t].z, p[4 * t + 3] *= ks[t].w;
+                w[4 * t] = vs[t].x, w[4 * t + 1] = vs[t].y, w[4 * t + 2] = vs[t].z, w[4 * t + 3] = vs[t].w;
+            }
+        }
+        if (is_masked(tok)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int kt = tok + 16 * (j >> 2) + 4 * g + (j & 3);
+                if (kt >= t1 || sh_off[(kt >> shift) - first] < 0) p[j] = kFloor, w[j] = 0.0f;
+            }
         }
         float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
         if (__any(top > m + 7.0f)) {                    // rare after the first steps: a new maximum for the head
@@ -231,7 +245,7 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a, Split sp)
         for (int j = 0; j < 8; ++j) p[j] = exp2_(p[j] + off);
         l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
         if constexpr (kInt8) {
-            float most = fmaxf(fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])), fmaxf(fmaxf(vs[4], vs[5]), fmaxf(vs[6], vs[7])));
+            float most = fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
             if (__any(most > cap)) {                    // scales of values over a power of two
                 most = fmaxf(most, __shfl_xor(most, 16, 64));
                 most = fmaxf(most, __shfl_xor(most, 32, 64));
@@ -244,7 +258,7 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a, Split sp)
                 for (int e = 0; e < VE; ++e) o[e] *= keep;
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] *= vs[j] * cap_inv;
+            for (int j = 0; j < 8; ++j) p[j] *= w[j] * cap_inv;
         }
         uint32_t hi[4], lo[4];
 #pragma unroll
@@ -257,121 +271,156 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a, Split sp)
         const f16x8 ph = half8(hi[0], hi[1], hi[2], hi[3]), pl = half8(lo[0], lo[1], lo[2], lo[3]);
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
-            const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
-            uint32_t t[4];
+            uint32_t x[4];
+            if constexpr (!kInt8) {
+                const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) t[j] = __builtin_amdgcn_perm(v[2 * j + 1][e >> 1], v[2 * j][e >> 1], sel);
-            const f16x8 vt = half8(t[0], t[1], t[2], t[3]);
+                for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_perm(v[2 * j + 1][e >> 1], v[2 * j][e >> 1], sel);
+            } else {
+                // byte e of the words of two tokens and two more, then as codes_to_half
+                const uint32_t sel = 0x0c0c0400u + 0x0101u * (e & 3);
+                uint32_t y[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    y[j] = __builtin_amdgcn_perm(v[4 * j + 1][e >> 2], v[4 * j][e >> 2], sel) |
+                           (__builtin_amdgcn_perm(v[4 * j + 3][e >> 2], v[4 * j + 2][e >> 2], sel) << 16);
+                codes_to_half(y[0], x[0], x[1]);
+                codes_to_half(y[1], x[2], x[3]);
+            }
+            const f16x8 vt = half8(x[0], x[1], x[2], x[3]);
             o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, ph, o[e], 0, 0, 0);
             o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, pl, o[e], 0, 0, 0);
         }
-    };
-    for (int tok = t0 + wave * kTile; tok < t1; tok += 4 * kTile) {
-        if (any_bad || tok + kTile > t1)
-            tile(std::true_type{}, tok);
-        else
-            tile(std::false_type{}, tok);
+        if (next < t1) ask_v(next);
     }
 
-    // the four waves' parts: m and l by head, o as [wave][head][d]
+    // The waves' parts: m and l by head, then sum_w 2^(m_w - max m) o_w in LDS, [wave][head][d], the upper half of the waves
+    // through the lower one's places.
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
-    __syncthreads();
-    float *const sh_o = (float *)lds;
     if (lane < 16) sh_m[wave][lane] = m, sh_l[wave][lane] = l;
-    if (lane == 0) sh_cap[wave] = kInt8 ? cap : 1.0f;
-    if (col < n_here) {
-        float *row = sh_o + (wave * n_here + col) * kD;
+    __syncthreads();
+    float top = sh_m[0][col];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh_m[w][col]);
+    const float f = weight_of(m, l, top) * (kInt8 ? cap : 1.0f);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) o[e] *= f;
+    float *const sh_o = (float *)lds;
+    float *const mine = sh_o + ((wave & 3) * n_here + col) * kD;
+    auto put = [&](bool add) {
+        if (col >= n_here) return;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < VE; e += 4) *(f32x4 *)(row + VE * (4 * g + i) + e) = f32x4{o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]};
+            for (int e = 0; e < VE; e += 4) {
+                f32x4 *at = (f32x4 *)(mine + VE * (4 * g + i) + e);
+                f32x4 x = {o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]};
+                if (add) x += *at;
+                *at = x;
+            }
+    };
+    if constexpr (kWaves == 8) {
+        if (wave >= 4) put(false);
+        __syncthreads();
+        if (wave < 4) put(true);
+    } else {
+        put(false);
     }
     __syncthreads();
-    for (int i = tid; i < n_here * (kD / 4); i += 256) {
+    for (int i = tid; i < n_here * (kD / 4); i += kThreads) {
         const int h = i / (kD / 4), e = (i - h * (kD / 4)) * 4;
         if (!kFull && e >= d) continue;
-        const float top = fmaxf(fmaxf(sh_m[0][h], sh_m[1][h]), fmaxf(sh_m[2][h], sh_m[3][h]));
-        f32x4 sum = {};
-        float all = 0.0f;
+        float most = sh_m[0][h], all = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = weight_of(sh_m[w][h], sh_l[w][h], top);
-            all += f * sh_l[w][h];
-            sum += (f * sh_cap[w]) * *(const f32x4 *)(sh_o + (w * n_here + h) * kD + e);
-        }
+        for (int w = 1; w < kWaves; ++w) most = fmaxf(most, sh_m[w][h]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all += weight_of(sh_m[w][h], sh_l[w][h], most) * sh_l[w][h];
+        f32x4 sum = {};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) sum += *(const f32x4 *)(sh_o + (w * n_here + h) * kD + e);
         if (sp.n == 1) {
-            typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-            const float inv = top == kFloor ? 0.0f : 1.0f / all;
-            h4 r;
+            const float inv = most == kFloor ? 0.0f : 1.0f / all;
+            f16x4 r;
 #pragma unroll
             for (int x = 0; x < 4; ++x) r[x] = (_Float16)(sum[x] * inv);
-            *(h4 *)(a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e) = r;
+            *(f16x4 *)(a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e) = r;
         } else {
             const long long part = ((long long)s * a.n_heads + head0 + h) * sp.n + split;
             *(f32x4 *)(sp.o + part * d + e) = sum;
-            if (e == 0) sp.ml[part] = make_float2(top, all);
+            if (e == 0) sp.ml[part] = make_float2(most, all);
         }
     }
 }
 
 // The splits of a sequence and head joined, with weights 2^(m - max m): a thread four dimensions of every
-// (256 / (d / 4))th split.
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, Split sp)
+// (512 / (d / 4))th split, its first eight requested before the weights are known.
+__global__ __launch_bounds__(512) void k_attend_join(AttendArgs a, Split sp)
 {
-    __shared__ float red[8];
-    __shared__ f32x4 part[256];
+    __shared__ float red[16], weight[512];
+    __shared__ f32x4 part[512];
     const int tid = threadIdx.x, h = blockIdx.x, s = blockIdx.y, d = a.c.head_dim;
     const int len = min(a.lengths[s], a.max_length), n = len <= 0 ? 0 : (len + sp.chunk - 1) / sp.chunk;
     const long long row = ((long long)s * a.n_heads + h) * sp.n;
     const float2 *const ml = sp.ml + row;
-    float top = kFloor;
-    for (int i = tid; i < n; i += 256) top = fmaxf(top, ml[i].x);
-    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+    const int lanes = d / 4, per = 512 / lanes, mine = tid / lanes, e = (tid - mine * lanes) * 4;
+    const float *const o = sp.o + row * d + e;
+    f32x4 early[8] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (mine < per && mine + i * per < n) early[i] = *(const f32x4 *)(o + (long long)(mine + i * per) * d);
+    float2 x = make_float2(kFloor, 0.0f);
+    if (tid < n) x = ml[tid];
+    float top = x.x;
+    for (int i = tid + 512; i < n; i += 512) top = fmaxf(top, ml[i].x);
+    for (int y = 1; y < 64; y <<= 1) top = fmaxf(top, __shfl_xor(top, y, 64));
     if ((tid & 63) == 0) red[tid >> 6] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    float all = 0.0f;
-    for (int i = tid; i < n; i += 256) all += weight_of(ml[i].x, ml[i].y, top) * ml[i].y;
-    for (int x = 1; x < 64; x <<= 1) all += __shfl_xor(all, x, 64);
-    if ((tid & 63) == 0) red[4 + (tid >> 6)] = all;
-    const int lanes = d / 4, per = 256 / lanes, mine = tid / lanes, e = (tid - mine * lanes) * 4;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, red[w]);
+    weight[tid] = weight_of(x.x, x.y, top);
+    float all = weight[tid] * x.y;
+    for (int i = tid + 512; i < n; i += 512) all += weight_of(ml[i].x, ml[i].y, top) * ml[i].y;
+    for (int y = 1; y < 64; y <<= 1) all += __shfl_xor(all, y, 64);
+    if ((tid & 63) == 0) red[8 + (tid >> 6)] = all;
+    __syncthreads();
     f32x4 sum = {};
-    if (mine < per)
-        for (int i = mine; i < n; i += per) sum += weight_of(ml[i].x, ml[i].y, top) * *(const f32x4 *)(sp.o + (row + i) * d + e);
+    if (mine < per) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += weight[min(mine + i * per, 511)] * early[i];
+        for (int i = mine + 8 * per; i < n; i += per) sum += weight_of(ml[i].x, ml[i].y, top) * *(const f32x4 *)(o + (long long)i * d);
+    }
     part[tid] = sum;
     __syncthreads();
-    all = (red[4] + red[5]) + (red[6] + red[7]);
     if (tid < lanes) {
-        for (int i = 1; i < per; ++i) sum += part[i * lanes + tid];
-        typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-        const float inv = top == kFloor ? 0.0f : 1.0f / all;
-        h4 r;
+        all = 0.0f;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) r[x] = (_Float16)(sum[x] * inv);
-        *(h4 *)(a.o + (long long)s * a.ldo + (long long)h * d + e) = r;
+        for (int w = 0; w < 8; ++w) all += red[8 + w];
+        for (int i = 1; i < per; ++i) sum += part[i * lanes + tid];
+        const float inv = top == kFloor ? 0.0f : 1.0f / all;
+        f16x4 r;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) r[y] = (_Float16)(sum[y] * inv);
+        *(f16x4 *)(a.o + (long long)s * a.ldo + (long long)h * d + e) = r;
     }
 }
 
 int heads_of(int head_dim) { return head_dim > 128 ? kHeads<256> : kHeads<128>; }
 
-// Tokens of a workgroup.
-int chunk_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
+Split split_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
 {
     const int group = n_heads / n_kv_heads, subs = (group + heads_of(head_dim) - 1) / heads_of(head_dim);
     const long long base = (long long)S * n_kv_heads * subs;
-    const long long want = (kWorkgroups + base - 1) / base;             // splits that give four workgroups a CU
+    const long long want = (kWorkgroups + base - 1) / base;
     const long long chunk = ((max_length + want - 1) / want + 255) / 256 * 256;
-    return (int)(chunk < kMinChunk ? kMinChunk : chunk > kMaxChunk ? kMaxChunk : chunk);
-}
-
-Split split_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
-{
     Split sp{};
-    sp.chunk = chunk_of(S, n_heads, n_kv_heads, head_dim, max_length);
+    sp.chunk = (int)(chunk < kMinChunk ? kMinChunk : chunk > kMaxChunk ? kMaxChunk : chunk);
     sp.n = (int)(((long long)max_length + sp.chunk - 1) / sp.chunk);
     return sp;
 }
+
+// 8 waves where each has a step or more and their parts are worth joining in LDS.
+int waves_of(const Split &sp, int max_length) { return min(sp.chunk, max_length) > 256 ? 8 : 4; }
 
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
@@ -380,20 +429,26 @@ size_t parts_bytes(size_t splits, int n_heads, int head_dim)
     return up256(splits * n_heads * head_dim * 4) + up256(splits * n_heads * 8);
 }
 
-template <int kD>
-hipError_t launch_d(const AttendArgs &a, const Split &sp, bool int8, hipStream_t s)
+template <int kD, int kWaves>
+hipError_t launch_w(const AttendArgs &a, const Split &sp, bool int8, hipStream_t s)
 {
     const int subs = (a.group + kHeads<kD> - 1) / kHeads<kD>;
-    const dim3 grid(a.c.n_kv_heads * subs, sp.n, a.S);
+    const dim3 grid(a.c.n_kv_heads * subs, sp.n, a.S), block(64 * kWaves);
     const size_t offs = ((size_t)(sp.chunk >> a.c.block_shift) + 5) * 8;
     const size_t join = (size_t)4 * (a.group < kHeads<kD> ? a.group : kHeads<kD>) * kD * 4;
     const size_t lds = offs > join ? offs : join;
     const bool full = a.c.head_dim == kD;
     if (int8)
-        return full ? launch_kernel(k_attend<kD, true, true>, grid, dim3(256), lds, s, a, sp)
-                    : launch_kernel(k_attend<kD, true, false>, grid, dim3(256), lds, s, a, sp);
-    return full ? launch_kernel(k_attend<kD, false, true>, grid, dim3(256), lds, s, a, sp)
-                : launch_kernel(k_attend<kD, false, false>, grid, dim3(256), lds, s, a, sp);
+        return full ? launch_kernel(k_attend<kD, true, true, kWaves>, grid, block, lds, s, a, sp)
+                    : launch_kernel(k_attend<kD, true, false, kWaves>, grid, block, lds, s, a, sp);
+    return full ? launch_kernel(k_attend<kD, false, true, kWaves>, grid, block, lds, s, a, sp)
+                : launch_kernel(k_attend<kD, false, false, kWaves>, grid, block, lds, s, a, sp);
+}
+
+template <int kD>
+hipError_t launch_d(const AttendArgs &a, const Split &sp, bool int8, hipStream_t s)
+{
+    return waves_of(sp, a.max_length) == 8 ? launch_w<kD, 8>(a, sp, int8, s) : launch_w<kD, 4>(a, sp, int8, s);
 }
 
 }  // namespace
@@ -426,7 +481,7 @@ hipError_t launch_attend(const AttendArgs &a, bool int8, hipStream_t s)
     const int d = a.c.head_dim;
     hipError_t e = d <= 64 ? launch_d<64>(a, sp, int8, s) : d <= 128 ? launch_d<128>(a, sp, int8, s) : launch_d<256>(a, sp, int8, s);
     if (e != hipSuccess || sp.n == 1) return e;
-    return launch_kernel(k_attend_join, dim3(a.n_heads, a.S), dim3(256), 0, s, a, sp);
+    return launch_kernel(k_attend_join, dim3(a.n_heads, a.S), dim3(512), 0, s, a, sp);
 }
 
 }  // namespace muxq
