@@ -674,9 +674,8 @@ def attention_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_length) -> i
 
 
 def alloc_attention_workspace(S, n_heads, n_kv_heads, head_dim, max_length, device="cuda"):
-    """Workspace of muxq_paged_attention (also good for a smaller S or max_length); None where none is needed."""
-    n = attention_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_length)
-    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    """Workspace of muxq_paged_attention, also good for a smaller S or max_length (empty where none is needed)."""
+    return torch.empty(attention_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_length), dtype=torch.uint8, device=device)
 
 
 def muxq_paged_attention(q, k_cache, v_cache, block_table, lengths, max_length, scale=None, k_scale=None, v_scale=None,
@@ -699,8 +698,7 @@ def muxq_paged_attention(q, k_cache, v_cache, block_table, lengths, max_length, 
     _check(lib().muxq_paged_attention(_p(q), S, n_heads, _rows(q, "q"), C.byref(c), _p(block_table),
                                       block_table.stride(0) if S > 1 else block_table.shape[1], _ints(lengths, S, "lengths"),
                                       max_length, d ** -0.5 if scale is None else scale, _p(out), _rows(out, "out"),
-                                      _p(workspace), 0 if workspace is None else workspace.numel(), _stream()),
-           "muxq_paged_attention")
+                                      workspace.data_ptr(), workspace.numel(), _stream()), "muxq_paged_attention")
     return out
 
 
@@ -729,9 +727,8 @@ def norm_slabs(M: int, K: int) -> int:
 
 
 def alloc_norm_scratch(M, K, device="cuda"):
-    """Scratch of a muxq_norm call that hands maxima over; None where none is needed."""
-    n = lib().muxq_norm_scratch_bytes(M, K)
-    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    """Scratch of a muxq_norm call that hands maxima over (empty where none is needed)."""
+    return torch.empty(lib().muxq_norm_scratch_bytes(M, K), dtype=torch.uint8, device=device)
 
 
 def muxq_norm(x, weight, bias=None, residual=None, residual_scale=1.0, post_weight=None, post_bias=None, gate=None,

@@ -16,6 +16,8 @@
 // in fp16; the scale of a key goes to its score, the scale of a value to its weight, over a running power of two.
 #include "muxq_block_kernels.h"
 
+#include <algorithm>
+
 namespace muxq {
 namespace {
 
@@ -25,8 +27,10 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32;               // tokens of a wave's step
-constexpr int kMaxChunk = kAttendMaxChunk, kMinChunk = 512;
-constexpr int kWorkgroups = 1024;      // to fill the chip, four on a CU
+constexpr int kStep = 4 * kTile;        // tokens of a step of the 4 waves that have shares
+constexpr int kBegin = 1;               // what beginning a sequence and head costs, in steps
+constexpr int kPages = 4096;            // tokens whose pages stand in LDS at a time
+constexpr int kMaxSeqs = 2048;          // sequences whose steps a workgroup counts for itself
 constexpr float kFloor = -__builtin_inff();
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -47,56 +51,120 @@ __device__ __forceinline__ f16x8 half8(uint32_t a, uint32_t b, uint32_t c, uint3
     return __builtin_bit_cast(f16x8, u32x4{a, b, c, d});
 }
 
+// kOnce: of what nobody reads again before the memory-side cache has let it go.
+template <typename V, bool kOnce>
+__device__ __forceinline__ V load(const char *p)
+{
+    typedef uint32_t Word __attribute__((ext_vector_type(sizeof(V) / 4)));
+    return __builtin_bit_cast(V, kOnce ? __builtin_nontemporal_load((const Word *)p) : *(const Word *)p);
+}
+
 // 2^(m - top) of a part with maximum m and sum l; one without weights counts nothing, unless NaN stands there.
 __device__ __forceinline__ float weight_of(float m, float l, float top) { return m == kFloor ? l : exp2_(m - top); }
 
-struct Split {
-    int chunk;          // tokens of a workgroup, a multiple of 256
-    int n;              // splits of the longest sequence
-    float *o;           // [S][heads][n][d], unnormalised
-    float2 *ml;         // [S][heads][n]: m and the sum
+// How the work is divided.  groups == 0: a workgroup to a sequence and key-value head.  Otherwise `groups` workgroups
+// have equal shares of all steps (kStep tokens of one key-value head, and kBegin steps before the first) in the order
+// sequence, head, step (fewer workgroups where there are fewer steps);
+// a share that begins or ends inside a sequence and head leaves its part of it in the workspace: the first
+// piece of a share in slot 0, the last one in slot 1.
+struct Plan {
+    int groups;
+    bool once;          // more is read than the memory-side cache holds
+    float *o;           // [groups][2][heads of a workgroup][d], unnormalised
+    float2 *ml;         // [groups][2][heads of a workgroup]: m and the sum
+    int4 *open;         // [groups]: {sequence, pair, pieces, slot of the first} that the share leaves open, pieces 0: none
 };
 
 // Heads of one key-value head that a workgroup takes: the columns of the products, and what the joining in LDS holds.
 template <int kD>
 constexpr int kHeads = kD == 256 ? 8 : 16;
 
-template <int kD, bool kInt8, bool kFull, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
+template <int kD, bool kInt8, bool kFull, int kWaves, bool kShares>
+__global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 8 ? 2 : 1) void k_attend(AttendArgs a, Plan plan)
 {
     constexpr int NS = kD / 32, VE = kD / 16, kThreads = 64 * kWaves;
     constexpr int KW = kInt8 ? NS / 2 : NS, VW = kInt8 ? VE / 4 : VE / 2;      // 16-byte pieces of a key row, words of a value row
     extern __shared__ __align__(16) char lds[];
-    __shared__ float sh_m[kWaves][16], sh_l[kWaves][16], sh_cap[kWaves];
-    __shared__ int sh_bad;
+    __shared__ float sh_m[kWaves][16], sh_l[kWaves][16];
+    __shared__ int sh_bad, sh_sum[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
-    const int subs = (a.group + kHeads<kD> - 1) / kHeads<kD>;
-    const int kvh = blockIdx.x / subs, sub = blockIdx.x - kvh * subs, split = blockIdx.y, s = blockIdx.z;
-    const int head0 = kvh * a.group + sub * kHeads<kD>, n_here = min(kHeads<kD>, a.group - sub * kHeads<kD>);
+    const int subs = (a.group + kHeads<kD> - 1) / kHeads<kD>, pairs = a.c.n_kv_heads * subs;
     const int d = a.c.head_dim, shift = a.c.block_shift, mask = (1 << shift) - 1;
-    const int len = min(a.lengths[s], a.max_length);
-    const int t0 = split * sp.chunk, t1 = min(len, t0 + sp.chunk);
-    if (t0 >= len) {
-        if (sp.n == 1)                       // an idle place
-            for (int i = tid; i < n_here * d; i += kThreads) a.o[(long long)s * a.ldo + (long long)head0 * d + i] = (_Float16)0.0f;
-        return;
+    auto length_of = [&](int s) { return max(0, min(a.lengths[s], a.max_length)); };
+    auto steps_of = [&](int s) {
+        const int len = length_of(s);
+        return len > 0 ? kBegin + (len + kStep - 1) / kStep : 0;
+    };
+
+    // The share: steps [at, end), `at` being step j of `n` of sequence s and pair `pair`.  Steps before a
+    // sequence, of one pair, are counted in LDS.
+    int s = blockIdx.y, pair = blockIdx.x, j = 0, n = 0;
+    long long at = 0, end = 0;
+    int *const sh_before = (int *)lds;
+    char *const rest = lds + (kShares ? ((a.S + 4) / 4) * 16 : 0);
+    long long total = 0;
+    int groups = 0;
+    if constexpr (kShares) {
+        for (int i = blockIdx.x; i < a.S; i += plan.groups)             // idle places
+            if (a.lengths[i] <= 0)
+                for (int e = tid; e < a.n_heads * d; e += kThreads) a.o[(long long)i * a.ldo + e] = (_Float16)0.0f;
+        const int per = (a.S + kThreads - 1) / kThreads;
+        int sum = 0;
+        for (int i = tid * per; i < min(a.S, (tid + 1) * per); ++i) sum += steps_of(i);
+        int incl = sum;
+        for (int x = 1; x < 64; x <<= 1) {
+            const int y = __shfl_up(incl, x, 64);
+            if (lane >= x) incl += y;
+        }
+        if (lane == 63) sh_sum[wave] = incl;
+        __syncthreads();
+        int before = incl - sum, all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) before += sh_sum[w];
+            all += sh_sum[w];
+        }
+        for (int i = tid * per; i < min(a.S, (tid + 1) * per); ++i) {
+            sh_before[i] = before;
+            before += steps_of(i);
+        }
+        if (tid == 0) sh_before[a.S] = all;
+        __syncthreads();
+        total = (long long)all * pairs;
+        groups = (int)min((long long)plan.groups, total);      // every share has a step
+        if ((int)blockIdx.x >= groups) {
+            if (tid == 0) plan.open[blockIdx.x] = int4{0, 0, 0, 0};
+            return;
+        }
+        at = total * blockIdx.x / groups;
+        end = total * (blockIdx.x + 1) / groups;
+        int lo = 0, hi = a.S;                     // the last sequence whose steps begin at or before `at`
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            ((long long)sh_before[mid] * pairs <= at ? lo : hi) = mid;
+        }
+        s = lo;
+        n = sh_before[s + 1] - sh_before[s];      // (at least one: `at` lies in it)
+        const long long in = at - (long long)sh_before[s] * pairs;
+        pair = (int)(in / n);
+        j = (int)(in - (long long)pair * n);
     }
 
-    // where the pages of the chunk stand, in elements (with codes: their numbers); -1: not in the cache
-    long long *const sh_off = (long long *)lds;
-    const int first = t0 >> shift, pages = ((t1 - 1) >> shift) - first + 1, room = pages + 4;
-    if (tid == 0) sh_bad = 0;
-    __syncthreads();
-    for (int i = tid; i < room; i += kThreads) {
-        long long at = -1;
-        if (i < pages) {
-            const int page = a.table[(long long)s * a.ld_table + first + i];
-            if (page >= 0 && page < a.c.n_blocks)
-                at = kInt8 ? page : page * a.c.ld_block + kvh * a.c.ld_head;
-            else
-                sh_bad = 1;
-        }
-        sh_off[i] = at;
+    for (int piece = 0;; ++piece) {
+    const int kvh = pair / subs, sub = pair - kvh * subs;
+    const int head0 = kvh * a.group + sub * kHeads<kD>, n_here = min(kHeads<kD>, a.group - sub * kHeads<kD>);
+    const int len = length_of(s);
+    int t0 = 0, t1 = len;
+    bool whole = true;
+    if constexpr (kShares) {
+        const int steps = (int)min((long long)(n - j), end - at);
+        t0 = min(len, max(0, j - kBegin) * kStep);
+        t1 = min(len, max(0, j + steps - kBegin) * kStep);
+        whole = steps == n;
+        at += steps;
+    } else if (len == 0) {                       // an idle place
+        for (int i = tid; i < n_here * d; i += kThreads) a.o[(long long)s * a.ldo + (long long)head0 * d + i] = (_Float16)0.0f;
+        return;
     }
 
     // queries: column `col` of the right operand, the dimensions in the left one's order
@@ -104,12 +172,10 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
     const _Float16 *qrow = a.q + (long long)s * a.ldq + (long long)(head0 + min(col, n_here - 1)) * d;
 #pragma unroll
     for (int st = 0; st < NS; ++st) {
-        const int at = kInt8 ? 64 * (st >> 1) + 16 * g + 8 * (st & 1) : 32 * st + 8 * g;
+        const int e = kInt8 ? 64 * (st >> 1) + 16 * g + 8 * (st & 1) : 32 * st + 8 * g;
         q[st] = f16x8{};
-        if (col < n_here && (kFull || at < d)) q[st] = *(const f16x8 *)(qrow + at);
+        if (col < n_here && (kFull || e < d)) q[st] = *(const f16x8 *)(qrow + e);
     }
-    __syncthreads();
-    const bool any_bad = sh_bad != 0;
 
     const float c = a.scale * 1.44269504088896f;
     float m = kFloor, l = 0.0f, cap = 0.0f, cap_inv = 0.0f;
@@ -119,26 +185,30 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
     uint32_t v[8][VW];
     float4 ks[2], vs[2];
 
-    auto is_masked = [&](int tok) { return any_bad || tok + kTile > t1; };
-    auto load_k = [&](auto masked_c, int tok) {
-        constexpr bool kMasked = decltype(masked_c)::value;
+    // where the pages from token `c0` on stand, in elements (with codes: their numbers); -1: not in the cache
+    long long *const sh_off = (long long *)rest;
+    int first = 0, c1 = 0;
+    bool any_bad = false;
+    auto is_masked = [&](int tok) { return any_bad || tok + kTile > c1; };
+    auto load_k = [&](auto masked_c, auto once_c, int tok) {
+        constexpr bool kMasked = decltype(masked_c)::value, kOnce = decltype(once_c)::value;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int kt = tok + 16 * t + col;
             long long at = sh_off[(kt >> shift) - first];
-            const bool there = !kMasked || (at >= 0 && kt < t1);
+            const bool there = !kMasked || (at >= 0 && kt < c1);
             if (kInt8) at = at * a.c.ld_block + kvh * a.c.ld_head;
             const long long row = there ? at + (kt & mask) * a.c.ld_token : 0;
 #pragma unroll
             for (int u = 0; u < KW; ++u) {
                 const int e = kInt8 ? 64 * u + 16 * g : 32 * u + 8 * g;
                 k[t][u] = uint4{0, 0, 0, 0};
-                if (kFull || e < d) k[t][u] = *(const uint4 *)(a.c.k + (row + e) * (kInt8 ? 1 : 2));
+                if (kFull || e < d) k[t][u] = load<uint4, kOnce>(a.c.k + (row + e) * (kInt8 ? 1 : 2));
             }
         }
     };
-    auto load_v = [&](auto masked_c, int tok) {
-        constexpr bool kMasked = decltype(masked_c)::value;
+    auto load_v = [&](auto masked_c, auto once_c, int tok) {
+        constexpr bool kMasked = decltype(masked_c)::value, kOnce = decltype(once_c)::value;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             // the lane's tokens are 16 t + 4 g + 0..3, in one page
@@ -152,21 +222,21 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool there = !kMasked || (page >= 0 && vt + i < t1);
+                const bool there = !kMasked || (page >= 0 && vt + i < c1);
                 const char *p = a.c.v + (there ? at + ((vt & mask) + i) * a.c.ld_token + VE * col : 0) * (kInt8 ? 1 : 2);
                 uint32_t *w = v[4 * t + i];
 #pragma unroll
                 for (int x = 0; x < VW; ++x) w[x] = 0;
                 if (kFull || VE * col < d) {
                     if constexpr (VW == 1) {
-                        w[0] = *(const uint32_t *)p;
+                        w[0] = load<uint32_t, kOnce>(p);
                     } else if constexpr (VW == 2) {
-                        const uint2 y = *(const uint2 *)p;
+                        const uint2 y = load<uint2, kOnce>(p);
                         w[0] = y.x, w[1] = y.y;
                     } else {
 #pragma unroll
                         for (int x = 0; x < VW / 4; ++x) {
-                            const uint4 y = ((const uint4 *)p)[x];
+                            const uint4 y = load<uint4, kOnce>(p + 16 * x);
                             w[4 * x] = y.x, w[4 * x + 1] = y.y, w[4 * x + 2] = y.z, w[4 * x + 3] = y.w;
                         }
                     }
@@ -178,21 +248,48 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
             }
         }
     };
+    const std::true_type yes;
+    const std::false_type no;
     auto ask_k = [&](int tok) {
-        if (is_masked(tok)) load_k(std::true_type{}, tok); else load_k(std::false_type{}, tok);
+        if (is_masked(tok)) load_k(yes, no, tok);
+        else if (plan.once) load_k(no, yes, tok);
+        else load_k(no, no, tok);
     };
     auto ask_v = [&](int tok) {
-        if (is_masked(tok)) load_v(std::true_type{}, tok); else load_v(std::false_type{}, tok);
+        if (is_masked(tok)) load_v(yes, no, tok);
+        else if (plan.once) load_v(no, yes, tok);
+        else load_v(no, no, tok);
     };
+
+    for (int c0 = t0; c0 < t1; c0 = c1) {
+    c1 = min(t1, c0 + kPages);
+    first = c0 >> shift;
+    const int pages = ((c1 - 1) >> shift) - first + 1;
+    __syncthreads();                              // the last piece's readers
+    if (tid == 0) sh_bad = 0;
+    __syncthreads();
+    for (int i = tid; i < pages + 4; i += kThreads) {
+        long long where = -1;
+        if (i < pages) {
+            const int page = a.table[(long long)s * a.ld_table + first + i];
+            if (page >= 0 && page < a.c.n_blocks)
+                where = kInt8 ? page : page * a.c.ld_block + kvh * a.c.ld_head;
+            else
+                sh_bad = 1;
+        }
+        sh_off[i] = where;
+    }
+    __syncthreads();
+    any_bad = sh_bad != 0;
 
     // The keys of the next step are requested when this step's are in the matrix pipes, its values when this step's are: the
     // same registers, and something is always on its way.
-    int tok = t0 + wave * kTile;
-    if (tok < t1) {
+    int tok = c0 + wave * kTile;
+    if (tok < c1) {
         ask_k(tok);
         ask_v(tok);
     }
-    for (; tok < t1; tok += kWaves * kTile) {
+    for (; tok < c1; tok += kWaves * kTile) {
         const int next = tok + kWaves * kTile;
         f32x4 acc[2] = {};
 #pragma unroll
@@ -211,7 +308,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
                     acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(h[4], h[5], h[6], h[7]), q[2 * u + 1], acc[t], 0, 0, 0);
                 }
             }
-        if (next < t1) ask_k(next);
+        if (next < c1) ask_k(next);
 
         float p[8], w[8];
 #pragma unroll
@@ -227,7 +324,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int kt = tok + 16 * (j >> 2) + 4 * g + (j & 3);
-                if (kt >= t1 || sh_off[(kt >> shift) - first] < 0) p[j] = kFloor, w[j] = 0.0f;
+                if (kt >= c1 || sh_off[(kt >> shift) - first] < 0) p[j] = kFloor, w[j] = 0.0f;
             }
         }
         float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
@@ -291,7 +388,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
             o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, ph, o[e], 0, 0, 0);
             o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, pl, o[e], 0, 0, 0);
         }
-        if (next < t1) ask_v(next);
+        if (next < c1) ask_v(next);
+    }
     }
 
     // The waves' parts: m and l by head, then sum_w 2^(m_w - max m) o_w in LDS, [wave][head][d], the upper half of the waves
@@ -306,7 +404,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
     const float f = weight_of(m, l, top) * (kInt8 ? cap : 1.0f);
 #pragma unroll
     for (int e = 0; e < VE; ++e) o[e] *= f;
-    float *const sh_o = (float *)lds;
+    float *const sh_o = (float *)rest;
     float *const mine = sh_o + ((wave & 3) * n_here + col) * kD;
     auto put = [&](bool add) {
         if (col >= n_here) return;
@@ -339,149 +437,174 @@ __global__ __launch_bounds__(64 * kWaves) void k_attend(AttendArgs a, Split sp)
         f32x4 sum = {};
 #pragma unroll
         for (int w = 0; w < 4; ++w) sum += *(const f32x4 *)(sh_o + (w * n_here + h) * kD + e);
-        if (sp.n == 1) {
+        if (whole) {
             const float inv = most == kFloor ? 0.0f : 1.0f / all;
             f16x4 r;
 #pragma unroll
             for (int x = 0; x < 4; ++x) r[x] = (_Float16)(sum[x] * inv);
             *(f16x4 *)(a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e) = r;
         } else {
-            const long long part = ((long long)s * a.n_heads + head0 + h) * sp.n + split;
-            *(f32x4 *)(sp.o + part * d + e) = sum;
-            if (e == 0) sp.ml[part] = make_float2(most, all);
+            const int part = (blockIdx.x * 2 + (piece ? 1 : 0)) * min(a.group, kHeads<kD>) + h;
+            *(f32x4 *)(plan.o + (long long)part * d + e) = sum;
+            if (e == 0) plan.ml[part] = make_float2(most, all);
         }
+    }
+    if constexpr (!kShares) return;
+    if (at >= end) {
+        if (tid == 0) {
+            // open: the first of the shares that have a part of this pair, which later ones finish
+            const long long from = (long long)sh_before[s] * pairs + (long long)pair * n, begin = total * blockIdx.x / groups;
+            const int last = (int)(((from + n) * groups - 1) / total);       // the share of the pair's last step
+            const bool first_of = begin <= from && end < from + n;
+            plan.open[blockIdx.x] = int4{s, pair, first_of ? last - (int)blockIdx.x + 1 : 0, begin == from ? 0 : 1};
+        }
+        return;
+    }
+    // on to the next pair, or the next sequence that has steps
+    j = 0;
+    if (++pair == pairs) {
+        pair = 0;
+        do ++s; while (sh_before[s + 1] == sh_before[s]);
+        n = sh_before[s + 1] - sh_before[s];
+    }
     }
 }
 
-// The splits of a sequence and head joined, with weights 2^(m - max m): a thread four dimensions of every
-// (512 / (d / 4))th split, its first eight requested before the weights are known.
-__global__ __launch_bounds__(512) void k_attend_join(AttendArgs a, Split sp)
+// The pieces of a pair that several shares have, joined by weights 2^(m - max m): a workgroup to a share that leaves a pair
+// open, a thread four dimensions of a head of every (512 / those)th piece.
+__global__ __launch_bounds__(512) void k_attend_join(AttendArgs a, Plan plan, int heads)
 {
-    __shared__ float red[16], weight[512];
+    __shared__ float sh_top[16], sh_inv[16];
     __shared__ f32x4 part[512];
-    const int tid = threadIdx.x, h = blockIdx.x, s = blockIdx.y, d = a.c.head_dim;
-    const int len = min(a.lengths[s], a.max_length), n = len <= 0 ? 0 : (len + sp.chunk - 1) / sp.chunk;
-    const long long row = ((long long)s * a.n_heads + h) * sp.n;
-    const float2 *const ml = sp.ml + row;
-    const int lanes = d / 4, per = 512 / lanes, mine = tid / lanes, e = (tid - mine * lanes) * 4;
-    const float *const o = sp.o + row * d + e;
-    f32x4 early[8] = {};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (mine < per && mine + i * per < n) early[i] = *(const f32x4 *)(o + (long long)(mine + i * per) * d);
-    float2 x = make_float2(kFloor, 0.0f);
-    if (tid < n) x = ml[tid];
-    float top = x.x;
-    for (int i = tid + 512; i < n; i += 512) top = fmaxf(top, ml[i].x);
-    for (int y = 1; y < 64; y <<= 1) top = fmaxf(top, __shfl_xor(top, y, 64));
-    if ((tid & 63) == 0) red[tid >> 6] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, red[w]);
-    weight[tid] = weight_of(x.x, x.y, top);
-    float all = weight[tid] * x.y;
-    for (int i = tid + 512; i < n; i += 512) all += weight_of(ml[i].x, ml[i].y, top) * ml[i].y;
-    for (int y = 1; y < 64; y <<= 1) all += __shfl_xor(all, y, 64);
-    if ((tid & 63) == 0) red[8 + (tid >> 6)] = all;
-    __syncthreads();
-    f32x4 sum = {};
-    if (mine < per) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += weight[min(mine + i * per, 511)] * early[i];
-        for (int i = mine + 8 * per; i < n; i += per) sum += weight_of(ml[i].x, ml[i].y, top) * *(const f32x4 *)(o + (long long)i * d);
+    const int4 open = plan.open[blockIdx.x];
+    if (open.z == 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, d = a.c.head_dim, s = open.x, pieces = open.z;
+    const int subs = (a.group + heads - 1) / heads, kvh = open.y / subs, sub = open.y - kvh * subs;
+    const int head0 = kvh * a.group + sub * heads, n_here = min(heads, a.group - sub * heads), stride = min(a.group, heads);
+    // the first share's piece is in the slot it says, the others begin with theirs
+    auto place = [&](int i) { return ((blockIdx.x + i) * 2 + (i == 0 ? open.w : 0)) * stride; };
+    for (int h = tid >> 6; h < n_here; h += 8) {
+        float top = kFloor, all = 0.0f;
+        for (int i = lane; i < pieces; i += 64) top = fmaxf(top, plan.ml[place(i) + h].x);
+        for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+        for (int i = lane; i < pieces; i += 64) {
+            const float2 x = plan.ml[place(i) + h];
+            all += weight_of(x.x, x.y, top) * x.y;
+        }
+        for (int x = 1; x < 64; x <<= 1) all += __shfl_xor(all, x, 64);
+        if (lane == 0) sh_top[h] = top, sh_inv[h] = top == kFloor ? 0.0f : 1.0f / all;
     }
-    part[tid] = sum;
     __syncthreads();
-    if (tid < lanes) {
-        all = 0.0f;
+    const int lanes = d / 4, items = n_here * lanes, per = items < 512 ? 512 / items : 1;
+    for (int base = 0; base < items; base += 512) {
+        const int mine = items < 512 ? tid / items : 0, item = base + (items < 512 ? tid - mine * items : tid);
+        const int h = item / lanes, e = (item - h * lanes) * 4;
+        const bool live = mine < per && item < items;
+        f32x4 sum = {};
+        if (live) {
+            const float top = sh_top[h];
+#pragma unroll 4
+            for (int i = mine; i < pieces; i += per) {
+                const float2 x = plan.ml[place(i) + h];
+                sum += weight_of(x.x, x.y, top) * *(const f32x4 *)(plan.o + (long long)(place(i) + h) * d + e);
+            }
+        }
+        if (per > 1) {
+            __syncthreads();
+            part[tid] = sum;
+            __syncthreads();
+            if (live && mine == 0)
+                for (int i = 1; i < per; ++i) sum += part[i * items + item];
+        }
+        if (live && mine == 0) {
+            f16x4 r;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) all += red[8 + w];
-        for (int i = 1; i < per; ++i) sum += part[i * lanes + tid];
-        const float inv = top == kFloor ? 0.0f : 1.0f / all;
-        f16x4 r;
-#pragma unroll
-        for (int y = 0; y < 4; ++y) r[y] = (_Float16)(sum[y] * inv);
-        *(f16x4 *)(a.o + (long long)s * a.ldo + (long long)h * d + e) = r;
+            for (int y = 0; y < 4; ++y) r[y] = (_Float16)(sum[y] * sh_inv[h]);
+            *(f16x4 *)(a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e) = r;
+        }
     }
 }
 
 int heads_of(int head_dim) { return head_dim > 128 ? kHeads<256> : kHeads<128>; }
 
-Split split_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
+// Workgroups that are on the chip at once, by their registers: of 4 waves with shares, and of 8 waves.
+int resident(int head_dim) { return head_dim <= 64 ? 1024 : head_dim <= 128 ? 512 : 256; }
+int resident8(int head_dim) { return head_dim <= 64 ? 512 : 256; }
+
+// Shares where a workgroup of 8 waves to each sequence and head would go through more than kDirect tokens one after the
+// other, unless there are so many of them that they even out.
+constexpr int kDirect = 2048, kMany = 4;
+bool shares_pay(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
 {
     const int group = n_heads / n_kv_heads, subs = (group + heads_of(head_dim) - 1) / heads_of(head_dim);
-    const long long base = (long long)S * n_kv_heads * subs;
-    const long long want = (kWorkgroups + base - 1) / base;
-    const long long chunk = ((max_length + want - 1) / want + 255) / 256 * 256;
-    Split sp{};
-    sp.chunk = (int)(chunk < kMinChunk ? kMinChunk : chunk > kMaxChunk ? kMaxChunk : chunk);
-    sp.n = (int)(((long long)max_length + sp.chunk - 1) / sp.chunk);
-    return sp;
+    const long long pairs = (long long)S * n_kv_heads * subs, rounds = (pairs + resident8(head_dim) - 1) / resident8(head_dim);
+    return max_length * rounds > kDirect && rounds <= kMany && S <= kMaxSeqs;
 }
-
-// 8 waves where each has a step or more and their parts are worth joining in LDS.
-int waves_of(const Split &sp, int max_length) { return min(sp.chunk, max_length) > 256 ? 8 : 4; }
 
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-size_t parts_bytes(size_t splits, int n_heads, int head_dim)
+size_t parts_of(int n_heads, int n_kv_heads, int head_dim)
 {
-    return up256(splits * n_heads * head_dim * 4) + up256(splits * n_heads * 8);
+    return (size_t)resident(head_dim) * 2 * std::min(n_heads / n_kv_heads, heads_of(head_dim));
 }
 
-template <int kD, int kWaves>
-hipError_t launch_w(const AttendArgs &a, const Split &sp, bool int8, hipStream_t s)
+template <int kD, int kWaves, bool kShares>
+hipError_t launch_w(const AttendArgs &a, const Plan &plan, bool int8, hipStream_t s)
 {
-    const int subs = (a.group + kHeads<kD> - 1) / kHeads<kD>;
-    const dim3 grid(a.c.n_kv_heads * subs, sp.n, a.S), block(64 * kWaves);
-    const size_t offs = ((size_t)(sp.chunk >> a.c.block_shift) + 5) * 8;
-    const size_t join = (size_t)4 * (a.group < kHeads<kD> ? a.group : kHeads<kD>) * kD * 4;
-    const size_t lds = offs > join ? offs : join;
+    const int pairs = a.c.n_kv_heads * ((a.group + kHeads<kD> - 1) / kHeads<kD>);
+    const dim3 grid = kShares ? dim3(plan.groups) : dim3(pairs, a.S), block(64 * kWaves);
+    const size_t offs = ((size_t)(std::min(a.max_length, kPages) >> a.c.block_shift) + 6) * 8;
+    const size_t join = (size_t)4 * std::min(a.group, kHeads<kD>) * kD * 4;
+    const size_t lds = std::max(offs, join) + (kShares ? (size_t)((a.S + 4) / 4) * 16 : 0);
     const bool full = a.c.head_dim == kD;
     if (int8)
-        return full ? launch_kernel(k_attend<kD, true, true, kWaves>, grid, block, lds, s, a, sp)
-                    : launch_kernel(k_attend<kD, true, false, kWaves>, grid, block, lds, s, a, sp);
-    return full ? launch_kernel(k_attend<kD, false, true, kWaves>, grid, block, lds, s, a, sp)
-                : launch_kernel(k_attend<kD, false, false, kWaves>, grid, block, lds, s, a, sp);
+        return full ? launch_kernel(k_attend<kD, true, true, kWaves, kShares>, grid, block, lds, s, a, plan)
+                    : launch_kernel(k_attend<kD, true, false, kWaves, kShares>, grid, block, lds, s, a, plan);
+    return full ? launch_kernel(k_attend<kD, false, true, kWaves, kShares>, grid, block, lds, s, a, plan)
+                : launch_kernel(k_attend<kD, false, false, kWaves, kShares>, grid, block, lds, s, a, plan);
 }
 
 template <int kD>
-hipError_t launch_d(const AttendArgs &a, const Split &sp, bool int8, hipStream_t s)
+hipError_t launch_d(const AttendArgs &a, const Plan &plan, bool int8, hipStream_t s)
 {
-    return waves_of(sp, a.max_length) == 8 ? launch_w<kD, 8>(a, sp, int8, s) : launch_w<kD, 4>(a, sp, int8, s);
+    if (plan.groups) return launch_w<kD, 4, true>(a, plan, int8, s);
+    // 8 waves where each has tokens
+    return a.max_length > 128 ? launch_w<kD, 8, false>(a, plan, int8, s) : launch_w<kD, 4, false>(a, plan, int8, s);
 }
 
 }  // namespace
 
-// Of this call.
 size_t attend_workspace_need(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
 {
-    const Split sp = split_of(S, n_heads, n_kv_heads, head_dim, max_length);
-    return sp.n == 1 ? 0 : parts_bytes((size_t)S * sp.n, n_heads, head_dim);
+    if (!shares_pay(S, n_heads, n_kv_heads, head_dim, max_length)) return 0;
+    const size_t parts = parts_of(n_heads, n_kv_heads, head_dim);
+    return up256(parts * head_dim * 4) + up256(parts * 8) + up256((size_t)resident(head_dim) * 16);
 }
 
-// Of this call and every smaller one (S and max_length): there are ceil(max_length / chunk) splits, at most `want` of
-// them unless the longest chunk forces more, and S want < 1024 / heads + S.
+// Enough for every smaller S and max_length: what one of them needs does not depend on which.
 size_t attend_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
 {
-    if (max_length <= kMinChunk) return 0;
-    const int group = n_heads / n_kv_heads, subs = (group + heads_of(head_dim) - 1) / heads_of(head_dim);
-    const size_t forced = (size_t)S * ((max_length + kMaxChunk - 1) / kMaxChunk), shortest = (size_t)S * ((max_length + kMinChunk - 1) / kMinChunk);
-    const size_t wanted = (size_t)(kWorkgroups / (n_kv_heads * subs)) + S;
-    const size_t most = shortest < wanted ? shortest : wanted;
-    return parts_bytes(forced > most ? forced : most, n_heads, head_dim);
+    size_t most = 0;
+    for (int x = 1; x <= S && x <= kMaxSeqs; ++x)
+        if ((most = attend_workspace_need(x, n_heads, n_kv_heads, head_dim, max_length)) > 0) break;
+    return most;
 }
 
 hipError_t launch_attend(const AttendArgs &a, bool int8, hipStream_t s)
 {
-    Split sp = split_of(a.S, a.n_heads, a.c.n_kv_heads, a.c.head_dim, a.max_length);
-    const size_t parts = (size_t)a.S * a.n_heads * sp.n;
-    sp.o = (float *)a.workspace;
-    sp.ml = (float2 *)((char *)a.workspace + up256(parts * a.c.head_dim * 4));
     const int d = a.c.head_dim;
-    hipError_t e = d <= 64 ? launch_d<64>(a, sp, int8, s) : d <= 128 ? launch_d<128>(a, sp, int8, s) : launch_d<256>(a, sp, int8, s);
-    if (e != hipSuccess || sp.n == 1) return e;
-    return launch_kernel(k_attend_join, dim3(a.n_heads, a.S), dim3(512), 0, s, a, sp);
+    Plan plan{};
+    plan.once = (double)a.S * a.max_length * a.c.n_kv_heads * d * (int8 ? 2 : 4) > 256.0 * 1024 * 1024;
+    if (attend_workspace_need(a.S, a.n_heads, a.c.n_kv_heads, d, a.max_length) > 0) {
+        const size_t parts = parts_of(a.n_heads, a.c.n_kv_heads, d);
+        plan.groups = resident(d);
+        plan.o = (float *)a.workspace;
+        plan.ml = (float2 *)((char *)a.workspace + up256(parts * d * 4));
+        plan.open = (int4 *)((char *)plan.ml + up256(parts * 8));
+    }
+    const hipError_t e = d <= 64 ? launch_d<64>(a, plan, int8, s) : d <= 128 ? launch_d<128>(a, plan, int8, s) : launch_d<256>(a, plan, int8, s);
+    if (e != hipSuccess || plan.groups == 0) return e;
+    return launch_kernel(k_attend_join, dim3(plan.groups), dim3(512), 0, s, a, plan, heads_of(d));
 }
 
 }  // namespace muxq

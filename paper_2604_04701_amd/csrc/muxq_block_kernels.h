@@ -35,7 +35,6 @@ struct AttendArgs {
     void *workspace;
     KvView c;
 };
-constexpr int kAttendMaxChunk = 4096;              // tokens of a workgroup at most: its page list stands in LDS
 size_t attend_workspace_need(int S, int n_heads, int n_kv_heads, int head_dim, int max_length);
 size_t attend_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_length);
 hipError_t launch_attend(const AttendArgs &a, bool int8, hipStream_t s);
