@@ -51,7 +51,8 @@ __device__ __forceinline__ f16x8 half8(uint32_t a, uint32_t b, uint32_t c, uint3
     return __builtin_bit_cast(f16x8, u32x4{a, b, c, d});
 }
 
-// kOnce: of what nobody reads again before the memory-side cache has let it go.
+// kOnce: past the caches.  Long caches are read once and gain a tenth by it (131072 tokens: 91 us against 100); short ones
+// may be in the memory-side cache from the step before and lose a third (24 sequences to 2000: 26 us against 20).
 template <typename V, bool kOnce>
 __device__ __forceinline__ V load(const char *p)
 {
@@ -69,7 +70,6 @@ __device__ __forceinline__ float weight_of(float m, float l, float top) { return
 // piece of a share in slot 0, the last one in slot 1.
 struct Plan {
     int groups;
-    bool once;          // more is read than the memory-side cache holds
     float *o;           // [groups][2][heads of a workgroup][d], unnormalised
     float2 *ml;         // [groups][2][heads of a workgroup]: m and the sum
     int4 *open;         // [groups]: {sequence, pair, pieces, slot of the first} that the share leaves open, pieces 0: none
@@ -190,8 +190,8 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
     int first = 0, c1 = 0;
     bool any_bad = false;
     auto is_masked = [&](int tok) { return any_bad || tok + kTile > c1; };
-    auto load_k = [&](auto masked_c, auto once_c, int tok) {
-        constexpr bool kMasked = decltype(masked_c)::value, kOnce = decltype(once_c)::value;
+    auto load_k = [&](auto masked_c, int tok) {
+        constexpr bool kMasked = decltype(masked_c)::value;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int kt = tok + 16 * t + col;
@@ -203,12 +203,12 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
             for (int u = 0; u < KW; ++u) {
                 const int e = kInt8 ? 64 * u + 16 * g : 32 * u + 8 * g;
                 k[t][u] = uint4{0, 0, 0, 0};
-                if (kFull || e < d) k[t][u] = load<uint4, kOnce>(a.c.k + (row + e) * (kInt8 ? 1 : 2));
+                if (kFull || e < d) k[t][u] = load<uint4, kShares>(a.c.k + (row + e) * (kInt8 ? 1 : 2));
             }
         }
     };
-    auto load_v = [&](auto masked_c, auto once_c, int tok) {
-        constexpr bool kMasked = decltype(masked_c)::value, kOnce = decltype(once_c)::value;
+    auto load_v = [&](auto masked_c, int tok) {
+        constexpr bool kMasked = decltype(masked_c)::value;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             // the lane's tokens are 16 t + 4 g + 0..3, in one page
@@ -229,14 +229,14 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                 for (int x = 0; x < VW; ++x) w[x] = 0;
                 if (kFull || VE * col < d) {
                     if constexpr (VW == 1) {
-                        w[0] = load<uint32_t, kOnce>(p);
+                        w[0] = load<uint32_t, kShares>(p);
                     } else if constexpr (VW == 2) {
-                        const uint2 y = load<uint2, kOnce>(p);
+                        const uint2 y = load<uint2, kShares>(p);
                         w[0] = y.x, w[1] = y.y;
                     } else {
 #pragma unroll
                         for (int x = 0; x < VW / 4; ++x) {
-                            const uint4 y = load<uint4, kOnce>(p + 16 * x);
+                            const uint4 y = load<uint4, kShares>(p + 16 * x);
                             w[4 * x] = y.x, w[4 * x + 1] = y.y, w[4 * x + 2] = y.z, w[4 * x + 3] = y.w;
                         }
                     }
@@ -248,17 +248,11 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
             }
         }
     };
-    const std::true_type yes;
-    const std::false_type no;
     auto ask_k = [&](int tok) {
-        if (is_masked(tok)) load_k(yes, no, tok);
-        else if (plan.once) load_k(no, yes, tok);
-        else load_k(no, no, tok);
+        if (is_masked(tok)) load_k(std::true_type{}, tok); else load_k(std::false_type{}, tok);
     };
     auto ask_v = [&](int tok) {
-        if (is_masked(tok)) load_v(yes, no, tok);
-        else if (plan.once) load_v(no, yes, tok);
-        else load_v(no, no, tok);
+        if (is_masked(tok)) load_v(std::true_type{}, tok); else load_v(std::false_type{}, tok);
     };
 
     for (int c0 = t0; c0 < t1; c0 = c1) {
@@ -531,14 +525,16 @@ int heads_of(int head_dim) { return head_dim > 128 ? kHeads<256> : kHeads<128>; 
 int resident(int head_dim) { return head_dim <= 64 ? 1024 : head_dim <= 128 ? 512 : 256; }
 int resident8(int head_dim) { return head_dim <= 64 ? 512 : 256; }
 
-// Shares where a workgroup of 8 waves to each sequence and head would go through more than kDirect tokens one after the
-// other, unless there are so many of them that they even out.
-constexpr int kDirect = 2048, kMany = 4;
+// Shares where a workgroup of 8 waves to each sequence and head would go through many tokens one after the other, fewer
+// where those workgroups leave most of the chip idle.  (us, shares against none: 8 x 8 heads of 128 to 1500 tokens
+// 16.2 / 20.6, 128 x 8 to 2048 104 / 117, 64 x 8 to 8192 189 / 247, 40 x 8 to 1024 29.1 / 24.3; heads of 64: 24 x 12 to 4000
+// 37.6 / 45.0, 24 x 20 to 2500 40.2 / 40.6, 64 x 12 to 2048 51.3 / 47.4, 4 x 12 to 1024 12.6 / 11.0.)
 bool shares_pay(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
 {
     const int group = n_heads / n_kv_heads, subs = (group + heads_of(head_dim) - 1) / heads_of(head_dim);
-    const long long pairs = (long long)S * n_kv_heads * subs, rounds = (pairs + resident8(head_dim) - 1) / resident8(head_dim);
-    return max_length * rounds > kDirect && rounds <= kMany && S <= kMaxSeqs;
+    const int most = head_dim <= 64 ? 2500 : 1500;
+    const bool idle = (long long)S * n_kv_heads * subs * 4 <= resident8(head_dim);
+    return max_length > (idle ? most / 2 : most) && S <= kMaxSeqs;
 }
 
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -594,7 +590,6 @@ hipError_t launch_attend(const AttendArgs &a, bool int8, hipStream_t s)
 {
     const int d = a.c.head_dim;
     Plan plan{};
-    plan.once = (double)a.S * a.max_length * a.c.n_kv_heads * d * (int8 ? 2 : 4) > 256.0 * 1024 * 1024;
     if (attend_workspace_need(a.S, a.n_heads, a.c.n_kv_heads, d, a.max_length) > 0) {
         const size_t parts = parts_of(a.n_heads, a.c.n_kv_heads, d);
         plan.groups = resident(d);
