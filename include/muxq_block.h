@@ -102,11 +102,15 @@ int muxq_paged_attention(const void *Q_fp16, int S, int n_heads, int ldq, const 
  * ascending, starts[0] = 0, starts[n_requests] = M) and the adapter adapters[q] (int32; outside
  * [0, n_adapters), e.g. -1: none, its rows are copied from Y).  Rows in no request are not written; bounds
  * are clamped to [0, M].
+ * workspace: muxq_lora_workspace_bytes(...) bytes, 16-byte aligned, content undefined on entry; NULL where
+ * that is 0.  Calls that share one must not overlap in time.
  * Rules: K, N, r multiples of 8, r <= 128, K, N <= 2^21, M <= 2^24, n_adapters >= 1,
  * 1 <= n_requests <= 2^20. */
+size_t muxq_lora_workspace_bytes(int M, int K, int N, int r, int n_requests);   /* 0 on bad shapes, and where none is needed */
 int muxq_lora(const void *X_fp16, int M, int K, int ldx, const void *A_fp16, const void *B_fp16,
               const float *scales, int n_adapters, int r, const int32_t *starts, const int32_t *adapters,
-              int n_requests, const void *Y_fp16, int ldy, int N, void *out_fp16, int ldo, void *stream);
+              int n_requests, const void *Y_fp16, int ldy, int N, void *out_fp16, int ldo, void *workspace,
+              size_t workspace_bytes, void *stream);
 
 /* The step between two blocks: the norm behind a block, its gate, the residual stream, and the norm in
  * front of the next block, row by row:

@@ -27,7 +27,7 @@ EXPORTS = ["muxq_version", "muxq_status_string", "muxq_k_pad", "muxq_wq_bytes",
            "muxq_probe_mfma_rate", "muxq_gemm_kernel", "muxq_code_kernel", "muxq_static_bytes", "muxq_static_layout_of",
            "muxq_prepare_static", "muxq_linear_static", "muxq_gelu_absmax",
            "muxq_kv_append", "muxq_kv_gather", "muxq_paged_attention", "muxq_paged_attention_workspace_bytes",
-           "muxq_lora", "muxq_norm", "muxq_norm_slabs", "muxq_norm_scratch_bytes"]
+           "muxq_lora", "muxq_lora_workspace_bytes", "muxq_norm", "muxq_norm_slabs", "muxq_norm_scratch_bytes"]
 
 
 class MuxqError(RuntimeError):
@@ -155,7 +155,9 @@ def lib():
         L.muxq_paged_attention.restype = i
         L.muxq_paged_attention.argtypes = [vp, i, i, i, kv, vp, i, vp, i, f, vp, i, vp, sz, vp]
         L.muxq_lora.restype = i
-        L.muxq_lora.argtypes = [vp, i, i, i, vp, vp, vp, i, i, vp, vp, i, vp, i, i, vp, i, vp]
+        L.muxq_lora.argtypes = [vp, i, i, i, vp, vp, vp, i, i, vp, vp, i, vp, i, i, vp, i, vp, sz, vp]
+        L.muxq_lora_workspace_bytes.restype = sz
+        L.muxq_lora_workspace_bytes.argtypes = [i, i, i, i, i]
         L.muxq_norm_slabs.restype = i
         L.muxq_norm_slabs.argtypes = [i, i]
         L.muxq_norm_scratch_bytes.restype = sz
@@ -702,7 +704,12 @@ def muxq_paged_attention(q, k_cache, v_cache, block_table, lengths, max_length, 
     return out
 
 
-def muxq_lora(X, A, B, scales, starts, adapters, Y, out=None):
+def alloc_lora_workspace(M, K, N, r, n_requests, device="cuda"):
+    """Workspace of a muxq_lora call of these sizes (empty where none is needed)."""
+    return torch.empty(lib().muxq_lora_workspace_bytes(M, K, N, r, n_requests), dtype=torch.uint8, device=device)
+
+
+def muxq_lora(X, A, B, scales, starts, adapters, Y, out=None, workspace=None):
     """out = Y + scales[i] (X A_i^T) B_i^T for rows starts[q]..starts[q + 1] of request q with adapter i =
     adapters[q] (-1: none).  X [M, K], Y [M, N] fp16; A [n, r, K], B [n, N, r] fp16; scales float [n]; starts int32
     [requests + 1], adapters int32 [requests].  out may be Y."""
@@ -714,10 +721,12 @@ def muxq_lora(X, A, B, scales, starts, adapters, Y, out=None):
         out = torch.empty((M, N), dtype=torch.float16, device=X.device)
     if not (k == K and B.shape == (n, N, r) and Y.shape[0] == M and out.shape == (M, N)):
         _refuse("muxq_lora: shapes of X, A, B, Y and out do not fit")
+    if workspace is None:
+        workspace = alloc_lora_workspace(M, K, N, r, requests, X.device)
     _check(lib().muxq_lora(_p(X), M, K, _rows(X, "X"), _vector(A, n * r * K, "A"), _vector(B, n * N * r, "B"),
                            _vector(scales, n, "scales", torch.float32), n, r, _ints(starts, requests + 1, "starts"),
                            _ints(adapters, requests, "adapters"), requests, _p(Y), _rows(Y, "Y"), N, _p(out),
-                           _rows(out, "out"), _stream()), "muxq_lora")
+                           _rows(out, "out"), workspace.data_ptr(), workspace.numel(), _stream()), "muxq_lora")
     return out
 
 

@@ -169,18 +169,33 @@ int muxq_paged_attention(const void *Q, int S, int n_heads, int ldq, const muxq_
     return MUXQ_OK;
 }
 
+static bool lora_shape_ok(int M, int K, int N, int r, int n_requests)
+{
+    return M >= 1 && M <= kMaxRows && K >= 8 && K % 8 == 0 && K <= kMaxCols && N >= 8 && N % 8 == 0 && N <= kMaxCols &&
+           r >= 8 && r % 8 == 0 && r <= 128 && n_requests >= 1 && n_requests <= (1 << 20);
+}
+
+size_t muxq_lora_workspace_bytes(int M, int K, int N, int r, int n_requests)
+{
+    return lora_shape_ok(M, K, N, r, n_requests) ? muxq::lora_workspace_bytes(M, K, N, r, n_requests) : 0;
+}
+
 int muxq_lora(const void *X, int M, int K, int ldx, const void *A, const void *B, const float *scales,
               int n_adapters, int r, const int32_t *starts, const int32_t *adapters, int n_requests,
-              const void *Y, int ldy, int N, void *out, int ldo, void *stream)
+              const void *Y, int ldy, int N, void *out, int ldo, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (!X || !A || !B || !scales || !starts || !adapters || !Y || !out) return MUXQ_ERR_NULL;
-    if (M < 1 || M > kMaxRows || K < 8 || K % 8 || K > kMaxCols || N < 8 || N % 8 || N > kMaxCols || r < 8 || r % 8 || r > 128 ||
-        n_adapters < 1 || n_requests < 1 || n_requests > (1 << 20) || bad_ld(ldx, K) || bad_ld(ldy, N) || bad_ld(ldo, N))
-        return MUXQ_ERR_SHAPE;
+    if (!lora_shape_ok(M, K, N, r, n_requests) || n_adapters < 1 || bad_ld(ldx, K) || bad_ld(ldy, N) || bad_ld(ldo, N)) return MUXQ_ERR_SHAPE;
     if (!aligned(X, 16) || !aligned(A, 16) || !aligned(B, 16) || !aligned(Y, 16) || !aligned(out, 16) || !aligned(scales, 4) ||
         !aligned(starts, 4) || !aligned(adapters, 4))
         return MUXQ_ERR_ALIGN;
     if (share(X, ldx, K, out, ldo, N, M) || ((Y != out || ldy != ldo) && share(Y, ldy, N, out, ldo, N, M))) return MUXQ_ERR_PARAM;
+    const size_t need = muxq::lora_workspace_bytes(M, K, N, r, n_requests);
+    if (need > 0) {
+        if (!workspace) return MUXQ_ERR_NULL;
+        if (!aligned(workspace, 16)) return MUXQ_ERR_ALIGN;
+        if (workspace_bytes < need) return MUXQ_ERR_WORKSPACE;
+    }
     muxq::LoraArgs g{};
     g.x = (const _Float16 *)X;
     g.a = (const _Float16 *)A;
@@ -193,6 +208,7 @@ int muxq_lora(const void *X, int M, int K, int ldx, const void *A, const void *B
     g.M = M; g.K = K; g.N = N; g.r = r;
     g.n_adapters = n_adapters; g.n_requests = n_requests;
     g.ldx = ldx; g.ldy = ldy; g.ldo = ldo;
+    g.h = (float *)workspace;
     MUXQ_TRY(muxq::launch_lora(g, (hipStream_t)stream));
     return MUXQ_OK;
 }

@@ -45,7 +45,9 @@ struct LoraArgs {
     const float *scales;
     const int32_t *starts, *adapters;
     int M, K, N, r, n_adapters, n_requests, ldx, ldy, ldo;
+    float *h;       // [pieces of K][M][r]
 };
+size_t lora_workspace_bytes(int M, int K, int N, int r, int n_requests);
 hipError_t launch_lora(const LoraArgs &a, hipStream_t s);
 
 struct NormArgs {

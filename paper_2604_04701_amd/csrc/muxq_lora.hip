@@ -6,7 +6,8 @@
 // are the operands of the matrix pipes), add their parts in LDS, and then divide the strip's channels for H B^T,
 // with rows of B as the left operand in an order that leaves a lane 16 neighbouring channels of a row of Y.
 // H is what several strips of a tile compute again: it costs reads of X and A from the L2s, and saves a second
-// launch and the way of H through memory.
+// launch and the way of H through memory.  Where it would cost more than that, two launches: the first
+// divides K over workgroups too and leaves its parts of H in the workspace, binary32, the second adds them.
 // H is binary32; the second product takes it as two fp16 parts (22 bits) of the row over a power of two,
 // whatever its size.
 #include "muxq_block_kernels.h"
@@ -17,17 +18,21 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kCols = 64 * kWaves;      // output channels of a workgroup's step
+constexpr int kDeep = 64 * kWaves;                                          // channels of X of one
 
 // First row of request q, whatever the caller's bounds hold.
 __device__ __forceinline__ int start_of(const LoraArgs &g, int q) { return min(max(g.starts[q], 0), g.M); }
 
-// kTM: tiles of 16 rows, kRT: tiles of 16 ranks (of the power of two at or above r).
-template <int kTM, int kRT>
-__global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int strip)
+enum Part { kBoth, kDown, kUp };
+
+// kTM: tiles of 16 rows, kRT: tiles of 16 ranks (of the power of two at or above r).  piece: what a workgroup in y takes,
+// channels of Y, or channels of X in the first of two launches; pieces: of X.
+template <int kTM, int kRT, Part kPart>
+__global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pieces)
 {
     constexpr int T = 16 * kTM, R = 16 * kRT, RS = kRT == 1 ? 1 : kRT / 2, LD = R + 4, LH = 32 * RS + 8;
-    __shared__ float part[kWaves / 2][T][LD];
-    __shared__ __align__(16) _Float16 h_hi[T][LH], h_lo[T][LH];
+    __shared__ float part[kPart == kUp ? 1 : kWaves / 2][T][LD];
+    __shared__ __align__(16) _Float16 h_hi[kPart == kDown ? 1 : T][LH], h_lo[kPart == kDown ? 1 : T][LH];
     __shared__ float factor[T];
     __shared__ int found[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, gr = lane >> 4;
@@ -58,69 +63,123 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int strip)
     const int first = start_of(g, q), row0 = first + (b - (first / T + q)) * T;
     const int rows = min(T, start_of(g, q + 1) - row0);
     if (rows <= 0 || row0 < first) return;
-    const int n0 = blockIdx.y * strip, n1 = min(g.N, n0 + strip);
+    const int n0 = blockIdx.y * piece, n1 = min(g.N, n0 + piece);
     const int ad = g.adapters[q];
     const _Float16 *const y = g.y + (long long)row0 * g.ldy;
     _Float16 *const out = g.out + (long long)row0 * g.ldo;
     if (ad < 0 || ad >= g.n_adapters) {
-        if (g.y != g.out)
+        if (kPart != kDown && g.y != g.out)
             for (int m = wave; m < rows; m += kWaves)
                 for (int n = n0 + lane * 8; n < n1; n += 512) *(f16x8 *)(out + (long long)m * g.ldo + n) = *(const f16x8 *)(y + (long long)m * g.ldy + n);
         return;
     }
 
-    // H: lanes of a 16-lane row read 64 bytes of 16 rows; rows past the tile's last repeat it, ranks past r the last one
-    const _Float16 *xr[kTM], *ar[kRT];
+    if constexpr (kPart != kUp) {
+        // H: lanes of a 16-lane row read 64 bytes of 16 rows; rows past the tile's last repeat it, ranks past r the last one
+        const _Float16 *xr[kTM], *ar[kRT];
 #pragma unroll
-    for (int t = 0; t < kTM; ++t) xr[t] = g.x + (long long)(row0 + min(16 * t + col, rows - 1)) * g.ldx;
+        for (int t = 0; t < kTM; ++t) xr[t] = g.x + (long long)(row0 + min(16 * t + col, rows - 1)) * g.ldx;
 #pragma unroll
-    for (int t = 0; t < kRT; ++t) ar[t] = g.a + ((long long)ad * g.r + min(16 * t + col, g.r - 1)) * g.K;
-    f32x4 acc[kTM][kRT] = {};
-    auto step = [&](auto whole, int k0) {
-        f16x8 xv[4][kTM], av[4][kRT];
+        for (int t = 0; t < kRT; ++t) ar[t] = g.a + ((long long)ad * g.r + min(16 * t + col, g.r - 1)) * g.K;
+        f32x4 acc[kTM][kRT] = {};
+        // 64 channels at a time, the next ones on their way while these are in the matrix pipes
+        struct Buffer {
+            f16x8 x[2][kTM], a[2][kRT];
+        } buf[2];
+        const int kb = kPart == kDown ? blockIdx.y * piece : 0, ke = kPart == kDown ? min(g.K, kb + piece) : g.K;
+        auto ask = [&](Buffer &w, int k0) {
+            const bool whole = k0 + 64 <= g.K;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int k = k0 + 32 * s + 8 * gr;
-            const bool there = decltype(whole)::value || k < g.K;
-            const int at = there ? k : 0;
+            for (int s = 0; s < 2; ++s) {
+                const int k = k0 + 32 * s + 8 * gr, at = whole || k < g.K ? k : 0;
 #pragma unroll
-            for (int t = 0; t < kTM; ++t) xv[s][t] = there ? *(const f16x8 *)(xr[t] + at) : f16x8{};
+                for (int t = 0; t < kTM; ++t) w.x[s][t] = *(const f16x8 *)(xr[t] + at);
 #pragma unroll
-            for (int t = 0; t < kRT; ++t) av[s][t] = there ? *(const f16x8 *)(ar[t] + at) : f16x8{};
+                for (int t = 0; t < kRT; ++t) w.a[s][t] = *(const f16x8 *)(ar[t] + at);
+            }
+            if (!whole) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+                    if (k0 + 32 * s + 8 * gr >= g.K) {
+#pragma unroll
+                        for (int t = 0; t < kTM; ++t) w.x[s][t] = f16x8{};
+#pragma unroll
+                        for (int t = 0; t < kRT; ++t) w.a[s][t] = f16x8{};
+                    }
+            }
+        };
+        auto add = [&](const Buffer &w) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int t = 0; t < kTM; ++t)
+#pragma unroll
+                    for (int u = 0; u < kRT; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.x[s][t], w.a[s][u], acc[t][u], 0, 0, 0);
+        };
+        int k0 = kb + wave * 64;
+        if (k0 < ke) ask(buf[0], k0);
+        for (; k0 < ke; k0 += 2 * kDeep) {
+            if (k0 + kDeep < ke) ask(buf[1], k0 + kDeep);
+            add(buf[0]);
+            if (k0 + kDeep >= ke) break;
+            if (k0 + 2 * kDeep < ke) ask(buf[0], k0 + 2 * kDeep);
+            add(buf[1]);
         }
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
+        // parts of the upper waves to the lower ones, then all of them to the rows' owners
+        auto put = [&](int at) {
 #pragma unroll
             for (int t = 0; t < kTM; ++t)
 #pragma unroll
-                for (int u = 0; u < kRT; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[s][t], av[s][u], acc[t][u], 0, 0, 0);
-    };
-    for (int k0 = wave * 128; k0 < g.K; k0 += 128 * kWaves)
-        if (k0 + 128 <= g.K)
-            step(std::true_type{}, k0);
-        else
-            step(std::false_type{}, k0);
-    // parts of the upper waves to the lower ones, then all of them to the rows' owners
-    auto put = [&](int at) {
+                for (int u = 0; u < kRT; ++u)
 #pragma unroll
-        for (int t = 0; t < kTM; ++t)
+                    for (int i = 0; i < 4; ++i) part[at][16 * t + 4 * gr + i][16 * u + col] = acc[t][u][i];
+        };
+        if (wave >= kWaves / 2) put(wave - kWaves / 2);
+        __syncthreads();
+        if (wave < kWaves / 2) {
 #pragma unroll
-            for (int u = 0; u < kRT; ++u)
+            for (int t = 0; t < kTM; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) part[at][16 * t + 4 * gr + i][16 * u + col] = acc[t][u][i];
-    };
-    if (wave >= kWaves / 2) put(wave - kWaves / 2);
-    __syncthreads();
-    if (wave < kWaves / 2) {
+                for (int u = 0; u < kRT; ++u)
 #pragma unroll
-        for (int t = 0; t < kTM; ++t)
-#pragma unroll
-            for (int u = 0; u < kRT; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[t][u][i] += part[wave][16 * t + 4 * gr + i][16 * u + col];
-        put(wave);                                // its own place, read by itself alone
+                    for (int i = 0; i < 4; ++i) acc[t][u][i] += part[wave][16 * t + 4 * gr + i][16 * u + col];
+            put(wave);                                // its own place, read by itself alone
+        }
+        __syncthreads();
     }
-    __syncthreads();
+    if constexpr (kPart == kDown) {
+        for (int i = tid; i < rows * g.r; i += kThreads) {
+            const int m = i / g.r, j = i - m * g.r;
+            g.h[((long long)blockIdx.y * g.M + row0 + m) * g.r + j] = (part[0][m][j] + part[1][m][j]) + (part[2][m][j] + part[3][m][j]);
+        }
+        return;
+    }
+    // 64 channels of the output: row m of operand u is channel nb + 32 (u / 2) + 8 (m / 4) + 4 (u % 2) + m % 4, so that a lane ends
+    // up with two runs of 8 of a row.  (Loads past the tile's rows, the strip's channels or the ranks go to what is
+    // there; none of it is stored or counts.)  The next ones are on their way while these are worked on, the first ones while
+    // H is.
+    struct Ahead {
+        f16x8 y[kTM][2], b[4][RS];
+    } ahead;
+    const _Float16 *const br = g.b + (long long)ad * g.N * g.r;
+    auto ask_up = [&](int nb) {
+#pragma unroll
+        for (int t = 0; t < kTM; ++t)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                ahead.y[t][x] = *(const f16x8 *)(y + (long long)min(16 * t + col, rows - 1) * g.ldy + min(nb + 32 * x + 8 * gr, n1 - 8));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int nn = min(nb + 32 * (u >> 1) + 8 * (col >> 2) + 4 * (u & 1) + (col & 3), n1 - 1);
+#pragma unroll
+            for (int s = 0; s < RS; ++s) {
+                const int k = 32 * s + 8 * gr;
+                ahead.b[u][s] = *(const f16x8 *)(br + (long long)nn * g.r + (k < g.r ? k : 0));
+            }
+        }
+    };
+    int nb = n0 + wave * 64;
+    if (kPart == kUp && nb < n1) ask_up(nb);
     const float scale = g.scales[ad];
     for (int m = wave; m < T; m += kWaves) {
         constexpr int per = R > 64 ? R / 64 : 1;
@@ -129,7 +188,14 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int strip)
         for (int i = 0; i < per; ++i) {
             const int j = lane + 64 * i;
             v[i] = 0.0f;
-            if (j < g.r) v[i] = (part[0][m][j] + part[1][m][j]) + (part[2][m][j] + part[3][m][j]);
+            if (j < g.r) {
+                if constexpr (kPart == kUp) {
+                    if (m < rows)
+                        for (int x = 0; x < pieces; ++x) v[i] += g.h[((long long)x * g.M + row0 + m) * g.r + j];
+                } else {
+                    v[i] = (part[0][m][j] + part[1][m][j]) + (part[2][m][j] + part[3][m][j]);
+                }
+            }
             top = fmaxf(top, fabsf(v[i]));
         }
         for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
@@ -160,70 +226,95 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int strip)
             hl[t][s] = *(const f16x8 *)&h_lo[16 * t + col][32 * s + 8 * gr];
         }
     }
-    const _Float16 *const br = g.b + (long long)ad * g.N * g.r;
-    for (int nb = n0 + wave * 64; nb < n1; nb += kCols) {
-        // 64 channels: row m of operand t is channel nb + 16 (m / 4) + 4 t + m % 4, so that a lane ends up with 16 in a row
-        // (loads past the tile's rows, the strip's channels or the ranks go to what is there; none of it is stored or counts)
-        f16x8 yv[kTM][2];
-        const int n = nb + 16 * gr;
-#pragma unroll
-        for (int t = 0; t < kTM; ++t)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) yv[t][x] = *(const f16x8 *)(y + (long long)min(16 * t + col, rows - 1) * g.ldy + min(n + 8 * x, n1 - 8));
-        f16x8 bv[4][RS];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int nn = min(nb + 16 * (col >> 2) + 4 * u + (col & 3), n1 - 1);
-#pragma unroll
-            for (int s = 0; s < RS; ++s) {
-                const int k = 32 * s + 8 * gr;
-                bv[u][s] = *(const f16x8 *)(br + (long long)nn * g.r + (k < g.r ? k : 0));
-                if (k >= g.r) bv[u][s] = f16x8{};
-            }
-        }
+    if (kPart != kUp && nb < n1) ask_up(nb);
+    for (; nb < n1; nb += kCols) {
         f32x4 o[kTM][4] = {};
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int s = 0; s < RS; ++s)
+            for (int s = 0; s < RS; ++s) {
+                const f16x8 b = 32 * s + 8 * gr < g.r ? ahead.b[u][s] : f16x8{};
 #pragma unroll
                 for (int t = 0; t < kTM; ++t) {
-                    o[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bv[u][s], hh[t][s], o[t][u], 0, 0, 0);
-                    o[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bv[u][s], hl[t][s], o[t][u], 0, 0, 0);
+                    o[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, hh[t][s], o[t][u], 0, 0, 0);
+                    o[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, hl[t][s], o[t][u], 0, 0, 0);
                 }
+            }
+        f16x8 yv[kTM][2];
+#pragma unroll
+        for (int t = 0; t < kTM; ++t)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) yv[t][x] = ahead.y[t][x];
+        if (nb + kCols < n1) ask_up(nb + kCols);
 #pragma unroll
         for (int t = 0; t < kTM; ++t)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                if (16 * t + col >= rows || n + 8 * x >= n1) continue;
+                const int n = nb + 32 * x + 8 * gr;
+                if (16 * t + col >= rows || n >= n1) continue;
                 f16x8 r;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) r[i] = (_Float16)((float)yv[t][x][i] + f[t] * o[t][2 * x + (i >> 2)][i & 3]);
-                *(f16x8 *)(out + (long long)(16 * t + col) * g.ldo + n + 8 * x) = r;
+                *(f16x8 *)(out + (long long)(16 * t + col) * g.ldo + n) = r;
             }
     }
 }
 
-template <int kTM, int kRT>
-hipError_t launch(const LoraArgs &g, hipStream_t s)
+// Pieces of about `want` in all, each of whole steps.
+int piece_of(int size, int step, int tiles, int want)
 {
-    // strips: about 512 workgroups, each a step of all its waves at least
-    const int tiles = g.M / (16 * kTM) + g.n_requests, steps = (g.N + kCols - 1) / kCols;
-    int strips = (512 + tiles - 1) / tiles;
-    strips = strips < steps ? strips : steps;
-    const int strip = (steps + strips - 1) / strips * kCols;
-    return launch_kernel(k_lora<kTM, kRT>, dim3(tiles, (g.N + strip - 1) / strip), dim3(kThreads), 0, s, g, strip);
+    const int steps = (size + step - 1) / step;
+    int pieces = (want + tiles - 1) / tiles;
+    pieces = pieces < steps ? pieces : steps;
+    return (steps + pieces - 1) / pieces * step;
+}
+
+struct Shape {
+    bool two_rows;      // tiles of 32 rows
+    bool two_launches;
+    int tiles, k_piece, k_pieces;
+};
+
+Shape shape_of(int M, int K, int N, int r, int n_requests)
+{
+    Shape s{};
+    s.two_rows = r <= 64 && (long long)M >= 32ll * n_requests;      // prompts: 32 rows share what is read of A and B
+    s.tiles = M / (s.two_rows ? 32 : 16) + n_requests;
+    s.two_launches = (long long)r * K >= 1 << 30;
+    s.k_piece = piece_of(K, kDeep, s.tiles, 512);
+    s.k_pieces = (K + s.k_piece - 1) / s.k_piece;
+    return s;
+}
+
+template <int kTM, int kRT>
+hipError_t launch(const LoraArgs &g, const Shape &p, hipStream_t s)
+{
+    const dim3 block(kThreads);
+    if (!p.two_launches) {
+        const int strip = piece_of(g.N, kCols, p.tiles, 512);
+        return launch_kernel(k_lora<kTM, kRT, kBoth>, dim3(p.tiles, (g.N + strip - 1) / strip), block, 0, s, g, strip, 1);
+    }
+    const hipError_t e = launch_kernel(k_lora<kTM, kRT, kDown>, dim3(p.tiles, p.k_pieces), block, 0, s, g, p.k_piece, p.k_pieces);
+    if (e != hipSuccess) return e;
+    const int strip = piece_of(g.N, kCols, p.tiles, 1024);
+    return launch_kernel(k_lora<kTM, kRT, kUp>, dim3(p.tiles, (g.N + strip - 1) / strip), block, 0, s, g, strip, p.k_pieces);
 }
 
 }  // namespace
 
+size_t lora_workspace_bytes(int M, int K, int N, int r, int n_requests)
+{
+    const Shape p = shape_of(M, K, N, r, n_requests);
+    return p.two_launches ? (size_t)p.k_pieces * M * r * 4 : 0;
+}
+
 hipError_t launch_lora(const LoraArgs &g, hipStream_t s)
 {
-    const bool two = (long long)g.M >= 32ll * g.n_requests;      // prompts: 32 rows share what is read of A and B
-    if (g.r <= 16) return two ? launch<2, 1>(g, s) : launch<1, 1>(g, s);
-    if (g.r <= 32) return two ? launch<2, 2>(g, s) : launch<1, 2>(g, s);
-    if (g.r <= 64) return two ? launch<2, 4>(g, s) : launch<1, 4>(g, s);
-    return launch<1, 8>(g, s);
+    const Shape p = shape_of(g.M, g.K, g.N, g.r, g.n_requests);
+    if (g.r <= 16) return p.two_rows ? launch<2, 1>(g, p, s) : launch<1, 1>(g, p, s);
+    if (g.r <= 32) return p.two_rows ? launch<2, 2>(g, p, s) : launch<1, 2>(g, p, s);
+    if (g.r <= 64) return p.two_rows ? launch<2, 4>(g, p, s) : launch<1, 4>(g, p, s);
+    return launch<1, 8>(g, p, s);
 }
 
 }  // namespace muxq

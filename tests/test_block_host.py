@@ -38,7 +38,7 @@ def gather(c=None, **kw):
 
 def lora(**kw):
     a = dict(x=FAKE, M=16, K=256, ldx=256, a=FAKE, b=FAKE, scales=FAKE, n=3, r=16, starts=FAKE, adapters=FAKE, requests=4, y=FAKE,
-             ldy=512, N=512, out=AWAY, ldo=512)
+             ldy=512, N=512, out=AWAY, ldo=512, ws=FAKE, ws_bytes=1 << 40)
     a.update(kw)
     return B.lib().muxq_lora(*a.values(), None)
 
@@ -110,6 +110,15 @@ def test_attention_workspace():
     (dict(x=AWAY), 4), (dict(y=AWAY + 16), 4)])
 def test_lora_refuses(kw, status):
     assert lora(**kw) == status
+
+
+def test_lora_workspace():
+    need = B.lib().muxq_lora_workspace_bytes
+    assert need(0, 256, 512, 16, 4) == 0 and need(16, 252, 512, 16, 4) == 0 and need(16, 256, 512, 12, 4) == 0 and need(16, 256, 512, 16, 0) == 0
+    big = dict(M=8192, K=4096, ldx=4096, N=4096, ldy=4096, ldo=4096, r=64)
+    n = need(8192, 4096, 4096, 64, 4)
+    if n:
+        assert lora(**big, ws_bytes=n - 1) == 5 and lora(**big, ws=None) == 1 and lora(**big, ws=FAKE + 8) == 3
 
 
 @pytest.mark.parametrize("kw,status", [
