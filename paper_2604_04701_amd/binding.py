@@ -563,7 +563,8 @@ _NORM = {"layer": NORM_LAYER, "rms": NORM_RMS, NORM_LAYER: NORM_LAYER, NORM_RMS:
 _F16, _F32, _I8, _I32 = torch.float16, torch.float32, torch.int8, torch.int32
 
 
-# (Messages are put together only where a check fails: a call of a few microseconds has a dozen checks.)
+# (A call of a few microseconds has dozens of checks: each entry point makes them in one expression, and goes through its
+# tensors one by one, with _rows and _flat, only to say which of them it refuses.)
 def _refuse(what):
     raise MuxqError(what)
 
@@ -576,18 +577,27 @@ def _rows(t, name):
     return st[0]
 
 
-def _ints(t, n, name):
-    if t.dtype is not _I32 or not t.is_cuda or t.numel() < n or not t.is_contiguous():
-        _refuse(f"{name}: a contiguous int32 GPU tensor of at least {n} entries is expected")
-    return t.data_ptr()
-
-
-def _vector(t, n, name, dtype=_F16):
+def _flat(t, n, dtype, name):
+    """t: n contiguous entries of a type (at least, for indices); returns its address, None for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or not t.is_cuda or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or (t.numel() != n and (dtype is not _I32 or t.numel() < n)):
         _refuse(f"{name}: a contiguous GPU tensor of {n} {dtype} is expected")
     return t.data_ptr()
+
+
+def _call(entry, args, workspace, stream, alloc, what):
+    """entry(*args, workspace, its bytes, stream).  Without a workspace the call goes out with none: it is refused for a NULL
+    pointer, with nothing enqueued, where one is needed, and only then is one allocated."""
+    if workspace is not None:
+        status = entry(*args, workspace.data_ptr(), workspace.numel(), stream)
+    else:
+        status = entry(*args, None, 0, stream)
+        if status == 1:
+            workspace = alloc()
+            status = entry(*args, workspace.data_ptr(), workspace.numel(), stream)
+    if status != 0:
+        _check(status, what)
 
 
 def _kv(k_cache, v_cache, k_scale, v_scale):
@@ -610,8 +620,8 @@ def _kv(k_cache, v_cache, k_scale, v_scale):
         if k_scale is None or v_scale is None:
             _refuse("cache: 8-bit codes come with k_scale and v_scale")
         scales = n * heads * block
-        return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), _vector(k_scale, scales, "k_scale", _F32),
-                       _vector(v_scale, scales, "v_scale", _F32), 1, n, block, heads, d, 0, lb, lh, lt)
+        return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), _flat(k_scale, scales, _F32, "k_scale"),
+                       _flat(v_scale, scales, _F32, "v_scale"), 1, n, block, heads, d, 0, lb, lh, lt)
     if dtype is not _F16 or k_scale is not None or v_scale is not None:
         _refuse("cache: fp16 without scales, or int8 with them")
     return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), None, None, 0, n, block, heads, d, 0, lb, lh, lt)
@@ -634,25 +644,35 @@ def muxq_kv_append(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, q=
     ranges of one tensor.  Returns q_out (made when not given; None without q)."""
     M, heads, d = k.shape
     c = _kv(k_cache, v_cache, k_scale, v_scale)
-    if not (v.shape == k.shape and heads == c.n_kv_heads and d == c.head_dim):
-        _refuse("muxq_kv_append: k, v and the cache differ in heads")
+    ks, vs = k.stride(), v.stride()
+    if not (k.dtype is v.dtype is _F16 and slots.dtype is _I32 and k.is_cuda and v.is_cuda and slots.is_cuda and v.shape == k.shape and
+            heads == c.n_kv_heads and d == c.head_dim and ks[2] == vs[2] == 1 and (heads == 1 or ks[1] == vs[1] == d) and
+            slots.is_contiguous() and slots.numel() == M):
+        _rows(k, "k"), _rows(v, "v"), _flat(slots, M, _I32, "slots")
+        _refuse("muxq_kv_append: k, v, slots and the cache differ in tokens or heads")
     n_heads = ldq = ldqo = 0
+    q_at = q_out_at = None
     if q is not None:
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=torch.float16, device=q.device)
+            q_out = torch.empty(q.shape, dtype=_F16, device=q.device)
         n_heads = q.shape[1]
-        if not (q.shape == (M, n_heads, d) and q_out.shape == q.shape):
-            _refuse("muxq_kv_append: q and k differ in tokens or head size")
-        ldq, ldqo = _rows(q, "q"), _rows(q_out, "q_out")
+        qs, os = q.stride(), q_out.stride()
+        if not (q.dtype is q_out.dtype is _F16 and q.is_cuda and q_out.is_cuda and q.shape == q_out.shape == (M, n_heads, d) and
+                qs[2] == os[2] == 1 and (n_heads == 1 or qs[1] == os[1] == d)):
+            _rows(q, "q"), _rows(q_out, "q_out")
+            _refuse("muxq_kv_append: q, q_out and k differ in tokens or head size")
+        ldq, ldqo, q_at, q_out_at = qs[0], os[0], q.data_ptr(), q_out.data_ptr()
     n_pos = rot = 0
+    cos_at = pos_at = None
     if cos_sin is not None:
         n_pos, rot = cos_sin.shape
-        if not (positions is not None):
+        if positions is None:
             _refuse("muxq_kv_append: cos_sin comes with positions")
-    _check(lib().muxq_kv_append(_p(k), _p(v), M, _rows(k, "k"), _rows(v, "v"), _p(q), n_heads, ldq, _p(q_out), ldqo,
-                                _ints(slots, M, "slots"), None if positions is None else _ints(positions, M, "positions"),
-                                _vector(cos_sin, n_pos * rot, "cos_sin", torch.float32), n_pos, rot,
-                                int(interleaved), C.byref(c), _stream()), "muxq_kv_append")
+        cos_at, pos_at = _flat(cos_sin, n_pos * rot, _F32, "cos_sin"), _flat(positions, M, _I32, "positions")
+    status = lib().muxq_kv_append(k.data_ptr(), v.data_ptr(), M, ks[0], vs[0], q_at, n_heads, ldq, q_out_at, ldqo, slots.data_ptr(),
+                                  pos_at, cos_at, n_pos, rot, int(interleaved), C.byref(c), _stream())
+    if status != 0:
+        _check(status, "muxq_kv_append")
     return q_out
 
 
@@ -664,10 +684,12 @@ def muxq_kv_gather(slots, k_cache, v_cache, k_scale=None, v_scale=None, k_out=No
         k_out = torch.empty(shape, dtype=torch.float16, device=k_cache.device)
     if v_out is None:
         v_out = torch.empty(shape, dtype=torch.float16, device=k_cache.device)
-    if not (k_out.shape == shape and v_out.shape == shape):
+    if k_out.shape != shape or v_out.shape != shape:
         _refuse(f"muxq_kv_gather: outputs of shape {shape} are expected")
-    _check(lib().muxq_kv_gather(_ints(slots, shape[0], "slots"), shape[0], C.byref(c), _p(k_out), _rows(k_out, "k_out"),
-                                _p(v_out), _rows(v_out, "v_out"), _stream()), "muxq_kv_gather")
+    status = lib().muxq_kv_gather(_flat(slots, shape[0], _I32, "slots"), shape[0], C.byref(c), k_out.data_ptr(), _rows(k_out, "k_out"),
+                                  v_out.data_ptr(), _rows(v_out, "v_out"), _stream())
+    if status != 0:
+        _check(status, "muxq_kv_gather")
     return k_out, v_out
 
 
@@ -689,18 +711,18 @@ def muxq_paged_attention(q, k_cache, v_cache, block_table, lengths, max_length, 
     c = _kv(k_cache, v_cache, k_scale, v_scale)
     if out is None:
         out = torch.empty((S, n_heads, d), dtype=torch.float16, device=q.device)
-    if not (d == c.head_dim and out.shape == q.shape):
-        _refuse("muxq_paged_attention: q, out and the cache differ in head size")
-    if not (block_table.dtype == torch.int32 and block_table.is_cuda and block_table.shape[0] == S and block_table.stride(1) == 1):
-        _refuse("muxq_paged_attention: block_table is an int32 GPU tensor [S, pages] with contiguous rows")
-    if workspace is None:
-        workspace = alloc_attention_workspace(S, n_heads, c.n_kv_heads, d, max_length, q.device)
-    if not (max_length <= block_table.shape[1] * c.block_size):
-        _refuse("muxq_paged_attention: max_length goes beyond the block table")
-    _check(lib().muxq_paged_attention(_p(q), S, n_heads, _rows(q, "q"), C.byref(c), _p(block_table),
-                                      block_table.stride(0) if S > 1 else block_table.shape[1], _ints(lengths, S, "lengths"),
-                                      max_length, d ** -0.5 if scale is None else scale, _p(out), _rows(out, "out"),
-                                      workspace.data_ptr(), workspace.numel(), _stream()), "muxq_paged_attention")
+    qs, os, ts = q.stride(), out.stride(), block_table.stride()
+    if not (q.dtype is out.dtype is _F16 and block_table.dtype is lengths.dtype is _I32 and q.is_cuda and out.is_cuda and
+            block_table.is_cuda and lengths.is_cuda and d == c.head_dim and out.shape == q.shape and qs[2] == os[2] == 1 and
+            (n_heads == 1 or qs[1] == os[1] == d) and block_table.shape[0] == S and ts[1] == 1 and lengths.is_contiguous() and
+            lengths.numel() == S and max_length <= block_table.shape[1] * c.block_size):
+        _rows(q, "q"), _rows(out, "out"), _flat(lengths, S, _I32, "lengths")
+        _refuse("muxq_paged_attention: q, out and the cache differ in head size, or block_table is no int32 GPU tensor [S, pages] "
+                "with contiguous rows of max_length tokens")
+    args = (q.data_ptr(), S, n_heads, qs[0], C.byref(c), block_table.data_ptr(), ts[0] if S > 1 else block_table.shape[1],
+            lengths.data_ptr(), max_length, d ** -0.5 if scale is None else scale, out.data_ptr(), os[0])
+    _call(lib().muxq_paged_attention, args, workspace, _stream(),
+          lambda: alloc_attention_workspace(S, n_heads, c.n_kv_heads, d, max_length, q.device), "muxq_paged_attention")
     return out
 
 
@@ -719,14 +741,18 @@ def muxq_lora(X, A, B, scales, starts, adapters, Y, out=None, workspace=None):
     requests = adapters.numel()
     if out is None:
         out = torch.empty((M, N), dtype=torch.float16, device=X.device)
-    if not (k == K and B.shape == (n, N, r) and Y.shape[0] == M and out.shape == (M, N)):
-        _refuse("muxq_lora: shapes of X, A, B, Y and out do not fit")
-    if workspace is None:
-        workspace = alloc_lora_workspace(M, K, N, r, requests, X.device)
-    _check(lib().muxq_lora(_p(X), M, K, _rows(X, "X"), _vector(A, n * r * K, "A"), _vector(B, n * N * r, "B"),
-                           _vector(scales, n, "scales", torch.float32), n, r, _ints(starts, requests + 1, "starts"),
-                           _ints(adapters, requests, "adapters"), requests, _p(Y), _rows(Y, "Y"), N, _p(out),
-                           _rows(out, "out"), workspace.data_ptr(), workspace.numel(), _stream()), "muxq_lora")
+    xs, ys, os = X.stride(), Y.stride(), out.stride()
+    if not (X.dtype is A.dtype is B.dtype is Y.dtype is out.dtype is _F16 and scales.dtype is _F32 and starts.dtype is adapters.dtype is _I32 and
+            X.is_cuda and A.is_cuda and B.is_cuda and scales.is_cuda and starts.is_cuda and adapters.is_cuda and Y.is_cuda and out.is_cuda and
+            k == K and B.shape == (n, N, r) and Y.shape == out.shape == (M, N) and xs[1] == ys[1] == os[1] == 1 and A.is_contiguous() and
+            B.is_contiguous() and scales.is_contiguous() and starts.is_contiguous() and adapters.is_contiguous() and
+            scales.numel() == n and starts.numel() == requests + 1):
+        _rows(X, "X"), _rows(Y, "Y"), _rows(out, "out"), _flat(A, n * r * K, _F16, "A"), _flat(B, n * N * r, _F16, "B")
+        _flat(scales, n, _F32, "scales"), _flat(starts, requests + 1, _I32, "starts"), _flat(adapters, requests, _I32, "adapters")
+        _refuse("muxq_lora: shapes of X, A, B, starts, adapters, Y and out do not fit")
+    args = (X.data_ptr(), M, K, xs[0], A.data_ptr(), B.data_ptr(), scales.data_ptr(), n, r, starts.data_ptr(), adapters.data_ptr(),
+            requests, Y.data_ptr(), ys[0], N, out.data_ptr(), os[0])
+    _call(lib().muxq_lora, args, workspace, _stream(), lambda: alloc_lora_workspace(M, K, N, r, requests, X.device), "muxq_lora")
     return out
 
 
@@ -751,24 +777,35 @@ def muxq_norm(x, weight, bias=None, residual=None, residual_scale=1.0, post_weig
         out = torch.empty((M, K), dtype=torch.float16, device=x.device)
     if residual_out is None and (residual is not None or gate is not None or post_weight is not None):
         residual_out = torch.empty((M, K), dtype=torch.float16, device=x.device)
-    if slabs is not None:
-        if not (slabs.is_cuda and slabs.is_contiguous() and slabs.numel() * slabs.element_size() >= norm_slabs(M, K) * k_pad(K) * 2):
-            _refuse("muxq_norm: slabs are too small")
-        if scratch is None:
-            scratch = alloc_norm_scratch(M, K, x.device)
-    for t, name in ((residual, "residual"), (out, "out"), (residual_out, "residual_out")):
-        if not (t is None or t.shape == x.shape):
-            _refuse(f"muxq_norm: {name} and x differ in shape")
-    ldg = 0
-    if gate is not None and gate.dim() == 2:
-        if not (gate.shape == x.shape):
+    if slabs is not None and not (slabs.is_cuda and slabs.is_contiguous() and
+                                  slabs.numel() * slabs.element_size() >= (M if M <= 64 else 1) * ((K + 63) // 64 * 128)):
+        _refuse("muxq_norm: slabs are too small")
+    shape, xs, os = x.shape, x.stride(), out.stride()
+    if not (x.dtype is out.dtype is weight.dtype is _F16 and x.is_cuda and out.is_cuda and weight.is_cuda and out.shape == shape and
+            xs[1] == os[1] == 1 and weight.is_contiguous() and weight.numel() == K):
+        _rows(x, "x"), _rows(out, "out"), _flat(weight, K, _F16, "weight")
+        _refuse("muxq_norm: out and x differ in shape")
+    ldr = ldro = ldg = 0
+    r_at = r_out_at = gate_at = None
+    if residual is not None:
+        r_at, ldr = residual.data_ptr(), _rows(residual, "residual")
+        if residual.shape != shape:
+            _refuse("muxq_norm: residual and x differ in shape")
+    if residual_out is not None:
+        r_out_at, ldro = residual_out.data_ptr(), _rows(residual_out, "residual_out")
+        if residual_out.shape != shape:
+            _refuse("muxq_norm: residual_out and x differ in shape")
+    if gate is not None:
+        gate_at = gate.data_ptr()
+        if gate.dim() == 1:
+            _flat(gate, K, _F16, "gate")
+        elif gate.shape == shape:
+            ldg = _rows(gate, "gate") if M > 1 else K
+        else:
             _refuse("muxq_norm: gate is [K] or [M, K]")
-        ldg = _rows(gate, "gate") if M > 1 else K
-    elif gate is not None:
-        _vector(gate, K, "gate")
-    _check(lib().muxq_norm(_p(x), M, K, _rows(x, "x"), _p(residual), 0 if residual is None else _rows(residual, "residual"),
-                           residual_scale, _vector(post_weight, K, "post_weight"), _vector(post_bias, K, "post_bias"), _p(gate), ldg,
-                           _vector(weight, K, "weight"), _vector(bias, K, "bias"), _NORM[kind], eps, _p(residual_out),
-                           0 if residual_out is None else _rows(residual_out, "residual_out"), _p(out), _rows(out, "out"),
-                           _p(slabs), _p(scratch), 0 if scratch is None else scratch.numel(), _stream()), "muxq_norm")
+    args = (x.data_ptr(), M, K, xs[0], r_at, ldr, residual_scale,
+            None if post_weight is None else _flat(post_weight, K, _F16, "post_weight"),
+            None if post_bias is None else _flat(post_bias, K, _F16, "post_bias"), gate_at, ldg, weight.data_ptr(),
+            None if bias is None else _flat(bias, K, _F16, "bias"), _NORM[kind], eps, r_out_at, ldro, out.data_ptr(), os[0], _p(slabs))
+    _call(lib().muxq_norm, args, scratch, _stream(), lambda: alloc_norm_scratch(M, K, x.device), "muxq_norm")
     return out, residual_out

@@ -280,7 +280,7 @@ Shape shape_of(int M, int K, int N, int r, int n_requests)
     Shape s{};
     s.two_rows = r <= 64 && (long long)M >= 32ll * n_requests;      // prompts: 32 rows share what is read of A and B
     s.tiles = M / (s.two_rows ? 32 : 16) + n_requests;
-    s.two_launches = (long long)r * K >= 1 << 30;
+    s.two_launches = (long long)r * K > 1 << 16;
     s.k_piece = piece_of(K, kDeep, s.tiles, 512);
     s.k_pieces = (K + s.k_piece - 1) / s.k_piece;
     return s;

@@ -541,3 +541,46 @@ def test_step_in_a_graph():
             assert torch.equal(a, b), f"replay {i}"
         want, tol = attend64(q_out, kc, vc, ks, vs, table, lens, d ** -0.5)
         check(o, want, tol, "attention in a graph")
+
+
+# ---- refusals of the binding ---------------------------------------------------------------------
+
+
+def test_bindings_refuse_tensors_that_do_not_fit():
+    g = gen(1)
+    kc, vc, ks, vs = make_cache(g, 4, 2, 16, 64, 8)
+    kh, vh, _, _ = make_cache(g, 4, 2, 16, 64, 16)
+    k, q, slots = normal(g, 3, 2, 64), normal(g, 3, 4, 64), ints([0, 1, 2])
+    table, lengths = ints([[0, 1]] * 3), ints([5, 6, 7])
+    X, Y, A, Bm = normal(g, 5, 64), normal(g, 5, 32), normal(g, 2, 8, 64), normal(g, 2, 32, 8)
+    scales, starts, adapters = torch.ones(2, device=DEV), ints([0, 2, 5]), ints([0, 1])
+    w = normal(g, 64)
+    say("[refuse] through the binding")
+    bad = [
+        lambda: B.muxq_kv_append(k.float(), k, slots, kh, vh), lambda: B.muxq_kv_append(k, k, slots.long(), kh, vh),
+        lambda: B.muxq_kv_append(k, k, slots[:2], kh, vh), lambda: B.muxq_kv_append(k, k[:, :1], slots, kh, vh),
+        lambda: B.muxq_kv_append(k.cpu(), k, slots, kh, vh), lambda: B.muxq_kv_append(k, k, slots, kh, vh[:3]),
+        lambda: B.muxq_kv_append(k, k, slots, kc, vc), lambda: B.muxq_kv_append(k, k, slots, kh, vh, k_scale=ks, v_scale=vs),
+        lambda: B.muxq_kv_append(k, k, slots, kc, vc, k_scale=ks[:2], v_scale=vs), lambda: B.muxq_kv_append(k, k, slots, kh.float(), vh.float()),
+        lambda: B.muxq_kv_append(k, k, slots, kh, vh, q=q[:2]), lambda: B.muxq_kv_append(k, k, slots, kh, vh, q=q.float()),
+        lambda: B.muxq_kv_append(k, k, slots, kh, vh, cos_sin=torch.ones(9, 64, device=DEV)),
+        lambda: B.muxq_kv_append(k, k, slots, kh, vh, cos_sin=torch.ones(9, 64, device=DEV).half(), positions=slots),
+        lambda: B.muxq_kv_append(k, k, slots, kh.transpose(2, 3), vh.transpose(2, 3)),
+        lambda: B.muxq_kv_gather(slots, kh, vh, k_out=k[:2]), lambda: B.muxq_kv_gather(slots.float(), kh, vh),
+        lambda: B.muxq_paged_attention(q[:, :3], kh, vh, table, lengths, 32), lambda: B.muxq_paged_attention(q, kh, vh, table, lengths, 33),
+        lambda: B.muxq_paged_attention(q, kh, vh, table[:2], lengths, 32), lambda: B.muxq_paged_attention(q, kh, vh, table, lengths[:2], 32),
+        lambda: B.muxq_paged_attention(q, kh, vh, table.long(), lengths, 32), lambda: B.muxq_paged_attention(q.cpu(), kh, vh, table, lengths, 32),
+        lambda: B.muxq_paged_attention(q, kh, vh, table, lengths, 32, out=q[:2]), lambda: B.muxq_paged_attention(q, kh, vh, table, lengths, 0),
+        lambda: B.muxq_lora(X, A, Bm, scales, starts, adapters, Y.float()), lambda: B.muxq_lora(X, A[:1], Bm, scales, starts, adapters, Y),
+        lambda: B.muxq_lora(X, A, Bm, scales, starts[:2], adapters, Y), lambda: B.muxq_lora(X, A, Bm.transpose(1, 2), scales, starts, adapters, Y),
+        lambda: B.muxq_lora(X[:, :56], A, Bm, scales, starts, adapters, Y), lambda: B.muxq_lora(X, A, Bm, scales.half(), starts, adapters, Y),
+        lambda: B.muxq_lora(X, A, Bm, scales, starts, adapters, Y, out=Y[:4]),
+        lambda: B.muxq_norm(X, w[:32]), lambda: B.muxq_norm(X, w.float()), lambda: B.muxq_norm(X, w, residual=X[:3]),
+        lambda: B.muxq_norm(X, w, gate=w[:8]), lambda: B.muxq_norm(X, w, post_bias=w), lambda: B.muxq_norm(X.t(), w),
+        lambda: B.muxq_norm(X, w, slabs=torch.empty(64, dtype=torch.uint8, device=DEV)), lambda: B.muxq_norm(X, w, out=X[:2]),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(B.MuxqError):
+            call()
+            pytest.fail(f"call {i} was accepted")
+    torch.cuda.synchronize()
