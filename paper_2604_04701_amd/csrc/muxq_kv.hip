@@ -1,15 +1,14 @@
 // The paged key-value cache: new tokens in, rotated on the way (k_kv_append), and rows back out (k_kv_gather).
 //
-// Both only move data: a token and head is head_dim values in and as many out.  Eight lanes' worth of 8
-// values are one head of 64, so a wave holds several (token, head) pairs side by side, each in a group of
-// P lanes, P the power of two at or above head_dim / 8; the abs-max of a head for its codes is a reduction
-// inside the group.
+// Both only move data: a token and head is head_dim values in and as many out, and what bounds them is memory, or a launch.
+// A lane takes two runs of E values of a head, E = 8 (16 bytes) where the rotation allows it: with halves as pairs
+// the second run is the partners of the first, so that no value crosses lanes.  P lanes, a power of two, stand for
+// a head, and with many tokens each goes through four heads of its token with the sines it has loaded once (the table is binary32: for
+// 8 + 8 values of a head it is twice the head's bytes).  The abs-max of a head for its codes is a reduction over its P lanes.
 #include "muxq_block_kernels.h"
 
 namespace muxq {
 namespace {
-
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float group_max(float v, int P)
 {
@@ -17,98 +16,133 @@ __device__ __forceinline__ float group_max(float v, int P)
     return v;
 }
 
-// Eight values of one head of a token: those at `e` (0, 8, ... of the head) unless they rotate in halves: then four
-// at j and the four at j + rot / 2, their partners.  lo / hi: where the two runs of four stand.
-__device__ __forceinline__ void runs(int unit, int rot, bool interleaved, int &lo, int &hi)
+template <bool kInt8, bool kInterleaved, int E, int kHeadsOf>
+__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int P, int slots_of)
 {
-    const int e = unit * 8;
-    if (e < rot && !interleaved) {
-        lo = unit * 4;
-        hi = lo + rot / 2;
-    } else {
-        lo = e;
-        hi = e + 4;
-    }
-}
-
-template <bool kInt8, bool kInterleaved>
-__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int P)
-{
+    typedef _Float16 Run __attribute__((ext_vector_type(E)));
     const int d = a.c.head_dim, Hkv = a.c.n_kv_heads, heads = a.n_heads + 2 * Hkv;
-    const long long pair = ((long long)blockIdx.x * 256 + threadIdx.x) / P;
+    const uint32_t at_lane = (uint32_t)(blockIdx.x * (256ull / P) + threadIdx.x / P);      // (the launch keeps it below 2^32)
     const int unit = threadIdx.x & (P - 1);
-    const int m = (int)(pair / heads), row = (int)(pair - (long long)m * heads);
+    const int m = (int)(at_lane / (uint32_t)slots_of), row0 = (int)(at_lane - (uint32_t)m * slots_of);
     if (m >= a.M) return;                                     // whole groups
-    const bool is_q = row < a.n_heads, is_v = row >= a.n_heads + Hkv;
-    const int head = is_q ? row : is_v ? row - a.n_heads - Hkv : row - a.n_heads;
-    const _Float16 *src = (is_q ? a.q + (long long)m * a.ldq : is_v ? a.v + (long long)m * a.ldv : a.k + (long long)m * a.ldk) + (long long)head * d;
-    const int rot = is_v ? 0 : a.rot_dim;
+    const bool live = unit * 2 * E < d;
+    const int rot = a.rot_dim, slot = a.slots[m], shift = a.c.block_shift;
     int position = 0;
     bool turned = true;
-    if (a.rot_dim) {
+    if (rot) {
         position = a.positions[m];
         turned = (unsigned)position < (unsigned)a.n_positions;
     }
-    const bool live = unit * 8 < d;
-    int lo = 0, hi = 4;
-    float v[8] = {};
-    if (live) {
-        runs(unit, rot, kInterleaved, lo, hi);
-        const f16x4 x = *(const f16x4 *)(src + lo), y = *(const f16x4 *)(src + hi);
+    // where the lane's two runs stand in a head that rotates (in halves: partners, then what stays as it is, again in halves)
+    // and in one that does not
+    const int flat_lo = unit * E, flat_hi = d / 2 + unit * E;
+    int lo = flat_lo, hi = flat_hi;
+    if (!kInterleaved && rot) {
+        const int u = unit - rot / (2 * E);
+        lo = u < 0 ? unit * E : rot + u * E;
+        hi = u < 0 ? rot / 2 + unit * E : rot + (d - rot) / 2 + u * E;
+    }
+    const bool turn_lo = turned && live && lo < rot, turn_hi = kInterleaved ? turned && live && hi < rot : turn_lo;
+    // angles: E pairs (lo[i], hi[i]), or interleaved E / 2 pairs of each run
+    float c[E], s[E];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (float)x[i], v[4 + i] = (float)y[i];
-        if (unit * 8 < rot && turned) {
-            const float *cs = a.cos_sin + (long long)position * rot + unit * 4;
-            const float4 c4 = *(const float4 *)cs, s4 = *(const float4 *)(cs + rot / 2);
-            const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+    for (int i = 0; i < E; ++i) c[i] = s[i] = 0.0f;
+    if (turn_lo || turn_hi) {
+        const float *const cs = a.cos_sin + (long long)position * rot;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float &p = kInterleaved ? v[2 * i] : v[i], &q = kInterleaved ? v[2 * i + 1] : v[4 + i];
-                const float t = p * c[i] - q * s[i];
-                q = q * c[i] + p * s[i];
-                p = t;
+        for (int i = 0; i < E; i += 4) {
+            const int j = !kInterleaved ? lo + i : E == 4 ? 0 : i < E / 2 ? lo / 2 + i : hi / 2 + i - E / 2;
+            if (i < E / 2 || !kInterleaved ? turn_lo : turn_hi) {
+                const float4 x = *(const float4 *)(cs + j), y = *(const float4 *)(cs + rot / 2 + j);
+                c[i] = x.x, c[i + 1] = x.y, c[i + 2] = x.z, c[i + 3] = x.w;
+                s[i] = y.x, s[i + 1] = y.y, s[i + 2] = y.z, s[i + 3] = y.w;
             }
         }
     }
-    if (is_q) {
-        if (live) {
-            _Float16 *dst = a.q_out + (long long)m * a.ldqo + (long long)head * d;
-            f16x4 x, y;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = (_Float16)v[i], y[i] = (_Float16)v[4 + i];
-            *(f16x4 *)(dst + lo) = x;
-            *(f16x4 *)(dst + hi) = y;
-        }
-        return;
-    }
-    const int slot = a.slots[m], shift = a.c.block_shift;
     const bool stored = turned && slot >= 0 && (slot >> shift) < a.c.n_blocks;
     const int page = stored ? slot >> shift : 0, t = slot & ((1 << shift) - 1);
-    const long long at = page * a.c.ld_block + head * a.c.ld_head + t * a.c.ld_token;
-    char *base = is_v ? a.c.v : a.c.k;
-    if constexpr (!kInt8) {
-        if (live && stored) {
-            f16x4 x, y;
+
+    Run x[kHeadsOf], y[kHeadsOf];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = (_Float16)v[i], y[i] = (_Float16)v[4 + i];
-            *(f16x4 *)((_Float16 *)base + at + lo) = x;
-            *(f16x4 *)((_Float16 *)base + at + hi) = y;
+    for (int h = 0; h < kHeadsOf; ++h) {
+        const int row = row0 + h * slots_of;
+        x[h] = y[h] = Run{};
+        if (live && row < heads) {
+            const bool is_q = row < a.n_heads, is_v = row >= a.n_heads + Hkv;
+            const _Float16 *const src = is_q ? a.q + (long long)m * a.ldq + (long long)row * d
+                                        : is_v ? a.v + (long long)m * a.ldv + (long long)(row - a.n_heads - Hkv) * d
+                                               : a.k + (long long)m * a.ldk + (long long)(row - a.n_heads) * d;
+            x[h] = *(const Run *)(src + (is_v ? flat_lo : lo));
+            y[h] = *(const Run *)(src + (is_v ? flat_hi : hi));
         }
-    } else {
-        float top = 0.0f;
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[i]));
-        top = group_max(top, P);
-        if (!stored) return;
-        const float inv = top > 0.0f ? 127.0f / top : 0.0f;
-        if (live) {
-            uint32_t w[8];
+    for (int h = 0; h < kHeadsOf; ++h) {
+        const int row = row0 + h * slots_of;
+        if (row >= heads) break;                               // whole groups
+        const bool is_q = row < a.n_heads, is_v = row >= a.n_heads + Hkv;
+        const int head = is_q ? row : is_v ? row - a.n_heads - Hkv : row - a.n_heads;
+        const int at_lo = is_v ? flat_lo : lo, at_hi = is_v ? flat_hi : hi;
+        float v[2 * E];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = quant_word(v[i], inv, 127.0f);
-            *(uint32_t *)(base + at + lo) = pack_low_bytes(w[0], w[1], w[2], w[3]);
-            *(uint32_t *)(base + at + hi) = pack_low_bytes(w[4], w[5], w[6], w[7]);
+        for (int i = 0; i < E; ++i) v[i] = (float)x[h][i], v[E + i] = (float)y[h][i];
+        auto turn = [&](float &p, float &q, int i) {
+            const float u = p * c[i] - q * s[i];
+            q = q * c[i] + p * s[i];
+            p = u;
+        };
+        if (!is_v) {
+            if constexpr (!kInterleaved) {
+                if (turn_lo) {
+#pragma unroll
+                    for (int i = 0; i < E; ++i) turn(v[i], v[E + i], i);
+                }
+            } else {
+                if (turn_lo) {
+#pragma unroll
+                    for (int i = 0; i < E / 2; ++i) turn(v[2 * i], v[2 * i + 1], i);
+                }
+                if (turn_hi) {
+#pragma unroll
+                    for (int i = E / 2; i < E; ++i) turn(v[2 * i], v[2 * i + 1], i);
+                }
+            }
         }
-        if (unit == 0) (is_v ? a.c.v_scale : a.c.k_scale)[((long long)page * Hkv + head) * (1 << shift) + t] = top / 127.0f;
+        if (is_q || !kInt8) {
+            _Float16 *dst;
+            if (is_q)
+                dst = a.q_out + (long long)m * a.ldqo + (long long)head * d;
+            else
+                dst = (_Float16 *)(is_v ? a.c.v : a.c.k) + page * a.c.ld_block + head * a.c.ld_head + t * a.c.ld_token;
+            Run u, w;
+#pragma unroll
+            for (int i = 0; i < E; ++i) u[i] = (_Float16)v[i], w[i] = (_Float16)v[E + i];
+            if (live && (is_q || stored)) {
+                *(Run *)(dst + at_lo) = u;
+                *(Run *)(dst + at_hi) = w;
+            }
+            continue;
+        }
+        if constexpr (kInt8) {
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 2 * E; ++i) top = fmaxf(top, fabsf(v[i]));
+            top = group_max(top, P);
+            if (!stored) continue;
+            const float inv = top > 0.0f ? 127.0f / top : 0.0f;
+            char *const dst = (is_v ? a.c.v : a.c.k) + page * a.c.ld_block + head * a.c.ld_head + t * a.c.ld_token;
+            uint32_t w[2 * E];
+#pragma unroll
+            for (int i = 0; i < 2 * E; ++i) w[i] = quant_word(v[i], inv, 127.0f);
+            if (live) {
+#pragma unroll
+                for (int i = 0; i < E; i += 4) {
+                    *(uint32_t *)(dst + at_lo + i) = pack_low_bytes(w[i], w[i + 1], w[i + 2], w[i + 3]);
+                    *(uint32_t *)(dst + at_hi + i) = pack_low_bytes(w[E + i], w[E + i + 1], w[E + i + 2], w[E + i + 3]);
+                }
+                if (unit == 0) (is_v ? a.c.v_scale : a.c.k_scale)[((long long)page * Hkv + head) * (1 << shift) + t] = top / 127.0f;
+            }
+        }
     }
 }
 
@@ -144,18 +178,32 @@ __global__ __launch_bounds__(256) void k_kv_gather(const int32_t *slots, int M, 
 
 }  // namespace
 
+template <int E, int kHeadsOf>
+static hipError_t launch_append(const AppendArgs &a, int P, bool int8, bool interleaved, hipStream_t s)
+{
+    const int heads = a.n_heads + 2 * a.c.n_kv_heads, slots_of = (heads + kHeadsOf - 1) / kHeadsOf;
+    const unsigned long long groups = (unsigned long long)a.M * slots_of, wgs = (groups + 256 / P - 1) / (256 / P);
+    if (wgs * (256 / P) > 0xffffffffull || wgs > 0x7fffffffull) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)wgs);
+    if constexpr (E == 8)
+        if (interleaved)
+            return int8 ? launch_kernel(k_kv_append<true, true, E, kHeadsOf>, grid, dim3(256), 0, s, a, P, slots_of)
+                        : launch_kernel(k_kv_append<false, true, E, kHeadsOf>, grid, dim3(256), 0, s, a, P, slots_of);
+    return int8 ? launch_kernel(k_kv_append<true, false, E, kHeadsOf>, grid, dim3(256), 0, s, a, P, slots_of)
+                : launch_kernel(k_kv_append<false, false, E, kHeadsOf>, grid, dim3(256), 0, s, a, P, slots_of);
+}
+
 hipError_t launch_kv_append(const AppendArgs &a, bool int8, bool interleaved, hipStream_t s)
 {
-    int P = 2;
-    while (P * 8 < a.c.head_dim) P *= 2;
-    const long long lanes = (long long)a.M * (a.n_heads + 2 * a.c.n_kv_heads) * P;
-    const long long wgs = (lanes + 255) / 256;
-    if (wgs > 0x7fffffffll) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)wgs);
-    if (int8) return interleaved ? launch_kernel(k_kv_append<true, true>, grid, dim3(256), 0, s, a, P)
-                                 : launch_kernel(k_kv_append<true, false>, grid, dim3(256), 0, s, a, P);
-    return interleaved ? launch_kernel(k_kv_append<false, true>, grid, dim3(256), 0, s, a, P)
-                       : launch_kernel(k_kv_append<false, false>, grid, dim3(256), 0, s, a, P);
+    // runs of 8 unless halves of the rotated dimensions are not whole runs (interleaved pairs stand inside a run)
+    const int E = interleaved || a.rot_dim % 16 == 0 ? 8 : 4;
+    int P = 1;
+    while (P * 2 * E < a.c.head_dim) P *= 2;
+    // one head to a lane while that does not fill the chip (64 tokens of 48 heads with 8-bit codes: 5.2 us with the read-back,
+    // 6.9 with four), then four (8192 tokens: 40.3 us, 50.3 with one)
+    const bool many = (long long)a.M * (a.n_heads + 2 * a.c.n_kv_heads) * P > 1 << 18;
+    if (E == 8) return many ? launch_append<8, 4>(a, P, int8, interleaved, s) : launch_append<8, 1>(a, P, int8, interleaved, s);
+    return many ? launch_append<4, 4>(a, P, int8, false, s) : launch_append<4, 1>(a, P, int8, false, s);
 }
 
 hipError_t launch_kv_gather(const int32_t *slots, int M, const KvView &c, bool int8, _Float16 *k_out, int ldk,
