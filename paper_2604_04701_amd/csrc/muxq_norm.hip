@@ -15,10 +15,22 @@ namespace {
 
 constexpr int kMaxGroups = 512;             // workgroups that leave maxima
 
+// The value of another lane of the same 16, without LDS.
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xf, 0xf, false));
+}
+
 template <int W>
 __device__ __forceinline__ float row_sum(float v, float *sh, int &turn)
 {
-    for (int x = 1; x < 64; x <<= 1) v += __shfl_xor(v, x, 64);
+    v += dpp<0xB1>(v);          // lanes xor 1, xor 2, then the other half of 8, of 16
+    v += dpp<0x4E>(v);
+    v += dpp<0x141>(v);
+    v += dpp<0x140>(v);
+    v += __shfl_xor(v, 16, 64);
+    v += __shfl_xor(v, 32, 64);
     if constexpr (W > 1) {                  // two buffers in turn: one barrier a sum
         float *const s = sh + (turn ^= W);
         if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
@@ -158,18 +170,28 @@ __global__ __launch_bounds__(64 * (W == 1 ? 8 : W)) void k_norm(NormArgs n, uint
     }
 }
 
-// Rows of maxima folded into one: 8 runs of 8 channels to a workgroup, 32 threads down each.
+// Rows of maxima folded into one: 4 runs of 8 channels (64 bytes) to a workgroup, 64 threads down each.
 __global__ __launch_bounds__(256) void k_norm_fold(const uint16_t *maxima, int rows, int k_pad, uint16_t *slab)
 {
-    __shared__ uint4 top[256];
-    const int c = (blockIdx.x * 8 + (threadIdx.x & 7)) * 8;
+    __shared__ uint4 top[4][4];
+    const int run = threadIdx.x & 3, c = (blockIdx.x * 4 + run) * 8;      // (k_pad is a multiple of 64)
+    const uint16_t *const p = maxima + c;
     uint4 x = {0, 0, 0, 0};
-    if (c < k_pad)
-        for (int m = threadIdx.x >> 3; m < rows; m += 32) x = absmax_step(x, *(const uint4 *)(maxima + (long long)m * k_pad + c));
-    top[threadIdx.x] = x;
+#pragma unroll
+    for (int i = 0; i < kMaxGroups / 64; ++i) {
+        const int m = (threadIdx.x >> 2) + 64 * i;
+        if (m < rows) x = absmax_step(x, *(const uint4 *)(p + (long long)m * k_pad));
+    }
+    for (int y = 4; y < 64; y <<= 1) {
+        const uint4 o = {(uint32_t)__shfl_xor((int)x.x, y, 64), (uint32_t)__shfl_xor((int)x.y, y, 64), (uint32_t)__shfl_xor((int)x.z, y, 64),
+                         (uint32_t)__shfl_xor((int)x.w, y, 64)};
+        x = absmax_step(x, o);
+    }
+    if ((threadIdx.x & 63) < 4) top[threadIdx.x >> 6][run] = x;
     __syncthreads();
-    if (threadIdx.x < 8 && c < k_pad) {
-        for (int i = 1; i < 32; ++i) x = absmax_step(x, top[i * 8 + threadIdx.x]);
+    if (threadIdx.x < 4) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) x = absmax_step(x, top[w][run]);
         *(uint4 *)(slab + c) = x;
     }
 }
@@ -209,7 +231,7 @@ hipError_t launch_norm(const NormArgs &n, bool rms, hipStream_t s)
     else
         e = C <= 2 ? launch<16, 2>(n, rms, maxima, s) : launch<16, 4>(n, rms, maxima, s);
     if (e != hipSuccess || maxima == nullptr) return e;
-    return launch_kernel(k_norm_fold, dim3((n.k_pad + 63) / 64), dim3(256), 0, s, maxima, groups_of(n.M, n.K), n.k_pad, n.slabs);
+    return launch_kernel(k_norm_fold, dim3(n.k_pad / 32), dim3(256), 0, s, maxima, groups_of(n.M, n.K), n.k_pad, n.slabs);
 }
 
 }  // namespace muxq
