@@ -104,7 +104,7 @@ int muxq_paged_attention(const void *Q_fp16, int S, int n_heads, int ldq, const 
  * are clamped to [0, M].
  * workspace: muxq_lora_workspace_bytes(...) bytes, 16-byte aligned, content undefined on entry; NULL where
  * that is 0.  Calls that share one must not overlap in time.
- * Rules: K, N, r multiples of 8, r <= 128, K, N <= 2^21, M <= 2^24, n_adapters >= 1,
+ * Rules: K, N, r multiples of 8, r <= 128, K, N <= 2^21, M <= 2^24, row strides <= 2^25, n_adapters >= 1,
  * 1 <= n_requests <= 2^20. */
 size_t muxq_lora_workspace_bytes(int M, int K, int N, int r, int n_requests);   /* 0 on bad shapes, and where none is needed */
 int muxq_lora(const void *X_fp16, int M, int K, int ldx, const void *A_fp16, const void *B_fp16,

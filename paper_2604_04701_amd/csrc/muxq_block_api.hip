@@ -169,6 +169,8 @@ int muxq_paged_attention(const void *Q, int S, int n_heads, int ldq, const muxq_
     return MUXQ_OK;
 }
 
+constexpr int kMaxLd = 1 << 25;              // 32 rows within 32-bit offsets
+
 static bool lora_shape_ok(int M, int K, int N, int r, int n_requests)
 {
     return M >= 1 && M <= kMaxRows && K >= 8 && K % 8 == 0 && K <= kMaxCols && N >= 8 && N % 8 == 0 && N <= kMaxCols &&
@@ -185,7 +187,9 @@ int muxq_lora(const void *X, int M, int K, int ldx, const void *A, const void *B
               const void *Y, int ldy, int N, void *out, int ldo, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (!X || !A || !B || !scales || !starts || !adapters || !Y || !out) return MUXQ_ERR_NULL;
-    if (!lora_shape_ok(M, K, N, r, n_requests) || n_adapters < 1 || bad_ld(ldx, K) || bad_ld(ldy, N) || bad_ld(ldo, N)) return MUXQ_ERR_SHAPE;
+    if (!lora_shape_ok(M, K, N, r, n_requests) || n_adapters < 1 || bad_ld(ldx, K) || bad_ld(ldy, N) || bad_ld(ldo, N) ||
+        ldx > kMaxLd || ldy > kMaxLd || ldo > kMaxLd)
+        return MUXQ_ERR_SHAPE;
     if (!aligned(X, 16) || !aligned(A, 16) || !aligned(B, 16) || !aligned(Y, 16) || !aligned(out, 16) || !aligned(scales, 4) ||
         !aligned(starts, 4) || !aligned(adapters, 4))
         return MUXQ_ERR_ALIGN;

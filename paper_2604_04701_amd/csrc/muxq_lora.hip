@@ -16,9 +16,18 @@ namespace muxq {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kCols = 64 * kWaves;      // output channels of a workgroup's step
 constexpr int kDeep = 64 * kWaves;                                          // channels of X of one
+
+// What this wave wrote to LDS is there for its other lanes.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 // First row of request q, whatever the caller's bounds hold.
 __device__ __forceinline__ int start_of(const LoraArgs &g, int q) { return min(max(g.starts[q], 0), g.M); }
@@ -26,21 +35,32 @@ __device__ __forceinline__ int start_of(const LoraArgs &g, int q) { return min(m
 enum Part { kBoth, kDown, kUp };
 
 // kTM: tiles of 16 rows, kRT: tiles of 16 ranks (of the power of two at or above r).  piece: what a workgroup in y takes,
-// channels of Y, or channels of X in the first of two launches; pieces: of X.
+// channels of Y, or channels of X in the first of two launches; pieces: of X.  (The pieces of a tile one after the other in the
+// grid are up to a sixth slower.)
 template <int kTM, int kRT, Part kPart>
 __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pieces)
 {
     constexpr int T = 16 * kTM, R = 16 * kRT, RS = kRT == 1 ? 1 : kRT / 2, LD = R + 4, LH = 32 * RS + 8;
-    __shared__ float part[kPart == kUp ? 1 : kWaves / 2][T][LD];
+    // The operands want 16 rows on neighbouring lanes, which memory gives 16 bytes at a time: with many rows each wave
+    // loads whole runs of rows and turns them in a place of its own in LDS (a fifth of the requests of the loads).
+    constexpr bool kTurnDown = kPart != kUp && kTM == 2, kTurnUp = kPart != kDown && kTM == 2 && RS == 1;
+    constexpr int kLdDown = 64 + 8, kDownBytes = kTurnDown ? kWaves * 32 * kLdDown * 2 : 0;
+    constexpr int kLdUp = 32 + 8, kUpBlock = 16 * kLdUp + 32, kUpBytes = kTurnUp ? kWaves * 4 * kUpBlock * 2 : 0;
+    constexpr int kPartBytes = kPart == kUp ? 0 : kWaves / 2 * T * LD * 4;
+    constexpr int kBytes = kDownBytes > kUpBytes ? (kDownBytes > kPartBytes ? kDownBytes : kPartBytes) : (kUpBytes > kPartBytes ? kUpBytes : kPartBytes);
+    __shared__ __align__(16) char lds[kBytes > 0 ? kBytes : 16];
+    float(*const part)[T][LD] = (float(*)[T][LD])lds;
+    _Float16 *const turn_down = (_Float16 *)lds + (threadIdx.x >> 6) * (32 * kLdDown);
+    _Float16 *const turn_up = (_Float16 *)lds + (threadIdx.x >> 6) * (4 * kUpBlock);
     __shared__ __align__(16) _Float16 h_hi[kPart == kDown ? 1 : T][LH], h_lo[kPart == kDown ? 1 : T][LH];
-    __shared__ float factor[T];
+    __shared__ __align__(16) float factor[T];
     __shared__ int found[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, gr = lane >> 4;
 
     // Tiles are numbered so that request q has those from starts[q] / T + q on: as many as it can need.  The
     // request of tile b is the last one that starts there or before: every thread looks at one (of R > 512: at
     // one of each so many, then at those in between).
-    const int b = blockIdx.x;
+    const int b = blockIdx.x, mine = blockIdx.y;
     int q = 0;
     for (int step = (g.n_requests + kThreads - 1) / kThreads;;) {
         int count = 0;
@@ -63,7 +83,7 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
     const int first = start_of(g, q), row0 = first + (b - (first / T + q)) * T;
     const int rows = min(T, start_of(g, q + 1) - row0);
     if (rows <= 0 || row0 < first) return;
-    const int n0 = blockIdx.y * piece, n1 = min(g.N, n0 + piece);
+    const int n0 = mine * piece, n1 = min(g.N, n0 + piece);
     const int ad = g.adapters[q];
     const _Float16 *const y = g.y + (long long)row0 * g.ldy;
     _Float16 *const out = g.out + (long long)row0 * g.ldo;
@@ -83,38 +103,91 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
         for (int t = 0; t < kRT; ++t) ar[t] = g.a + ((long long)ad * g.r + min(16 * t + col, g.r - 1)) * g.K;
         f32x4 acc[kTM][kRT] = {};
         // 64 channels at a time, the next ones on their way while these are in the matrix pipes
+        constexpr int NX = kTurnDown ? 4 : 2 * kTM, NA = 2 * kRT;          // loads of a lane
         struct Buffer {
-            f16x8 x[2][kTM], a[2][kRT];
+            f16x8 x[NX], a[NA];
         } buf[2];
-        const int kb = kPart == kDown ? blockIdx.y * piece : 0, ke = kPart == kDown ? min(g.K, kb + piece) : g.K;
+        const int kb = kPart == kDown ? mine * piece : 0, ke = kPart == kDown ? min(g.K, kb + piece) : g.K;
+        const int turn_row = lane >> 3, turn_k = (lane & 7) * 8;           // rows of 64 channels, 8 at a time
         auto ask = [&](Buffer &w, int k0) {
+            if constexpr (kTurnDown) {
+                const int k = k0 + turn_k;
+                const bool there = k < g.K;
+#pragma unroll
+                for (int i = 0; i < NX; ++i) w.x[i] = *(const f16x8 *)(g.x + (long long)(row0 + min(8 * i + turn_row, rows - 1)) * g.ldx + (there ? k : 0));
+#pragma unroll
+                for (int i = 0; i < NA; ++i)
+                    w.a[i] = *(const f16x8 *)(g.a + ((long long)ad * g.r + min(8 * i + turn_row, g.r - 1)) * g.K + (there ? k : 0));
+                if (k0 + 64 > g.K && !there) {
+#pragma unroll
+                    for (int i = 0; i < NX; ++i) w.x[i] = f16x8{};
+#pragma unroll
+                    for (int i = 0; i < NA; ++i) w.a[i] = f16x8{};
+                }
+                return;
+            }
             const bool whole = k0 + 64 <= g.K;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const int k = k0 + 32 * s + 8 * gr, at = whole || k < g.K ? k : 0;
 #pragma unroll
-                for (int t = 0; t < kTM; ++t) w.x[s][t] = *(const f16x8 *)(xr[t] + at);
+                for (int t = 0; t < kTM; ++t) w.x[s * kTM + t] = *(const f16x8 *)(xr[t] + at);
 #pragma unroll
-                for (int t = 0; t < kRT; ++t) w.a[s][t] = *(const f16x8 *)(ar[t] + at);
+                for (int t = 0; t < kRT; ++t) w.a[s * kRT + t] = *(const f16x8 *)(ar[t] + at);
             }
             if (!whole) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
                     if (k0 + 32 * s + 8 * gr >= g.K) {
 #pragma unroll
-                        for (int t = 0; t < kTM; ++t) w.x[s][t] = f16x8{};
+                        for (int t = 0; t < kTM; ++t) w.x[s * kTM + t] = f16x8{};
 #pragma unroll
-                        for (int t = 0; t < kRT; ++t) w.a[s][t] = f16x8{};
+                        for (int t = 0; t < kRT; ++t) w.a[s * kRT + t] = f16x8{};
                     }
             }
         };
         auto add = [&](const Buffer &w) {
+            if constexpr (kTurnDown) {
+                f16x8 xv[2][kTM];
+                auto turn = [&](const f16x8 *from) {                       // 32 rows through the wave's place
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) *(f16x8 *)(turn_down + (8 * i + turn_row) * kLdDown + turn_k) = from[i];
+                    wave_sync();
+                };
+                auto turned = [&](int s, int t) { return *(const f16x8 *)(turn_down + (16 * t + col) * kLdDown + 32 * s + 8 * gr); };
+                turn(w.x);
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int t = 0; t < kTM; ++t) xv[s][t] = turned(s, t);
+                wave_sync();
+#pragma unroll
+                for (int u0 = 0; u0 < kRT; u0 += 2) {
+                    if constexpr (kRT == 1) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) *(f16x8 *)(turn_down + (8 * i + turn_row) * kLdDown + turn_k) = w.a[i];
+                        wave_sync();
+                    } else {
+                        turn(w.a + 2 * u0);
+                    }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int u = 0; u < (kRT == 1 ? 1 : 2); ++u) {
+                            const f16x8 av = turned(s, u);
+#pragma unroll
+                            for (int t = 0; t < kTM; ++t) acc[t][u0 + u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[s][t], av, acc[t][u0 + u], 0, 0, 0);
+                        }
+                    wave_sync();
+                }
+                return;
+            }
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int t = 0; t < kTM; ++t)
 #pragma unroll
-                    for (int u = 0; u < kRT; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.x[s][t], w.a[s][u], acc[t][u], 0, 0, 0);
+                    for (int u = 0; u < kRT; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.x[s * kTM + t], w.a[s * kRT + u], acc[t][u], 0, 0, 0);
         };
         int k0 = kb + wave * 64;
         if (k0 < ke) ask(buf[0], k0);
@@ -125,6 +198,7 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
             if (k0 + 2 * kDeep < ke) ask(buf[0], k0 + 2 * kDeep);
             add(buf[1]);
         }
+        if constexpr (kTurnDown) __syncthreads();                  // the parts stand where the waves' places were
         // parts of the upper waves to the lower ones, then all of them to the rows' owners
         auto put = [&](int at) {
 #pragma unroll
@@ -150,63 +224,88 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
     if constexpr (kPart == kDown) {
         for (int i = tid; i < rows * g.r; i += kThreads) {
             const int m = i / g.r, j = i - m * g.r;
-            g.h[((long long)blockIdx.y * g.M + row0 + m) * g.r + j] = (part[0][m][j] + part[1][m][j]) + (part[2][m][j] + part[3][m][j]);
+            g.h[((long long)mine * g.M + row0 + m) * g.r + j] = (part[0][m][j] + part[1][m][j]) + (part[2][m][j] + part[3][m][j]);
         }
         return;
     }
-    // 64 channels of the output: row m of operand u is channel nb + 32 (u / 2) + 8 (m / 4) + 4 (u % 2) + m % 4, so that a lane ends
-    // up with two runs of 8 of a row.  (Loads past the tile's rows, the strip's channels or the ranks go to what is
+    // 64 channels of the output: column c of operand u is channel nb + 4 c + u, so that a lane ends up with 4 neighbours of 4 rows and
+    // 16 lanes with 128 bytes of a row of Y.  (Loads past the tile's rows, the strip's channels or the ranks go to what is
     // there; none of it is stored or counts.)  The next ones are on their way while these are worked on, the first ones while
     // H is.
+    constexpr int NB = kTurnUp ? 4 : 4 * RS;           // loads of a lane: 64 rows of B, at most 64 bytes each, or as operands
     struct Ahead {
-        f16x8 y[kTM][2], b[4][RS];
+        f16x4 y[kTM][4];
+        f16x8 b[NB];
     } ahead;
     const _Float16 *const br = g.b + (long long)ad * g.N * g.r;
+    const uint32_t per_row = (65536 + (g.r >> 3) - 1) / (g.r >> 3);        // q / (r / 8) is q * this >> 16 for q < 256
     auto ask_up = [&](int nb) {
 #pragma unroll
         for (int t = 0; t < kTM; ++t)
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-                ahead.y[t][x] = *(const f16x8 *)(y + (long long)min(16 * t + col, rows - 1) * g.ldy + min(nb + 32 * x + 8 * gr, n1 - 8));
+            for (int i = 0; i < 4; ++i)
+                ahead.y[t][i] = *(const f16x4 *)(y + (uint32_t)(min(16 * t + 4 * gr + i, rows - 1) * g.ldy + min(nb + 4 * col, n1 - 4)));
+        if constexpr (kTurnUp) {
+            const int last = (n1 - nb) * g.r - 8;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int nn = min(nb + 32 * (u >> 1) + 8 * (col >> 2) + 4 * (u & 1) + (col & 3), n1 - 1);
+            for (int i = 0; i < NB; ++i) ahead.b[i] = *(const f16x8 *)(br + (long long)nb * g.r + (uint32_t)min((64 * i + lane) * 8, last));
+        } else {
 #pragma unroll
-            for (int s = 0; s < RS; ++s) {
-                const int k = 32 * s + 8 * gr;
-                ahead.b[u][s] = *(const f16x8 *)(br + (long long)nn * g.r + (k < g.r ? k : 0));
-            }
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int s = 0; s < RS; ++s) {
+                    const int k = 32 * s + 8 * gr;
+                    ahead.b[u * RS + s] = *(const f16x8 *)(br + (long long)min(nb + 4 * col + u, n1 - 1) * g.r + (k < g.r ? k : 0));
+                }
         }
     };
     int nb = n0 + wave * 64;
     if (kPart == kUp && nb < n1) ask_up(nb);
     const float scale = g.scales[ad];
-    for (int m = wave; m < T; m += kWaves) {
-        constexpr int per = R > 64 ? R / 64 : 1;
-        float v[per], top = 0.0f;
+    // the wave's rows of H, all of their parts requested before the first is used
+    constexpr int per = R > 64 ? R / 64 : 1, kOwn = T / kWaves;
+    float v[kOwn][per];
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o)
 #pragma unroll
         for (int i = 0; i < per; ++i) {
-            const int j = lane + 64 * i;
-            v[i] = 0.0f;
-            if (j < g.r) {
-                if constexpr (kPart == kUp) {
-                    if (m < rows)
-                        for (int x = 0; x < pieces; ++x) v[i] += g.h[((long long)x * g.M + row0 + m) * g.r + j];
-                } else {
-                    v[i] = (part[0][m][j] + part[1][m][j]) + (part[2][m][j] + part[3][m][j]);
-                }
-            }
-            top = fmaxf(top, fabsf(v[i]));
+            const int m = wave + kWaves * o, j = lane + 64 * i;
+            v[o][i] = 0.0f;
+            if (kPart == kBoth && j < g.r) v[o][i] = (part[0][m][j] + part[1][m][j]) + (part[2][m][j] + part[3][m][j]);
         }
-        for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-        const uint32_t ex = min(max(__float_as_uint(top) >> 23, 15u), 250u);
+    if constexpr (kPart == kUp) {
+#pragma unroll 4
+        for (int x = 0; x < pieces; ++x)
+#pragma unroll
+            for (int o = 0; o < kOwn; ++o)
+#pragma unroll
+                for (int i = 0; i < per; ++i)
+                    v[o][i] += g.h[((long long)x * g.M + row0 + min(wave + kWaves * o, rows - 1)) * g.r + min(lane + 64 * i, g.r - 1)];
+    }
+    float top[kOwn];
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o) {
+        top[o] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            if (lane + 64 * i >= g.r) v[o][i] = 0.0f;
+            top[o] = fmaxf(top[o], fabsf(v[o][i]));
+        }
+    }
+    for (int x = 1; x < 64; x <<= 1)
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o) top[o] = fmaxf(top[o], __shfl_xor(top[o], x, 64));
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o) {
+        const int m = wave + kWaves * o;
+        const uint32_t ex = min(max(__float_as_uint(top[o]) >> 23, 15u), 250u);
         const float up = __uint_as_float((268u - ex) << 23);            // the row's largest to 2^14 .. 2^15
         if (lane == 0) factor[m] = scale * __uint_as_float((ex - 14u) << 23);
 #pragma unroll
         for (int i = 0; i < per; ++i) {
             const int j = lane + 64 * i;
             if (j < 32 * RS) {
-                const float w = v[i] * up;
+                const float w = v[o][i] * up;
                 const _Float16 hi = (_Float16)w;
                 h_hi[m][j] = hi;
                 h_lo[m][j] = (_Float16)(w - (float)hi);
@@ -216,10 +315,10 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
     __syncthreads();
 
     f16x8 hh[kTM][RS], hl[kTM][RS];
-    float f[kTM];
+    f32x4 f[kTM];
 #pragma unroll
     for (int t = 0; t < kTM; ++t) {
-        f[t] = factor[16 * t + col];
+        f[t] = *(const f32x4 *)&factor[16 * t + 4 * gr];
 #pragma unroll
         for (int s = 0; s < RS; ++s) {
             hh[t][s] = *(const f16x8 *)&h_hi[16 * t + col][32 * s + 8 * gr];
@@ -229,33 +328,49 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
     if (kPart != kUp && nb < n1) ask_up(nb);
     for (; nb < n1; nb += kCols) {
         f32x4 o[kTM][4] = {};
+        if constexpr (kTurnUp) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const int q = 64 * i + lane, n = (q * per_row) >> 16, k = q - n * (g.r >> 3);
+                if (n < 64) *(f16x8 *)(turn_up + (n & 3) * kUpBlock + (n >> 2) * kLdUp + 8 * k) = ahead.b[i];
+            }
+            wave_sync();
+        }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int s = 0; s < RS; ++s) {
-                const f16x8 b = 32 * s + 8 * gr < g.r ? ahead.b[u][s] : f16x8{};
+                f16x8 b = {};
+                if (32 * s + 8 * gr < g.r) {
+                    if constexpr (kTurnUp)
+                        b = *(const f16x8 *)(turn_up + u * kUpBlock + col * kLdUp + 8 * gr);
+                    else
+                        b = ahead.b[u * RS + s];
+                }
 #pragma unroll
                 for (int t = 0; t < kTM; ++t) {
-                    o[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, hh[t][s], o[t][u], 0, 0, 0);
-                    o[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, hl[t][s], o[t][u], 0, 0, 0);
+                    o[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hh[t][s], b, o[t][u], 0, 0, 0);
+                    o[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hl[t][s], b, o[t][u], 0, 0, 0);
                 }
             }
-        f16x8 yv[kTM][2];
+        if constexpr (kTurnUp) wave_sync();
+        f16x4 yv[kTM][4];
 #pragma unroll
         for (int t = 0; t < kTM; ++t)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) yv[t][x] = ahead.y[t][x];
+            for (int i = 0; i < 4; ++i) yv[t][i] = ahead.y[t][i];
         if (nb + kCols < n1) ask_up(nb + kCols);
+        const int n = nb + 4 * col;
 #pragma unroll
         for (int t = 0; t < kTM; ++t)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int n = nb + 32 * x + 8 * gr;
-                if (16 * t + col >= rows || n >= n1) continue;
-                f16x8 r;
+            for (int i = 0; i < 4; ++i) {
+                const int m = 16 * t + 4 * gr + i;
+                if (m >= rows || n >= n1) continue;
+                f16x4 r;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r[i] = (_Float16)((float)yv[t][x][i] + f[t] * o[t][2 * x + (i >> 2)][i & 3]);
-                *(f16x8 *)(out + (long long)(16 * t + col) * g.ldo + n) = r;
+                for (int u = 0; u < 4; ++u) r[u] = (_Float16)((float)yv[t][i][u] + f[t][i] * o[t][u][i]);
+                *(f16x4 *)(out + (uint32_t)(m * g.ldo + n)) = r;
             }
     }
 }
