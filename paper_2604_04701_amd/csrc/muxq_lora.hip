@@ -38,7 +38,7 @@ enum Part { kBoth, kDown, kUp };
 // channels of Y, or channels of X in the first of two launches; pieces: of X.  (The pieces of a tile one after the other in the
 // grid are up to a sixth slower.)
 template <int kTM, int kRT, Part kPart>
-__global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pieces)
+__global__ __launch_bounds__(kThreads, kRT == 1 || (kRT == 2 && (kTM == 1 || kPart == kUp)) ? 4 : 2) void k_lora(LoraArgs g, int piece, int pieces)
 {
     constexpr int T = 16 * kTM, R = 16 * kRT, RS = kRT == 1 ? 1 : kRT / 2, LD = R + 4, LH = 32 * RS + 8;
     // The operands want 16 rows on neighbouring lanes, which memory gives 16 bytes at a time: with many rows each wave
@@ -94,6 +94,41 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
         return;
     }
 
+    // 64 channels of the output: column c of operand u is channel nb + 4 c + u, so that a lane ends up with 4 neighbours of 4 rows and
+    // 16 lanes with 128 bytes of a row of Y.  (Loads past the tile's rows, the strip's channels or the ranks go to what is
+    // there; none of it is stored or counts.)  The next ones are on their way while these are worked on, the first ones while
+    // H is.
+    constexpr int NB = kTurnUp ? 4 : 4 * RS;           // loads of a lane: 64 rows of B, at most 64 bytes each, or as operands
+    struct Ahead {
+        f16x4 y[kTM][4];
+        f16x8 b[NB];
+    } ahead;
+    const _Float16 *const br = g.b + (long long)ad * g.N * g.r;
+    const uint32_t per_row = (65536 + (g.r >> 3) - 1) / (g.r >> 3);        // q / (r / 8) is q * this >> 16 for q < 256
+    auto ask_up = [&](int nb) {
+#pragma unroll
+        for (int t = 0; t < kTM; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                ahead.y[t][i] = *(const f16x4 *)(y + (uint32_t)(min(16 * t + 4 * gr + i, rows - 1) * g.ldy + min(nb + 4 * col, n1 - 4)));
+        if constexpr (kTurnUp) {
+            const int last = (n1 - nb) * g.r - 8;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) ahead.b[i] = *(const f16x8 *)(br + (long long)nb * g.r + (uint32_t)min((64 * i + lane) * 8, last));
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int s = 0; s < RS; ++s) {
+                    const int k = 32 * s + 8 * gr;
+                    ahead.b[u * RS + s] = *(const f16x8 *)(br + (long long)min(nb + 4 * col + u, n1 - 1) * g.r + (k < g.r ? k : 0));
+                }
+        }
+    };
+    int nb = n0 + wave * 64;
+    constexpr bool kEarly = kPart == kUp || (kPart == kBoth && kTM == 1 && kRT <= 2);      // (else the first product needs the registers)
+    if (kEarly && nb < n1) ask_up(nb);
+    const float scale = g.scales[ad];
     if constexpr (kPart != kUp) {
         // H: lanes of a 16-lane row read 64 bytes of 16 rows; rows past the tile's last repeat it, ranks past r the last one
         const _Float16 *xr[kTM], *ar[kRT];
@@ -228,40 +263,6 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
         }
         return;
     }
-    // 64 channels of the output: column c of operand u is channel nb + 4 c + u, so that a lane ends up with 4 neighbours of 4 rows and
-    // 16 lanes with 128 bytes of a row of Y.  (Loads past the tile's rows, the strip's channels or the ranks go to what is
-    // there; none of it is stored or counts.)  The next ones are on their way while these are worked on, the first ones while
-    // H is.
-    constexpr int NB = kTurnUp ? 4 : 4 * RS;           // loads of a lane: 64 rows of B, at most 64 bytes each, or as operands
-    struct Ahead {
-        f16x4 y[kTM][4];
-        f16x8 b[NB];
-    } ahead;
-    const _Float16 *const br = g.b + (long long)ad * g.N * g.r;
-    const uint32_t per_row = (65536 + (g.r >> 3) - 1) / (g.r >> 3);        // q / (r / 8) is q * this >> 16 for q < 256
-    auto ask_up = [&](int nb) {
-#pragma unroll
-        for (int t = 0; t < kTM; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                ahead.y[t][i] = *(const f16x4 *)(y + (uint32_t)(min(16 * t + 4 * gr + i, rows - 1) * g.ldy + min(nb + 4 * col, n1 - 4)));
-        if constexpr (kTurnUp) {
-            const int last = (n1 - nb) * g.r - 8;
-#pragma unroll
-            for (int i = 0; i < NB; ++i) ahead.b[i] = *(const f16x8 *)(br + (long long)nb * g.r + (uint32_t)min((64 * i + lane) * 8, last));
-        } else {
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int s = 0; s < RS; ++s) {
-                    const int k = 32 * s + 8 * gr;
-                    ahead.b[u * RS + s] = *(const f16x8 *)(br + (long long)min(nb + 4 * col + u, n1 - 1) * g.r + (k < g.r ? k : 0));
-                }
-        }
-    };
-    int nb = n0 + wave * 64;
-    if (kPart == kUp && nb < n1) ask_up(nb);
-    const float scale = g.scales[ad];
     // the wave's rows of H, all of their parts requested before the first is used
     constexpr int per = R > 64 ? R / 64 : 1, kOwn = T / kWaves;
     float v[kOwn][per];
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
             hl[t][s] = *(const f16x8 *)&h_lo[16 * t + col][32 * s + 8 * gr];
         }
     }
-    if (kPart != kUp && nb < n1) ask_up(nb);
+    if (!kEarly && nb < n1) ask_up(nb);
     for (; nb < n1; nb += kCols) {
         f32x4 o[kTM][4] = {};
         if constexpr (kTurnUp) {
@@ -354,12 +355,6 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
                 }
             }
         if constexpr (kTurnUp) wave_sync();
-        f16x4 yv[kTM][4];
-#pragma unroll
-        for (int t = 0; t < kTM; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) yv[t][i] = ahead.y[t][i];
-        if (nb + kCols < n1) ask_up(nb + kCols);
         const int n = nb + 4 * col;
 #pragma unroll
         for (int t = 0; t < kTM; ++t)
@@ -369,9 +364,10 @@ __global__ __launch_bounds__(kThreads) void k_lora(LoraArgs g, int piece, int pi
                 if (m >= rows || n >= n1) continue;
                 f16x4 r;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) r[u] = (_Float16)((float)yv[t][i][u] + f[t][i] * o[t][u][i]);
+                for (int u = 0; u < 4; ++u) r[u] = (_Float16)((float)ahead.y[t][i][u] + f[t][i] * o[t][u][i]);
                 *(f16x4 *)(out + (uint32_t)(m * g.ldo + n)) = r;
             }
+        if (nb + kCols < n1) ask_up(nb + kCols);
     }
 }
 
@@ -395,7 +391,7 @@ Shape shape_of(int M, int K, int N, int r, int n_requests)
     Shape s{};
     s.two_rows = r <= 64 && (long long)M >= 32ll * n_requests;      // prompts: 32 rows share what is read of A and B
     s.tiles = M / (s.two_rows ? 32 : 16) + n_requests;
-    s.two_launches = (long long)r * K > 1 << 16;
+    s.two_launches = (long long)r * K >= 1 << 16;
     s.k_piece = piece_of(K, kDeep, s.tiles, 512);
     s.k_pieces = (K + s.k_piece - 1) / s.k_piece;
     return s;
