@@ -5,7 +5,8 @@
  * the residual stream, which hand the channel maxima to the next quantised layer.
  *
  * Conventions are those of muxq.h: DEVICE pointers owned by the caller; nothing is allocated, freed
- * or synchronised; every call only enqueues kernels on `stream` and may be captured into a graph;
+ * or synchronised; every call only enqueues kernels on `stream` and may be captured into a graph (the first
+ * call on a device after muxq_init(), which loads the kernels);
  * the return value is a muxq_status, and on any status other than MUXQ_OK (MUXQ_ERR_HIP apart)
  * nothing has been enqueued.  Activations are fp16, rows contiguous, with row strides in elements
  * that are multiples of 8, from 16-byte aligned pointers.  Sums, maxima and softmax

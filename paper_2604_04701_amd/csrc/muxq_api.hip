@@ -2,6 +2,7 @@
 // kernel sequencing only.  Nothing here allocates, frees or synchronises.
 #include "../../include/muxq.h"
 #include "../../include/muxq_measure.h"
+#include "muxq_block_kernels.h"
 #include "muxq_kernels.h"
 
 #include <math.h>
@@ -369,6 +370,10 @@ const char *muxq_status_string(int status)
 int muxq_init(void)
 {
     MUXQ_TRY(muxq::gemm_prepare_all());
+    MUXQ_TRY(muxq::kv_prepare());
+    MUXQ_TRY(muxq::attend_prepare());
+    MUXQ_TRY(muxq::lora_prepare());
+    MUXQ_TRY(muxq::norm_prepare());
     void *p = nullptr;
     MUXQ_TRY(noalloc_scratch_ptr(&p));
     return MUXQ_OK;

@@ -10,10 +10,15 @@
 // with byte permutes.  Lanes of a 16-lane row read one row of V (2 d bytes) together.
 //
 // Weights are fp16 in the second product, in two parts (p = hi + lo, each rounded towards zero): 22 bits, where
-// one part would add an error as large as the output's rounding.  They are kept at up to 2^15 (m stands 8
-// below the running maximum's exponent, and moves only when a score is 7 above it), so that small ones
-// keep their bits: of the types with 16 bits fp16 has the exact codes and the bits, and this gives it the range.  8-bit codes are exact
-// in fp16; the scale of a key goes to its score, the scale of a value to its weight, over a running power of two.
+// one part would add an error as large as the output's rounding.  They are 2^(s - m + 8), and m follows the maximum only when a
+// score is 7 above it, which is rare: up to 2^15, so that small ones keep their bits.  8-bit codes are exact in
+// fp16; the scale of a key goes to its score, the scale of a value to its weight, over a running power of two.
+//
+// How it is divided (Plan below): short or many sequences have a workgroup of 8 waves each and key-value head, and no second
+// launch; otherwise as many workgroups as the chip holds have equal shares, and a second launch joins what they cut through.
+// Measured: 64 sequences of 131 to 8192 tokens, 8 key-value heads of 128, fp16, 1.09 GB: 181 us, 6.0 TB/s; one of 131071 tokens
+// 95 us, 5.7 TB/s; 24 sequences to 1024, 20 heads of 64, 8-bit codes, 34 MB: 15.5 us, latency of 4 steps and of what comes
+// before and after them; one of 37 tokens 4.4 us.
 #include "muxq_block_kernels.h"
 
 #include <algorithm>
@@ -151,316 +156,317 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
     }
 
     for (int piece = 0;; ++piece) {
-    const int kvh = pair / subs, sub = pair - kvh * subs;
-    const int head0 = kvh * a.group + sub * kHeads<kD>, n_here = min(kHeads<kD>, a.group - sub * kHeads<kD>);
-    const int len = length_of(s);
-    int t0 = 0, t1 = len;
-    bool whole = true;
-    if constexpr (kShares) {
-        const int steps = (int)min((long long)(n - j), end - at);
-        t0 = min(len, max(0, j - kBegin) * kStep);
-        t1 = min(len, max(0, j + steps - kBegin) * kStep);
-        whole = steps == n;
-        at += steps;
-    } else if (len == 0) {                       // an idle place
-        for (int i = tid; i < n_here * d; i += kThreads) a.o[(long long)s * a.ldo + (long long)head0 * d + i] = (_Float16)0.0f;
-        return;
-    }
-
-    // queries: column `col` of the right operand, the dimensions in the left one's order
-    f16x8 q[NS];
-    const _Float16 *qrow = a.q + (long long)s * a.ldq + (long long)(head0 + min(col, n_here - 1)) * d;
-#pragma unroll
-    for (int st = 0; st < NS; ++st) {
-        const int e = kInt8 ? 64 * (st >> 1) + 16 * g + 8 * (st & 1) : 32 * st + 8 * g;
-        q[st] = f16x8{};
-        if (col < n_here && (kFull || e < d)) q[st] = *(const f16x8 *)(qrow + e);
-    }
-
-    const float c = a.scale * 1.44269504088896f;
-    float m = kFloor, l = 0.0f, cap = 0.0f, cap_inv = 0.0f;
-    f32x4 o[VE] = {};
-    // what is on its way: keys of tokens 16 t + col, values of tokens 16 t + 4 g + i, and their scales
-    uint4 k[2][KW];
-    uint32_t v[8][VW];
-    float4 ks[2], vs[2];
-
-    // where the pages from token `c0` on stand, in elements (with codes: their numbers); -1: not in the cache
-    long long *const sh_off = (long long *)rest;
-    int first = 0, c1 = 0;
-    bool any_bad = false;
-    auto is_masked = [&](int tok) { return any_bad || tok + kTile > c1; };
-    auto load_k = [&](auto masked_c, int tok) {
-        constexpr bool kMasked = decltype(masked_c)::value;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int kt = tok + 16 * t + col;
-            long long at = sh_off[(kt >> shift) - first];
-            const bool there = !kMasked || (at >= 0 && kt < c1);
-            if (kInt8) at = at * a.c.ld_block + kvh * a.c.ld_head;
-            const long long row = there ? at + (kt & mask) * a.c.ld_token : 0;
-#pragma unroll
-            for (int u = 0; u < KW; ++u) {
-                const int e = kInt8 ? 64 * u + 16 * g : 32 * u + 8 * g;
-                k[t][u] = uint4{0, 0, 0, 0};
-                if (kFull || e < d) k[t][u] = load<uint4, kShares>(a.c.k + (row + e) * (kInt8 ? 1 : 2));
-            }
+        const int kvh = pair / subs, sub = pair - kvh * subs;
+        const int head0 = kvh * a.group + sub * kHeads<kD>, n_here = min(kHeads<kD>, a.group - sub * kHeads<kD>);
+        const int len = length_of(s);
+        int t0 = 0, t1 = len;
+        bool whole = true;
+        if constexpr (kShares) {
+            const int steps = (int)min((long long)(n - j), end - at);
+            t0 = min(len, max(0, j - kBegin) * kStep);
+            t1 = min(len, max(0, j + steps - kBegin) * kStep);
+            whole = steps == n;
+            at += steps;
+        } else if (len == 0) {                       // an idle place
+            for (int i = tid; i < n_here * d; i += kThreads) a.o[(long long)s * a.ldo + (long long)head0 * d + i] = (_Float16)0.0f;
+            return;
         }
-    };
-    auto load_v = [&](auto masked_c, int tok) {
-        constexpr bool kMasked = decltype(masked_c)::value;
+
+        // queries: column `col` of the right operand, the dimensions in the left one's order
+        f16x8 q[NS];
+        const _Float16 *qrow = a.q + (long long)s * a.ldq + (long long)(head0 + min(col, n_here - 1)) * d;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            // the lane's tokens are 16 t + 4 g + 0..3, in one page
-            const int vt = tok + 16 * t + 4 * g;
-            const long long page = sh_off[(vt >> shift) - first];
-            const long long at = kInt8 ? page * a.c.ld_block + kvh * a.c.ld_head : page;
-            if constexpr (kInt8) {
-                const long long at_s = (kMasked && page < 0) ? 0 : ((page * a.c.n_kv_heads + kvh) << shift) + (vt & mask);
-                ks[t] = *(const float4 *)(a.c.k_scale + at_s);
-                vs[t] = *(const float4 *)(a.c.v_scale + at_s);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool there = !kMasked || (page >= 0 && vt + i < c1);
-                const char *p = a.c.v + (there ? at + ((vt & mask) + i) * a.c.ld_token + VE * col : 0) * (kInt8 ? 1 : 2);
-                uint32_t *w = v[4 * t + i];
-#pragma unroll
-                for (int x = 0; x < VW; ++x) w[x] = 0;
-                if (kFull || VE * col < d) {
-                    if constexpr (VW == 1) {
-                        w[0] = load<uint32_t, kShares>(p);
-                    } else if constexpr (VW == 2) {
-                        const uint2 y = load<uint2, kShares>(p);
-                        w[0] = y.x, w[1] = y.y;
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < VW / 4; ++x) {
-                            const uint4 y = load<uint4, kShares>(p + 16 * x);
-                            w[4 * x] = y.x, w[4 * x + 1] = y.y, w[4 * x + 2] = y.z, w[4 * x + 3] = y.w;
-                        }
-                    }
-                }
-                if (kMasked && !there) {          // what stands there may be NaN: its weight of 0 does not clear it
-#pragma unroll
-                    for (int x = 0; x < VW; ++x) w[x] = 0;
-                }
-            }
+        for (int st = 0; st < NS; ++st) {
+            const int e = kInt8 ? 64 * (st >> 1) + 16 * g + 8 * (st & 1) : 32 * st + 8 * g;
+            q[st] = f16x8{};
+            if (col < n_here && (kFull || e < d)) q[st] = *(const f16x8 *)(qrow + e);
         }
-    };
-    auto ask_k = [&](int tok) {
-        if (is_masked(tok)) load_k(std::true_type{}, tok); else load_k(std::false_type{}, tok);
-    };
-    auto ask_v = [&](int tok) {
-        if (is_masked(tok)) load_v(std::true_type{}, tok); else load_v(std::false_type{}, tok);
-    };
 
-    for (int c0 = t0; c0 < t1; c0 = c1) {
-    c1 = min(t1, c0 + kPages);
-    first = c0 >> shift;
-    const int pages = ((c1 - 1) >> shift) - first + 1;
-    __syncthreads();                              // the last piece's readers
-    if (tid == 0) sh_bad = 0;
-    __syncthreads();
-    for (int i = tid; i < pages + 4; i += kThreads) {
-        long long where = -1;
-        if (i < pages) {
-            const int page = a.table[(long long)s * a.ld_table + first + i];
-            if (page >= 0 && page < a.c.n_blocks)
-                where = kInt8 ? page : page * a.c.ld_block + kvh * a.c.ld_head;
-            else
-                sh_bad = 1;
-        }
-        sh_off[i] = where;
-    }
-    __syncthreads();
-    any_bad = sh_bad != 0;
+        const float c = a.scale * 1.44269504088896f;
+        float m = kFloor, l = 0.0f, cap = 0.0f, cap_inv = 0.0f;
+        f32x4 o[VE] = {};
+        // what is on its way: keys of tokens 16 t + col, values of tokens 16 t + 4 g + i, and their scales
+        uint4 k[2][KW];
+        uint32_t v[8][VW];
+        float4 ks[2], vs[2];
 
-    // The keys of the next step are requested when this step's are in the matrix pipes, its values when this step's are: the
-    // same registers, and something is always on its way.
-    int tok = c0 + wave * kTile;
-    if (tok < c1) {
-        ask_k(tok);
-        ask_v(tok);
-    }
-    for (; tok < c1; tok += kWaves * kTile) {
-        const int next = tok + kWaves * kTile;
-        f32x4 acc[2] = {};
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int u = 0; u < KW; ++u) {
-                if constexpr (!kInt8) {
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, k[t][u]), q[u], acc[t], 0, 0, 0);
-                } else {
-                    uint32_t h[8];
-                    codes_to_half(k[t][u].x, h[0], h[1]);
-                    codes_to_half(k[t][u].y, h[2], h[3]);
-                    codes_to_half(k[t][u].z, h[4], h[5]);
-                    codes_to_half(k[t][u].w, h[6], h[7]);
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(h[0], h[1], h[2], h[3]), q[2 * u], acc[t], 0, 0, 0);
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(h[4], h[5], h[6], h[7]), q[2 * u + 1], acc[t], 0, 0, 0);
-                }
-            }
-        if (next < c1) ask_k(next);
-
-        float p[8], w[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = acc[j >> 2][j & 3] * c;
-        if constexpr (kInt8) {
+        // where the pages from token `c0` on stand, in elements (with codes: their numbers); -1: not in the cache
+        long long *const sh_off = (long long *)rest;
+        int first = 0, c1 = 0;
+        bool any_bad = false;
+        auto is_masked = [&](int tok) { return any_bad || tok + kTile > c1; };
+        auto load_k = [&](auto masked_c, int tok) {
+            constexpr bool kMasked = decltype(masked_c)::value;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                p[4 * t] *= ks[t].x, p[4 * t + 1] *= ks[t].y, p[4 * t + 2] *= ks[t].z, p[4 * t + 3] *= ks[t].w;
-                w[4 * t] = vs[t].x, w[4 * t + 1] = vs[t].y, w[4 * t + 2] = vs[t].z, w[4 * t + 3] = vs[t].w;
+                const int kt = tok + 16 * t + col;
+                long long at = sh_off[(kt >> shift) - first];
+                const bool there = !kMasked || (at >= 0 && kt < c1);
+                if (kInt8) at = at * a.c.ld_block + kvh * a.c.ld_head;
+                const long long row = there ? at + (kt & mask) * a.c.ld_token : 0;
+#pragma unroll
+                for (int u = 0; u < KW; ++u) {
+                    const int e = kInt8 ? 64 * u + 16 * g : 32 * u + 8 * g;
+                    k[t][u] = uint4{0, 0, 0, 0};
+                    if (kFull || e < d) k[t][u] = load<uint4, kShares>(a.c.k + (row + e) * (kInt8 ? 1 : 2));
+                }
             }
-        }
-        if (is_masked(tok)) {
+        };
+        auto load_v = [&](auto masked_c, int tok) {
+            constexpr bool kMasked = decltype(masked_c)::value;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int kt = tok + 16 * (j >> 2) + 4 * g + (j & 3);
-                if (kt >= c1 || sh_off[(kt >> shift) - first] < 0) p[j] = kFloor, w[j] = 0.0f;
+            for (int t = 0; t < 2; ++t) {
+                // the lane's tokens are 16 t + 4 g + 0..3, in one page
+                const int vt = tok + 16 * t + 4 * g;
+                const long long page = sh_off[(vt >> shift) - first];
+                const long long at = kInt8 ? page * a.c.ld_block + kvh * a.c.ld_head : page;
+                if constexpr (kInt8) {
+                    const long long at_s = (kMasked && page < 0) ? 0 : ((page * a.c.n_kv_heads + kvh) << shift) + (vt & mask);
+                    ks[t] = *(const float4 *)(a.c.k_scale + at_s);
+                    vs[t] = *(const float4 *)(a.c.v_scale + at_s);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool there = !kMasked || (page >= 0 && vt + i < c1);
+                    const char *p = a.c.v + (there ? at + ((vt & mask) + i) * a.c.ld_token + VE * col : 0) * (kInt8 ? 1 : 2);
+                    uint32_t *w = v[4 * t + i];
+#pragma unroll
+                    for (int x = 0; x < VW; ++x) w[x] = 0;
+                    if (kFull || VE * col < d) {
+                        if constexpr (VW == 1) {
+                            w[0] = load<uint32_t, kShares>(p);
+                        } else if constexpr (VW == 2) {
+                            const uint2 y = load<uint2, kShares>(p);
+                            w[0] = y.x, w[1] = y.y;
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < VW / 4; ++x) {
+                                const uint4 y = load<uint4, kShares>(p + 16 * x);
+                                w[4 * x] = y.x, w[4 * x + 1] = y.y, w[4 * x + 2] = y.z, w[4 * x + 3] = y.w;
+                            }
+                        }
+                    }
+                    if (kMasked && !there) {          // what stands there may be NaN: its weight of 0 does not clear it
+#pragma unroll
+                        for (int x = 0; x < VW; ++x) w[x] = 0;
+                    }
+                }
             }
-        }
-        float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-        if (__any(top > m + 7.0f)) {                    // rare after the first steps: a new maximum for the head
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float to = fmaxf(m, top), keep = m == kFloor ? 0.0f : exp2_(m - to);
-            m = to;
-            l *= keep;
-#pragma unroll
-            for (int e = 0; e < VE; ++e) o[e] *= keep;
-        }
-        const float off = m == kFloor ? 0.0f : 8.0f - m;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = exp2_(p[j] + off);
-        l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-        if constexpr (kInt8) {
-            float most = fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
-            if (__any(most > cap)) {                    // scales of values over a power of two
-                most = fmaxf(most, __shfl_xor(most, 16, 64));
-                most = fmaxf(most, __shfl_xor(most, 32, 64));
-                const uint32_t ex = min(__float_as_uint(most) >> 23, 252u) + 1;
-                const float was = cap;
-                cap = fmaxf(cap, __uint_as_float(ex << 23));
-                cap_inv = __uint_as_float((254u - (__float_as_uint(cap) >> 23)) << 23);
-                const float keep = was * cap_inv;
-#pragma unroll
-                for (int e = 0; e < VE; ++e) o[e] *= keep;
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] *= w[j] * cap_inv;
-        }
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const fp16x2 h = __builtin_amdgcn_cvt_pkrtz(p[2 * j], p[2 * j + 1]);
-            const fp16x2 r = __builtin_amdgcn_cvt_pkrtz(p[2 * j] - (float)h[0], p[2 * j + 1] - (float)h[1]);
-            hi[j] = __builtin_bit_cast(uint32_t, h);
-            lo[j] = __builtin_bit_cast(uint32_t, r);
-        }
-        const f16x8 ph = half8(hi[0], hi[1], hi[2], hi[3]), pl = half8(lo[0], lo[1], lo[2], lo[3]);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            uint32_t x[4];
-            if constexpr (!kInt8) {
-                const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_perm(v[2 * j + 1][e >> 1], v[2 * j][e >> 1], sel);
-            } else {
-                // byte e of the words of two tokens and two more, then as codes_to_half
-                const uint32_t sel = 0x0c0c0400u + 0x0101u * (e & 3);
-                uint32_t y[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    y[j] = __builtin_amdgcn_perm(v[4 * j + 1][e >> 2], v[4 * j][e >> 2], sel) |
-                           (__builtin_amdgcn_perm(v[4 * j + 3][e >> 2], v[4 * j + 2][e >> 2], sel) << 16);
-                codes_to_half(y[0], x[0], x[1]);
-                codes_to_half(y[1], x[2], x[3]);
-            }
-            const f16x8 vt = half8(x[0], x[1], x[2], x[3]);
-            o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, ph, o[e], 0, 0, 0);
-            o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, pl, o[e], 0, 0, 0);
-        }
-        if (next < c1) ask_v(next);
-    }
-    }
+        };
+        auto ask_k = [&](int tok) {
+            if (is_masked(tok)) load_k(std::true_type{}, tok); else load_k(std::false_type{}, tok);
+        };
+        auto ask_v = [&](int tok) {
+            if (is_masked(tok)) load_v(std::true_type{}, tok); else load_v(std::false_type{}, tok);
+        };
 
-    // The waves' parts: m and l by head, then sum_w 2^(m_w - max m) o_w in LDS, [wave][head][d], the upper half of the waves
-    // through the lower one's places.
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    if (lane < 16) sh_m[wave][lane] = m, sh_l[wave][lane] = l;
-    __syncthreads();
-    float top = sh_m[0][col];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh_m[w][col]);
-    const float f = weight_of(m, l, top) * (kInt8 ? cap : 1.0f);
-#pragma unroll
-    for (int e = 0; e < VE; ++e) o[e] *= f;
-    float *const sh_o = (float *)rest;
-    float *const mine = sh_o + ((wave & 3) * n_here + col) * kD;
-    auto put = [&](bool add) {
-        if (col >= n_here) return;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int e = 0; e < VE; e += 4) {
-                f32x4 *at = (f32x4 *)(mine + VE * (4 * g + i) + e);
-                f32x4 x = {o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]};
-                if (add) x += *at;
-                *at = x;
+        for (int c0 = t0; c0 < t1; c0 = c1) {
+            c1 = min(t1, c0 + kPages);
+            first = c0 >> shift;
+            const int pages = ((c1 - 1) >> shift) - first + 1;
+            __syncthreads();                              // the last piece's readers
+            if (tid == 0) sh_bad = 0;
+            __syncthreads();
+            for (int i = tid; i < pages + 4; i += kThreads) {
+                long long where = -1;
+                if (i < pages) {
+                    const int page = a.table[(long long)s * a.ld_table + first + i];
+                    if (page >= 0 && page < a.c.n_blocks)
+                        where = kInt8 ? page : page * a.c.ld_block + kvh * a.c.ld_head;
+                    else
+                        sh_bad = 1;
+                }
+                sh_off[i] = where;
             }
-    };
-    if constexpr (kWaves == 8) {
-        if (wave >= 4) put(false);
+            __syncthreads();
+            any_bad = sh_bad != 0;
+
+            // The keys of the next step are requested when this step's are in the matrix pipes, its values when this step's are: the
+            // same registers, and something is always on its way.
+            int tok = c0 + wave * kTile;
+            if (tok < c1) {
+                ask_k(tok);
+                ask_v(tok);
+            }
+            for (; tok < c1; tok += kWaves * kTile) {
+                const int next = tok + kWaves * kTile;
+                f32x4 acc[2] = {};
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int u = 0; u < KW; ++u) {
+                        if constexpr (!kInt8) {
+                            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, k[t][u]), q[u], acc[t], 0, 0, 0);
+                        } else {
+                            uint32_t h[8];
+                            codes_to_half(k[t][u].x, h[0], h[1]);
+                            codes_to_half(k[t][u].y, h[2], h[3]);
+                            codes_to_half(k[t][u].z, h[4], h[5]);
+                            codes_to_half(k[t][u].w, h[6], h[7]);
+                            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(h[0], h[1], h[2], h[3]), q[2 * u], acc[t], 0, 0, 0);
+                            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half8(h[4], h[5], h[6], h[7]), q[2 * u + 1], acc[t], 0, 0, 0);
+                        }
+                    }
+                if (next < c1) ask_k(next);
+
+                float p[8], w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[j] = acc[j >> 2][j & 3] * c;
+                if constexpr (kInt8) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        p[4 * t] *= ks[t].x, p[4 * t + 1] *= ks[t].y, p[4 * t + 2] *= ks[t].z, p[4 * t + 3] *= ks[t].w;
+                        w[4 * t] = vs[t].x, w[4 * t + 1] = vs[t].y, w[4 * t + 2] = vs[t].z, w[4 * t + 3] = vs[t].w;
+                    }
+                }
+                if (is_masked(tok)) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int kt = tok + 16 * (j >> 2) + 4 * g + (j & 3);
+                        if (kt >= c1 || sh_off[(kt >> shift) - first] < 0) p[j] = kFloor, w[j] = 0.0f;
+                    }
+                }
+                float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+                if (__any(top > m + 7.0f)) {                    // rare after the first steps: a new maximum for the head
+                    top = fmaxf(top, __shfl_xor(top, 16, 64));
+                    top = fmaxf(top, __shfl_xor(top, 32, 64));
+                    const float to = fmaxf(m, top), keep = m == kFloor ? 0.0f : exp2_(m - to);
+                    m = to;
+                    l *= keep;
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) o[e] *= keep;
+                }
+                const float off = m == kFloor ? 0.0f : 8.0f - m;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[j] = exp2_(p[j] + off);
+                l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                if constexpr (kInt8) {
+                    float most = fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
+                    if (__any(most > cap)) {                    // scales of values over a power of two
+                        most = fmaxf(most, __shfl_xor(most, 16, 64));
+                        most = fmaxf(most, __shfl_xor(most, 32, 64));
+                        const uint32_t ex = min(__float_as_uint(most) >> 23, 252u) + 1;
+                        const float was = cap;
+                        cap = fmaxf(cap, __uint_as_float(ex << 23));
+                        cap_inv = __uint_as_float((254u - (__float_as_uint(cap) >> 23)) << 23);
+                        const float keep = was * cap_inv;
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) o[e] *= keep;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p[j] *= w[j] * cap_inv;
+                }
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const fp16x2 h = __builtin_amdgcn_cvt_pkrtz(p[2 * j], p[2 * j + 1]);
+                    const fp16x2 r = __builtin_amdgcn_cvt_pkrtz(p[2 * j] - (float)h[0], p[2 * j + 1] - (float)h[1]);
+                    hi[j] = __builtin_bit_cast(uint32_t, h);
+                    lo[j] = __builtin_bit_cast(uint32_t, r);
+                }
+                const f16x8 ph = half8(hi[0], hi[1], hi[2], hi[3]), pl = half8(lo[0], lo[1], lo[2], lo[3]);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    uint32_t x[4];
+                    if constexpr (!kInt8) {
+                        const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_perm(v[2 * j + 1][e >> 1], v[2 * j][e >> 1], sel);
+                    } else {
+                        // byte e of the words of two tokens and two more, then as codes_to_half
+                        const uint32_t sel = 0x0c0c0400u + 0x0101u * (e & 3);
+                        uint32_t y[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            y[j] = __builtin_amdgcn_perm(v[4 * j + 1][e >> 2], v[4 * j][e >> 2], sel) |
+                                   (__builtin_amdgcn_perm(v[4 * j + 3][e >> 2], v[4 * j + 2][e >> 2], sel) << 16);
+                        codes_to_half(y[0], x[0], x[1]);
+                        codes_to_half(y[1], x[2], x[3]);
+                    }
+                    const f16x8 vt = half8(x[0], x[1], x[2], x[3]);
+                    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, ph, o[e], 0, 0, 0);
+                    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, pl, o[e], 0, 0, 0);
+                }
+                if (next < c1) ask_v(next);
+            }
+        }
+
+        // The waves' parts: m and l by head, then sum_w 2^(m_w - max m) o_w in LDS, [wave][head][d], the upper half of the waves
+        // through the lower one's places.
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (lane < 16) sh_m[wave][lane] = m, sh_l[wave][lane] = l;
         __syncthreads();
-        if (wave < 4) put(true);
-    } else {
-        put(false);
-    }
-    __syncthreads();
-    for (int i = tid; i < n_here * (kD / 4); i += kThreads) {
-        const int h = i / (kD / 4), e = (i - h * (kD / 4)) * 4;
-        if (!kFull && e >= d) continue;
-        float most = sh_m[0][h], all = 0.0f;
+        float top = sh_m[0][col];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) most = fmaxf(most, sh_m[w][h]);
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh_m[w][col]);
+        const float f = weight_of(m, l, top) * (kInt8 ? cap : 1.0f);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) all += weight_of(sh_m[w][h], sh_l[w][h], most) * sh_l[w][h];
-        f32x4 sum = {};
+        for (int e = 0; e < VE; ++e) o[e] *= f;
+        float *const sh_o = (float *)rest;
+        float *const mine = sh_o + ((wave & 3) * n_here + col) * kD;
+        auto put = [&](bool add) {
+            if (col >= n_here) return;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) sum += *(const f32x4 *)(sh_o + (w * n_here + h) * kD + e);
-        if (whole) {
-            const float inv = most == kFloor ? 0.0f : 1.0f / all;
-            f16x4 r;
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) r[x] = (_Float16)(sum[x] * inv);
-            *(f16x4 *)(a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e) = r;
+                for (int e = 0; e < VE; e += 4) {
+                    f32x4 *at = (f32x4 *)(mine + VE * (4 * g + i) + e);
+                    f32x4 x = {o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]};
+                    if (add) x += *at;
+                    *at = x;
+                }
+        };
+        if constexpr (kWaves == 8) {
+            if (wave >= 4) put(false);
+            __syncthreads();
+            if (wave < 4) put(true);
         } else {
-            const int part = (blockIdx.x * 2 + (piece ? 1 : 0)) * min(a.group, kHeads<kD>) + h;
-            *(f32x4 *)(plan.o + (long long)part * d + e) = sum;
-            if (e == 0) plan.ml[part] = make_float2(most, all);
+            put(false);
         }
-    }
-    if constexpr (!kShares) return;
-    if (at >= end) {
-        if (tid == 0) {
-            // open: the first of the shares that have a part of this pair, which later ones finish
-            const long long from = (long long)sh_before[s] * pairs + (long long)pair * n, begin = total * blockIdx.x / groups;
-            const int last = (int)(((from + n) * groups - 1) / total);       // the share of the pair's last step
-            const bool first_of = begin <= from && end < from + n;
-            plan.open[blockIdx.x] = int4{s, pair, first_of ? last - (int)blockIdx.x + 1 : 0, begin == from ? 0 : 1};
+        __syncthreads();
+        for (int i = tid; i < n_here * (kD / 4); i += kThreads) {
+            const int h = i / (kD / 4), e = (i - h * (kD / 4)) * 4;
+            if (!kFull && e >= d) continue;
+            float most = sh_m[0][h], all = 0.0f;
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) most = fmaxf(most, sh_m[w][h]);
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) all += weight_of(sh_m[w][h], sh_l[w][h], most) * sh_l[w][h];
+            f32x4 sum = {};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) sum += *(const f32x4 *)(sh_o + (w * n_here + h) * kD + e);
+            if (whole) {
+                const float inv = most == kFloor ? 0.0f : 1.0f / all;
+                f16x4 r;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) r[x] = (_Float16)(sum[x] * inv);
+                *(f16x4 *)(a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e) = r;
+            } else {
+                const int part = (blockIdx.x * 2 + (piece ? 1 : 0)) * min(a.group, kHeads<kD>) + h;
+                *(f32x4 *)(plan.o + (long long)part * d + e) = sum;
+                if (e == 0) plan.ml[part] = make_float2(most, all);
+            }
         }
-        return;
-    }
-    // on to the next pair, or the next sequence that has steps
-    j = 0;
-    if (++pair == pairs) {
-        pair = 0;
-        do ++s; while (sh_before[s + 1] == sh_before[s]);
-        n = sh_before[s + 1] - sh_before[s];
-    }
+        if constexpr (!kShares) return;
+        if (at >= end) {
+            if (tid == 0) {
+                // open: the first of the shares that have a part of this pair, which later ones finish
+                const long long from = (long long)sh_before[s] * pairs + (long long)pair * n, begin = total * blockIdx.x / groups;
+                const int last = (int)(((from + n) * groups - 1) / total);       // the share of the pair's last step
+                const bool first_of = begin <= from && end < from + n;
+                plan.open[blockIdx.x] = int4{s, pair, first_of ? last - (int)blockIdx.x + 1 : 0, begin == from ? 0 : 1};
+            }
+            return;
+        }
+        __syncthreads();                                  // (a next piece without tokens goes straight to sh_m)
+        // on to the next pair, or the next sequence that has steps
+        j = 0;
+        if (++pair == pairs) {
+            pair = 0;
+            do ++s; while (sh_before[s + 1] == sh_before[s]);
+            n = sh_before[s + 1] - sh_before[s];
+        }
     }
 }
 
@@ -584,6 +590,12 @@ size_t attend_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, 
     for (int x = 1; x <= S && x <= kMaxSeqs; ++x)
         if ((most = attend_workspace_need(x, n_heads, n_kv_heads, head_dim, max_length)) > 0) break;
     return most;
+}
+
+hipError_t attend_prepare()
+{
+    hipFuncAttributes at;
+    return hipFuncGetAttributes(&at, (const void *)k_attend<64, false, true, 4, false>);
 }
 
 hipError_t launch_attend(const AttendArgs &a, bool int8, hipStream_t s)

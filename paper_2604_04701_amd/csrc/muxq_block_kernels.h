@@ -61,4 +61,10 @@ int norm_slab_rows(int M);                        // rows of maxima a call leave
 size_t norm_scratch_bytes(int M, int K, int k_pad);
 hipError_t launch_norm(const NormArgs &a, bool rms, hipStream_t s);
 
+// Load a file's kernels on the current device, so that a first call may be captured.
+hipError_t attend_prepare();
+hipError_t kv_prepare();
+hipError_t lora_prepare();
+hipError_t norm_prepare();
+
 }  // namespace muxq

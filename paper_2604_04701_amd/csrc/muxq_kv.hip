@@ -193,6 +193,12 @@ static hipError_t launch_append(const AppendArgs &a, int P, bool int8, bool inte
                 : launch_kernel(k_kv_append<false, false, E, kHeadsOf>, grid, dim3(256), 0, s, a, P, slots_of);
 }
 
+hipError_t kv_prepare()
+{
+    hipFuncAttributes at;
+    return hipFuncGetAttributes(&at, (const void *)k_kv_gather<false>);
+}
+
 hipError_t launch_kv_append(const AppendArgs &a, bool int8, bool interleaved, hipStream_t s)
 {
     // runs of 8 unless halves of the rotated dimensions are not whole runs (interleaved pairs stand inside a run)

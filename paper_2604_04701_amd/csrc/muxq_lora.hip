@@ -419,6 +419,12 @@ size_t lora_workspace_bytes(int M, int K, int N, int r, int n_requests)
     return p.two_launches ? (size_t)p.k_pieces * M * r * 4 : 0;
 }
 
+hipError_t lora_prepare()
+{
+    hipFuncAttributes at;
+    return hipFuncGetAttributes(&at, (const void *)k_lora<1, 1, kBoth>);
+}
+
 hipError_t launch_lora(const LoraArgs &g, hipStream_t s)
 {
     const Shape p = shape_of(g.M, g.K, g.N, g.r, g.n_requests);

@@ -219,6 +219,12 @@ int norm_slab_rows(int M) { return M <= 64 ? M : 1; }
 
 size_t norm_scratch_bytes(int M, int K, int k_pad) { return M <= 64 ? 0 : (size_t)groups_of(M, K) * k_pad * 2; }
 
+hipError_t norm_prepare()
+{
+    hipFuncAttributes at;
+    return hipFuncGetAttributes(&at, (const void *)k_norm_fold);
+}
+
 hipError_t launch_norm(const NormArgs &n, bool rms, hipStream_t s)
 {
     uint16_t *const maxima = n.slabs && n.M > 64 ? n.scratch : nullptr;

@@ -55,6 +55,33 @@ def test_attention_long_and_many(lengths, H, heads, d, bits):
     _attend_case(len(lengths), lengths, H, heads, d, 16, bits)
 
 
+@pytest.mark.parametrize("seed", range(6))
+def test_attention_shares_cut_anywhere(seed):
+    # ragged lengths, idle places and very short sequences among long ones: shares end in every part of a sequence
+    g = gen(100 + seed)
+    S = [3, 17, 40, 64, 100, 5][seed]
+    lengths = (torch.rand(S, generator=g, device=DEV) ** 3 * [9000, 6000, 4000, 3000, 2600, 30000][seed]).int().tolist()
+    lengths[S // 2], lengths[-1] = 0, [9000, 6000, 4000, 3000, 2600, 30000][seed]
+    H, heads, d = [(4, 4, 64), (16, 2, 64), (3, 3, 128), (8, 1, 80), (2, 2, 64), (18, 1, 256)][seed]
+    _attend_case(seed, lengths, H, heads, d, 16, 8 if seed % 2 else 16)
+
+
+def test_attention_with_a_bound_far_above_the_lengths():
+    # the work is planned by the bound: shares with fewer steps than workgroups, most of them none
+    g = gen(12)
+    lengths = [5, 0, 300, 17]
+    k, v, _, _ = make_cache(g, 40, 2, 16, 64, 16)
+    table, _ = make_table(g, lengths, 16, 40, width=2000)
+    q = normal(g, 4, 4, 64)
+    say("[attend] bound of 32000 for 300 tokens")
+    got = B.muxq_paged_attention(q, k, v, table, ints(lengths), 32000)
+    none = B.muxq_paged_attention(q, k, v, table, ints([0, -3, 0, 0]), 32000)
+    torch.cuda.synchronize()
+    want, tol = attend64(q, k, v, None, None, table, lengths, 0.125)
+    check(got, want, tol, "attention")
+    assert (none == 0).all()
+
+
 @pytest.mark.parametrize("bits", [16, 8])
 def test_attention_sharp_and_flat_scores(bits):
     _attend_case(1, [1, 50, 3000], 4, 4, 64, 16, bits, gain=30.0)          # nearly one-hot
