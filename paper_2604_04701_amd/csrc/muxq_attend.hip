@@ -570,7 +570,7 @@ template <int kD>
 hipError_t launch_d(const AttendArgs &a, const Plan &plan, bool int8, hipStream_t s)
 {
     if (plan.groups) return launch_w<kD, 4, true>(a, plan, int8, s);
-    // 8 waves where each has tokens
+    // 8 waves where each has tokens (4 sequences of 12 heads to 1024 tokens: 10.8 us, 13.0 with 4)
     return a.max_length > 128 ? launch_w<kD, 8, false>(a, plan, int8, s) : launch_w<kD, 4, false>(a, plan, int8, s);
 }
 

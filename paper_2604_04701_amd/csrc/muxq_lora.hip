@@ -8,6 +8,8 @@
 // H is what several strips of a tile compute again: it costs reads of X and A from the L2s, and saves a second
 // launch and the way of H through memory.  Where it would cost more than that, two launches: the first
 // divides K over workgroups too and leaves its parts of H in the workspace, binary32, the second adds them.
+// One token 768 -> 2304 at rank 8 4.6 us, 64 requests 1280 -> 3840 at rank 16 9.2 us, 8192 rows 4096 -> 4096 at rank 32 57 us (22 + 35
+// in two launches, 3.5 TB/s of what has to move).
 // H is binary32; the second product takes it as two fp16 parts (22 bits) of the row over a power of two,
 // whatever its size.
 #include "muxq_block_kernels.h"
@@ -42,7 +44,7 @@ __global__ __launch_bounds__(kThreads, kRT == 1 || (kRT == 2 && (kTM == 1 || kPa
 {
     constexpr int T = 16 * kTM, R = 16 * kRT, RS = kRT == 1 ? 1 : kRT / 2, LD = R + 4, LH = 32 * RS + 8;
     // The operands want 16 rows on neighbouring lanes, which memory gives 16 bytes at a time: with many rows each wave
-    // loads whole runs of rows and turns them in a place of its own in LDS (a fifth of the requests of the loads).
+    // loads whole runs of rows and turns them in a place of its own in LDS (8192 x 4096 at rank 32: half of the requests).
     constexpr bool kTurnDown = kPart != kUp && kTM == 2, kTurnUp = kPart != kDown && kTM == 2 && RS == 1;
     constexpr int kLdDown = 64 + 8, kDownBytes = kTurnDown ? kWaves * 32 * kLdDown * 2 : 0;
     constexpr int kLdUp = 32 + 8, kUpBlock = 16 * kLdUp + 32, kUpBytes = kTurnUp ? kWaves * 4 * kUpBlock * 2 : 0;
@@ -389,8 +391,13 @@ struct Shape {
 Shape shape_of(int M, int K, int N, int r, int n_requests)
 {
     Shape s{};
-    s.two_rows = r <= 64 && (long long)M >= 32ll * n_requests;      // prompts: 32 rows share what is read of A and B
+    // Prompts: 32 rows share what is read of A and B (8192 x 4096 -> 4096 at rank 32 70.6 us, 83.6 with 16 rows; short K the other
+    // way, 2000 x 1280 -> 3840 at rank 16 22.6 and 17.9).
+    s.two_rows = r <= 64 && (long long)M >= 32ll * n_requests;
     s.tiles = M / (s.two_rows ? 32 : 16) + n_requests;
+    // Two launches where A is more than a workgroup should read by itself.  us, one and two: a token at K = 4096 and rank 64
+    // 20.4 / 9.9, 16 tokens at 4096 and 16 9.1 / 7.6, 40 requests in 512 rows at 4096 and 32 28.3 / 15.1; 64 tokens at 1280 and 16
+    // 8.9 / 9.9, a token at 768 and 8 4.6 / 6.6, 8192 at 1280 and 16 14.7 / 20.5.
     s.two_launches = (long long)r * K >= 1 << 16;
     s.k_piece = piece_of(K, kDeep, s.tiles, 512);
     s.k_pieces = (K + s.k_piece - 1) / s.k_piece;
@@ -407,7 +414,7 @@ hipError_t launch(const LoraArgs &g, const Shape &p, hipStream_t s)
     }
     const hipError_t e = launch_kernel(k_lora<kTM, kRT, kDown>, dim3(p.tiles, p.k_pieces), block, 0, s, g, p.k_piece, p.k_pieces);
     if (e != hipSuccess) return e;
-    const int strip = piece_of(g.N, kCols, p.tiles, 1024);
+    const int strip = piece_of(g.N, kCols, p.tiles, 1024);        // (512: 60.9 us for 58.0 at rank 32, 256: 66.6)
     return launch_kernel(k_lora<kTM, kRT, kUp>, dim3(p.tiles, (g.N + strip - 1) / strip), block, 0, s, g, strip, p.k_pieces);
 }
 

@@ -2,12 +2,12 @@
 //
 // Each element is read once and written once: X and R in, the stream and Y out, 8 bytes a channel and token.  A
 // row stays in the registers of its W waves in binary32 from the first load to the last store, both means of
-// both norms taken from there (the mean first, then the squares of what is left: no cancellation).  Prompts:
-// a wave a row.  Few rows: four waves
-// a row, and 16 beyond 8192 channels, so that a lane has few elements and its loads go out together.
+// both norms taken from there (the mean first, then the squares of what is left: no cancellation).  Prompts
+// have a wave a row; few rows, or long ones, four waves each, 16 beyond 8192 channels, so that a lane has few
+// elements and its loads go out together.
 // Column maxima: every wave keeps those of the rows it writes; a workgroup's go to the scratch and a second launch folds
-// them (half of what the abs-max pass over Y would read is not even written).  Up to 64 rows their magnitudes are
-// the maxima, and there is one launch.
+// them.  Up to 64 rows their magnitudes are the maxima, and there is one launch.
+// Measured: 24 x 1280 3.1 us, 16384 x 1280 with both norms, a gate and the maxima 41 us, of which the rows take 36 (4.6 TB/s).
 #include "muxq_block_kernels.h"
 
 namespace muxq {
@@ -196,8 +196,9 @@ __global__ __launch_bounds__(256) void k_norm_fold(const uint16_t *maxima, int r
     }
 }
 
-// Waves to a row.
-int waves_of(int M, int K) { return K > 8192 ? 16 : K > 2048 || M < 2048 ? 4 : 1; }
+// Waves to a row.  us, one and four: 24 x 1280 3.7 / 2.8, 64 x 768 3.2 / 2.8, 256 x 1280 6.3 / 6.5, 1024 x 768 6.5 / 9.4,
+// 16384 x 1280 41.9 / 71.3, 4096 x 2048 (32 channels a lane) 19.9 / 18.0.
+int waves_of(int M, int K) { return K > 8192 ? 16 : K > 1536 || M <= 64 ? 4 : 1; }
 
 int groups_of(int M, int K)
 {
@@ -231,7 +232,7 @@ hipError_t launch_norm(const NormArgs &n, bool rms, hipStream_t s)
     const int W = waves_of(n.M, n.K), C = (n.k_pad + 512 * W - 1) / (512 * W);
     hipError_t e;
     if (W == 1)
-        e = C == 1 ? launch<1, 1>(n, rms, maxima, s) : C == 2 ? launch<1, 2>(n, rms, maxima, s) : C == 3 ? launch<1, 3>(n, rms, maxima, s) : launch<1, 4>(n, rms, maxima, s);
+        e = C == 1 ? launch<1, 1>(n, rms, maxima, s) : C == 2 ? launch<1, 2>(n, rms, maxima, s) : launch<1, 3>(n, rms, maxima, s);
     else if (W == 4)
         e = C == 1 ? launch<4, 1>(n, rms, maxima, s) : C == 2 ? launch<4, 2>(n, rms, maxima, s) : C == 3 ? launch<4, 3>(n, rms, maxima, s) : launch<4, 4>(n, rms, maxima, s);
     else
