@@ -105,7 +105,7 @@ def test_attention_workspace():
 @pytest.mark.parametrize("kw,status", [
     (dict(x=None), 1), (dict(a=None), 1), (dict(b=None), 1), (dict(scales=None), 1), (dict(starts=None), 1), (dict(adapters=None), 1),
     (dict(y=None), 1), (dict(out=None), 1), (dict(M=0), 2), (dict(K=252), 2), (dict(K=0), 2), (dict(N=500), 2), (dict(r=0), 2), (dict(r=12), 2),
-    (dict(r=136), 2), (dict(n=0), 2), (dict(requests=0), 2), (dict(ldx=248), 2), (dict(ldx=260), 2), (dict(ldy=504), 2), (dict(ldo=510), 2),
+    (dict(r=136), 2), (dict(n=0), 2), (dict(requests=0), 2), (dict(ldx=248), 2), (dict(ldx=260), 2), (dict(ldy=504), 2), (dict(ldo=510), 2), (dict(ldx=(1 << 25) + 8), 2), (dict(ldo=1 << 26), 2),
     (dict(x=FAKE + 8), 3), (dict(a=FAKE + 2), 3), (dict(out=AWAY + 4), 3), (dict(starts=FAKE + 2), 3), (dict(out=FAKE + 512), 4),
     (dict(x=AWAY), 4), (dict(y=AWAY + 16), 4)])
 def test_lora_refuses(kw, status):
