@@ -391,9 +391,10 @@ struct Shape {
 Shape shape_of(int M, int K, int N, int r, int n_requests)
 {
     Shape s{};
-    // Prompts: 32 rows share what is read of A and B (8192 x 4096 -> 4096 at rank 32 70.6 us, 83.6 with 16 rows; short K the other
-    // way, 2000 x 1280 -> 3840 at rank 16 22.6 and 17.9).
-    s.two_rows = r <= 64 && (long long)M >= 32ll * n_requests;
+    // Prompts: 32 rows share what is read of A and B.  us, 32 rows and 16: 8192 x 4096 -> 4096 at rank 32 57.6 / 79.0, 8192 x 1280 ->
+    // 1280 at 16 14.8 / 17.1, 500 x 5000 -> 5000 at 16 13.1 / 13.6; with little to share 16 are more workgroups, 600 x 2000 -> 600 at
+    // 16 8.4 / 7.5, 300 x 1000 -> 1000 6.9 / 5.5.
+    s.two_rows = r <= 64 && (long long)M >= 32ll * n_requests && (long long)M * K >= 3 << 19;
     s.tiles = M / (s.two_rows ? 32 : 16) + n_requests;
     // Two launches where A is more than a workgroup should read by itself.  us, one and two: a token at K = 4096 and rank 64
     // 20.4 / 9.9, 16 tokens at 4096 and 16 9.1 / 7.6, 40 requests in 512 rows at 4096 and 32 28.3 / 15.1; 64 tokens at 1280 and 16

@@ -611,3 +611,11 @@ def test_bindings_refuse_tensors_that_do_not_fit():
             call()
             pytest.fail(f"call {i} was accepted")
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("M,K,N,r", [(2000, 800, 328, 16), (900, 1752, 264, 24), (700, 2304, 136, 32), (420, 4104, 520, 40), (1100, 1608, 200, 64),
+                                     (450, 3592, 72, 72), (3000, 600, 1000, 8)])
+def test_lora_prompts_on_either_side_of_the_rows_and_launches(M, K, N, r):
+    # tiles of 32 and of 16 rows, one launch and two, ragged ends in rows, channels and ranks
+    _lora_case(M, [0, 1, 34, 34, M // 2 + 3, M - 5, M], [1, 0, 1, -1, 2, 0], K, N, r, 3)
+    _lora_case(M + 1, [0, M], [0], K, N, r, 1, in_place=True, pad=8)
