@@ -619,3 +619,15 @@ def test_lora_prompts_on_either_side_of_the_rows_and_launches(M, K, N, r):
     # tiles of 32 and of 16 rows, one launch and two, ragged ends in rows, channels and ranks
     _lora_case(M, [0, 1, 34, 34, M // 2 + 3, M - 5, M], [1, 0, 1, -1, 2, 0], K, N, r, 3)
     _lora_case(M + 1, [0, M], [0], K, N, r, 1, in_place=True, pad=8)
+
+
+@pytest.mark.parametrize("requests", [510, 511, 512, 513, 1023, 1025, 3000])
+def test_lora_many_requests(requests):
+    # runs of 0 to 3 rows: the request of a tile is found among few, or in two rounds among many
+    g = gen(requests)
+    lengths = torch.randint(0, 4, (requests,), generator=g, device=DEV).tolist()
+    starts = [0]
+    for n in lengths:
+        starts.append(starts[-1] + n)
+    adapters = torch.randint(-1, 5, (requests,), generator=g, device=DEV).tolist()
+    _lora_case(requests, starts, adapters, 64, 72, 8, 5)
