@@ -62,7 +62,7 @@ constexpr int kMaxRows = 1 << 24, kMaxCols = 1 << 21;
 int check_attend(int S, int n_heads, int n_kv_heads, int head_dim, int max_length)
 {
     if (S < 1 || S > 65535 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || max_length < 1 ||
-        max_length > (1 << 28) ||
+        max_length > (1 << 26) ||
         head_dim < 16 || head_dim > 256 || head_dim % 16 != 0 || n_heads > kMaxCols / head_dim)
         return MUXQ_ERR_SHAPE;
     return MUXQ_OK;

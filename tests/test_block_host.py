@@ -86,7 +86,7 @@ def test_gather_refuses(kw, status):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(q=None), 1), (dict(o=None), 1), (dict(table=None), 1), (dict(lengths=None), 1), (dict(S=0), 2), (dict(S=65536), 2), (dict(n_heads=6), 2),
-    (dict(n_heads=0), 2), (dict(ldq=504), 2), (dict(ldo=513), 2), (dict(ldt=0), 2), (dict(most=0), 2), (dict(most=129), 2),
+    (dict(n_heads=0), 2), (dict(ldq=504), 2), (dict(ldo=513), 2), (dict(ldt=0), 2), (dict(most=0), 2), (dict(most=129), 2), (dict(ldt=1 << 28, most=(1 << 26) + 1), 2),
     (dict(scale=float("nan")), 4), (dict(scale=float("inf")), 4), (dict(q=FAKE + 8), 3), (dict(o=AWAY + 4), 3), (dict(table=FAKE + 2), 3),
     (dict(lengths=FAKE + 1), 3), (dict(o=FAKE + 64), 4)])
 def test_attention_refuses(kw, status):
