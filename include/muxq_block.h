@@ -81,7 +81,8 @@ int muxq_kv_gather(const int32_t *slots, int M, const muxq_kv_cache *cache, void
  * A length below 1 (an idle place of the batch) gives a row of zeros, one above max_length counts as
  * max_length.  Tokens of a page outside [0, n_blocks) are left out as if masked.  What the cache holds
  * beyond a sequence's length, NaN included, has no influence.  max_length: the host's bound on
- * lengths[], 1 <= max_length <= ld_table * block_size, at most 2^26 (S <= 65535); the work is divided by it, so a bound near
+ * lengths[], 1 <= max_length <= ld_table * block_size, at most 2^26 (S <= 65535); the work is divided
+ * by it, so a bound near
  * the longest sequence is best.
  * Arithmetic: products of fp16 (codes are exact in fp16) with binary32 sums; the softmax weights enter
  * the second product as two 16-bit parts (see the kernel).
