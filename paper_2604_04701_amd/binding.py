@@ -800,7 +800,9 @@ def muxq_norm(x, weight, bias=None, residual=None, residual_scale=1.0, post_weig
         if gate.dim() == 1:
             _flat(gate, K, _F16, "gate")
         elif gate.shape == shape:
-            ldg = _rows(gate, "gate") if M > 1 else K
+            ldg = _rows(gate, "gate")
+            if M == 1:                  # (the stride of a single row says nothing)
+                ldg = K
         else:
             _refuse("muxq_norm: gate is [K] or [M, K]")
     args = (x.data_ptr(), M, K, xs[0], r_at, ldr, residual_scale,

@@ -1,0 +1,58 @@
+"""What the bindings of muxq_block.h make of their tensors, without a GPU: tensors that only say that they are on one, and a
+library that records its arguments."""
+import pytest
+import torch
+
+from paper_2604_04701_amd import binding as B
+
+
+class OnGpu(torch.Tensor):
+    """A tensor that passes for one on the GPU; what is made from it by indexing does too."""
+    is_cuda = True
+
+
+class Library:
+    """Entry points that write their arguments down and succeed."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def entry(*args):
+            self.calls.append((name, args))
+            return 0
+        return entry
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    library = Library()
+    monkeypatch.setattr(B, "lib", lambda: library)
+    monkeypatch.setattr(B, "_stream", lambda: None)
+    return library.calls
+
+
+def gpu(*shape, dtype=torch.float16):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
+
+
+def norm_args(M, K):
+    return dict(x=gpu(M, K), weight=gpu(K), out=gpu(M, K), residual_out=gpu(M, K))
+
+
+@pytest.mark.parametrize("M", [1, 3])
+def test_gates_that_are_refused(calls, M):
+    K = 64
+    wrong = {"every second channel": gpu(M, 2 * K)[:, ::2], "binary32": gpu(M, K, dtype=torch.float32), "host memory": torch.zeros(M, K).half()}
+    for what, gate in wrong.items():
+        with pytest.raises(B.MuxqError, match="gate"):
+            B.muxq_norm(**norm_args(M, K), gate=gate)
+        assert calls == [], what
+
+
+@pytest.mark.parametrize("M,of,stride", [(1, 64, 64), (1, 128, 64), (3, 64, 64), (3, 128, 128)])
+def test_gates_of_rows(calls, M, of, stride):
+    gate = gpu(M, of)[:, :64]
+    B.muxq_norm(**norm_args(M, 64), gate=gate)
+    (name, args), = calls
+    assert name == "muxq_norm" and args[9] == gate.data_ptr() and args[10] == stride
