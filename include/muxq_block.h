@@ -97,7 +97,8 @@ int muxq_paged_attention(const void *Q_fp16, int S, int n_heads, int ldq, const 
 
 /* Low-rank adapters of many requests beside a projection that they share:
  *   out[m] = Y[m] + scales[i] * (X[m] A_i^T) B_i^T,   i the adapter of m's request,
- * in binary32, rounded once to fp16.  X: M x K (the projection's input), Y: M x N (its output), out:
+ * in binary32, rounded once to fp16; X A_i^T enters the second product as two 16-bit parts of its row (22 bits of
+ * the row's largest); infinities and NaN come out as the formula has them.  X: M x K (the projection's input), Y: M x N (its output), out:
  * M x N, may be Y itself (same stride) but share no memory with X.  A: fp16 [n_adapters][r][K], B: fp16
  * [n_adapters][N][r], scales: float [n_adapters]; smaller ranks are padded with zeros.
  * Requests are runs of rows: request q has the rows starts[q] <= m < starts[q + 1] (int32 [n_requests + 1],

@@ -31,6 +31,19 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// w = hi + lo, hi cut towards zero, so that both have w's sign, and neither is 0 unless w is (`some`: w != 0 before it was scaled;
+// 2^-24 is beyond the 38 bits that stand below the row's largest): what an infinity on the other side of the product makes of w it makes of each part,
+// where lo = 0, or one of the other sign, would give NaN.  An infinity is both of its parts.
+__device__ __forceinline__ void store_parts(float w, bool some, _Float16 &hi_at, _Float16 &lo_at)
+{
+    const float tiny = some ? copysignf(5.9604645e-8f, w) : 0.0f;
+    const _Float16 cut = (_Float16)__builtin_amdgcn_cvt_pkrtz(w, 0.0f)[0];
+    const _Float16 hi = cut == (_Float16)0.0f ? (_Float16)tiny : cut;
+    const _Float16 rest = (_Float16)(w - (float)cut);
+    hi_at = hi;
+    lo_at = rest == (_Float16)0.0f ? (_Float16)tiny : (float)cut == w ? hi : rest;
+}
+
 // First row of request q, whatever the caller's bounds hold.
 __device__ __forceinline__ int start_of(const LoraArgs &g, int q) { return min(max(g.starts[q], 0), g.M); }
 
@@ -308,10 +321,7 @@ __global__ __launch_bounds__(kThreads, kRT == 1 || (kRT == 2 && (kTM == 1 || kPa
         for (int i = 0; i < per; ++i) {
             const int j = lane + 64 * i;
             if (j < 32 * RS) {
-                const float w = v[o][i] * up;
-                const _Float16 hi = (_Float16)w;
-                h_hi[m][j] = hi;
-                h_lo[m][j] = (_Float16)(w - (float)hi);
+                store_parts(v[o][i] * up, v[o][i] != 0.0f, h_hi[m][j], h_lo[m][j]);
             }
         }
     }
