@@ -65,8 +65,15 @@ __device__ __forceinline__ V load(const char *p)
     return __builtin_bit_cast(V, kOnce ? __builtin_nontemporal_load((const Word *)p) : *(const Word *)p);
 }
 
-// 2^(m - top) of a part with maximum m and sum l; one without weights counts nothing, unless NaN stands there.
-__device__ __forceinline__ float weight_of(float m, float l, float top) { return m == kFloor ? l : exp2_(m - top); }
+// 2^(m - top) of a part with maximum m and sum l, never quite 0, so that an infinity among the values stays one; one without
+// weights counts nothing, unless NaN stands there.
+__device__ __forceinline__ float weight_of(float m, float l, float top) { return m == kFloor ? l : fmaxf(exp2_(m - top), 1.1754944e-38f); }
+
+// The halves of a word that are infinite or NaN; the others as 0.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w)
+{
+    return w & ((((w & 0x7c007c00u) + 0x04000400u) >> 15 & 0x00010001u) * 0xffffu);
+}
 
 // How the work is divided.  groups == 0: a workgroup to a sequence and key-value head.  Otherwise `groups` workgroups
 // have equal shares of all steps (kStep tokens of one key-value head, and kBegin steps before the first) in the order
@@ -91,7 +98,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
     constexpr int KW = kInt8 ? NS / 2 : NS, VW = kInt8 ? VE / 4 : VE / 2;      // 16-byte pieces of a key row, words of a value row
     extern __shared__ __align__(16) char lds[];
     __shared__ float sh_m[kWaves][16], sh_l[kWaves][16];
-    __shared__ int sh_bad, sh_sum[kWaves];
+    __shared__ int sh_bad, sh_sum[kWaves], sh_loose[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
     const int subs = (a.group + kHeads<kD> - 1) / kHeads<kD>, pairs = a.c.n_kv_heads * subs;
     const int d = a.c.head_dim, shift = a.c.block_shift, mask = (1 << shift) - 1;
@@ -155,14 +162,19 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
         j = (int)(in - (long long)pair * n);
     }
 
-    for (int piece = 0;; ++piece) {
+    // A value that is infinite or NaN makes NaN of its sums, since the low part of its weight, or all of it, may be 0.  Where NaN is found
+    // the piece is gone through a second time for those values alone, at a weight of 1 (0 where the score is -infinity), which is all that
+    // counts there: `again`.
+    bool again = false;
+    for (int piece = 0;;) {
         const int kvh = pair / subs, sub = pair - kvh * subs;
         const int head0 = kvh * a.group + sub * kHeads<kD>, n_here = min(kHeads<kD>, a.group - sub * kHeads<kD>);
         const int len = length_of(s);
         int t0 = 0, t1 = len;
+        int steps = 0;
         bool whole = true;
         if constexpr (kShares) {
-            const int steps = (int)min((long long)(n - j), end - at);
+            steps = (int)min((long long)(n - j), end - at);
             t0 = min(len, max(0, j - kBegin) * kStep);
             t1 = min(len, max(0, j + steps - kBegin) * kStep);
             whole = steps == n;
@@ -330,11 +342,16 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                 if (__any(top > m + 7.0f)) {                    // rare after the first steps: a new maximum for the head
                     top = fmaxf(top, __shfl_xor(top, 16, 64));
                     top = fmaxf(top, __shfl_xor(top, 32, 64));
-                    const float to = fmaxf(m, top), keep = m == kFloor ? 0.0f : exp2_(m - to);
+                    const float to = fmaxf(m, top), keep = weight_of(m, 0.0f, to);
                     m = to;
                     l *= keep;
 #pragma unroll
                     for (int e = 0; e < VE; ++e) o[e] *= keep;
+                }
+                uint32_t some = 0;
+                if (again) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) some |= p[j] != kFloor ? 1u << j : 0u;
                 }
                 const float off = m == kFloor ? 0.0f : 8.0f - m;
 #pragma unroll
@@ -363,6 +380,21 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                     const fp16x2 r = __builtin_amdgcn_cvt_pkrtz(p[2 * j] - (float)h[0], p[2 * j + 1] - (float)h[1]);
                     hi[j] = __builtin_bit_cast(uint32_t, h);
                     lo[j] = __builtin_bit_cast(uint32_t, r);
+                }
+                if (again) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if constexpr (!kInt8) {
+                            hi[j] = (some >> (2 * j) & 1) * 0x3c00u | (some >> (2 * j + 1) & 1) * 0x3c000000u;
+#pragma unroll
+                            for (int x = 0; x < VW; ++x) v[2 * j][x] = not_finite(v[2 * j][x]), v[2 * j + 1][x] = not_finite(v[2 * j + 1][x]);
+                        } else {
+                            const fp16x2 h = __builtin_amdgcn_cvt_pkrtz(some >> (2 * j) & 1 ? w[2 * j] : 0.0f * w[2 * j],
+                                                                        some >> (2 * j + 1) & 1 ? w[2 * j + 1] : 0.0f * w[2 * j + 1]);
+                            hi[j] = not_finite(__builtin_bit_cast(uint32_t, h));
+                        }
+                        lo[j] = hi[j];
+                    }
                 }
                 const f16x8 ph = half8(hi[0], hi[1], hi[2], hi[3]), pl = half8(lo[0], lo[1], lo[2], lo[3]);
 #pragma unroll
@@ -396,7 +428,17 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
         if (lane < 16) sh_m[wave][lane] = m, sh_l[wave][lane] = l;
+        float any = 0.0f;                                 // NaN where a sum is infinite or NaN
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) any = __builtin_fmaf(o[e][i], 0.0f, any);
+        const bool wave_loose = __any(any != any && col < n_here);
+        if (lane == 0) sh_loose[wave] = wave_loose;
         __syncthreads();
+        bool loose = false;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) loose |= sh_loose[w] != 0;
         float top = sh_m[0][col];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh_m[w][col]);
@@ -436,17 +478,32 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
             f32x4 sum = {};
 #pragma unroll
             for (int w = 0; w < 4; ++w) sum += *(const f32x4 *)(sh_o + (w * n_here + h) * kD + e);
-            if (whole) {
-                const float inv = most == kFloor ? 0.0f : 1.0f / all;
+            _Float16 *const dst = a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e;
+            const int part = (blockIdx.x * 2 + (piece ? 1 : 0)) * min(a.group, kHeads<kD>) + h;
+            const float inv = most == kFloor ? 0.0f : 1.0f / all;
+            if (again) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    if (sum[x] - sum[x] == 0.0f) continue;
+                    if (whole)
+                        dst[x] = (_Float16)(sum[x] * inv);
+                    else
+                        plan.o[(long long)part * d + e + x] = sum[x];
+                }
+            } else if (whole) {
                 f16x4 r;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) r[x] = (_Float16)(sum[x] * inv);
-                *(f16x4 *)(a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e) = r;
+                *(f16x4 *)dst = r;
             } else {
-                const int part = (blockIdx.x * 2 + (piece ? 1 : 0)) * min(a.group, kHeads<kD>) + h;
                 *(f32x4 *)(plan.o + (long long)part * d + e) = sum;
                 if (e == 0) plan.ml[part] = make_float2(most, all);
             }
+        }
+        if (loose && !again) {
+            again = true;
+            at -= steps;
+            continue;
         }
         if constexpr (!kShares) return;
         if (at >= end) {
@@ -461,6 +518,8 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
         }
         __syncthreads();                                  // (a next piece without tokens goes straight to sh_m)
         // on to the next pair, or the next sequence that has steps
+        again = false;
+        ++piece;
         j = 0;
         if (++pair == pairs) {
             pair = 0;

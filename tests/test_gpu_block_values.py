@@ -66,3 +66,114 @@ def test_lora_infinities(M, K, N, r, starts):
     got = B.muxq_lora(*(t.to(DEV) for t in (X, A, Bm, scales)), ints(starts), ints(adapters), Y.to(DEV))
     torch.cuda.synchronize()
     check_places(got, want, tol, "adapters")
+
+
+# ---- attention of one new token ----------------------------------------------------------------
+
+
+def _exact_places(q, k, v, ks, vs, table, lengths, scale):
+    """attend64 on the CPU, with a bound that leaves out what is not finite."""
+    S, H, d = q.shape
+    heads, page = k.shape[1], k.shape[2]
+    want, tol = torch.zeros(S, H, d, dtype=torch.float64), torch.zeros(S, H, d, dtype=torch.float64)
+    for s, n in enumerate(lengths):
+        pages = table[s, :-(-n // page)].long()
+        for h in range(heads if n else 0):
+            kk, vv = (x[pages, h].double().reshape(-1, d)[:n] for x in (k, v))
+            if ks is not None:
+                kk, vv = kk * ks[pages, h].double().reshape(-1)[:n, None], vv * vs[pages, h].double().reshape(-1)[:n, None]
+            at = slice(h * (H // heads), (h + 1) * (H // heads))
+            qq = q[s, at].double()
+            p = torch.softmax(qq @ kk.t() * scale, 1)
+            want[s, at] = p @ vv
+            size_k, size_v = (torch.where(x.isfinite(), x.abs(), 0.0) for x in (kk, vv))
+            off = scale * (d + 8) * U32 * (qq.abs() @ size_k.t()).amax(1, keepdim=True) + 2.0 ** -16
+            tol[s, at] = U16 * want[s, at].abs() + TINY16 + 3 * off * (torch.nan_to_num(p) @ size_v)
+    return want, tol
+
+
+def _loose_cache(seed, lengths, H, heads, d, bits):
+    """A cache on the CPU, a table, queries, and set(s, t, ...): changes token t of sequence s in all heads."""
+    g = torch.Generator()
+    g.manual_seed(seed)
+    page = 16
+    need = [-(-n // page) for n in lengths]
+    order = torch.randperm(sum(need) + 1, generator=g).tolist()
+    table = torch.zeros(len(lengths), max(need), dtype=torch.int32)
+    at = 0
+    for i, n in enumerate(need):
+        table[i, :n] = torch.tensor(order[at:at + n], dtype=torch.int32)
+        at += n
+    shape = (len(order), heads, page, d)
+    k, v = (torch.randn(shape, generator=g).half() if bits == 16 else torch.randint(-127, 128, shape, generator=g).to(torch.int8) for _ in "kv")
+    ks, vs = (0.005 + 0.01 * torch.rand(shape[:3], generator=g) for _ in "kv") if bits == 8 else (None, None)
+    q = torch.randn(len(lengths), H, d, generator=g).half()
+    q[:, :, 0] = q[:, :, 0].abs() + 0.5
+    q[:, 1::2, 0] *= -1                          # what is -infinity to one query is infinity to its neighbour
+
+    def place(s, t):
+        return int(table[s, t // page]), slice(None), t % page
+    return q, k, v, ks, vs, table, place
+
+
+def _loose_check(q, k, v, ks, vs, table, lengths, what):
+    scale = q.shape[2] ** -0.5
+    want, tol = _exact_places(q, k, v, ks, vs, table, lengths, scale)
+    say(f"[attend] {what}, S={len(lengths)} H={q.shape[1]}/{k.shape[1]} d={q.shape[2]} {k.dtype} longest={max(lengths)}")
+    on = [None if x is None else x.to(DEV) for x in (q, k, v, table, ks, vs)]
+    got = B.muxq_paged_attention(*on[:4], ints(lengths), max(lengths), scale=scale, k_scale=on[4], v_scale=on[5])
+    torch.cuda.synchronize()
+    check_places(got, want, tol, what)
+    return want
+
+
+ROUTES = [[37, 20, 9, 64, 100, 128], [300, 257, 64, 700, 33, 512], [5000, 2700, 2600, 4000, 4097, 2900]]       # 4 waves, 8 waves, shares
+
+
+@pytest.mark.parametrize("lengths", ROUTES)
+@pytest.mark.parametrize("H,heads,d", [(4, 2, 64), (8, 1, 80), (3, 3, 128), (4, 2, 256)])
+def test_attention_infinities_of_fp16(lengths, H, heads, d):
+    q, k, v, ks, vs, table, place = _loose_cache(d, lengths, H, heads, d, 16)
+
+    def far(s, t):                               # a score of about -60: a weight that is 0 in 16 bits
+        group = q[s].view(heads, H // heads, d).float().mean(1)
+        k[place(s, t)] = (-60.0 * d ** 0.5 * group / group.square().sum(1, keepdim=True)).half()
+    n = lengths[0]
+    for t, x in ((1, INF), (n // 2, -INF)):                       # in full weight, alone, together, and NaN
+        v[place(0, t)][..., 3 if t == 1 else 4] = x
+        v[place(0, t)][..., 5] = x
+    v[place(0, n - 1)][..., 6] = math.nan
+    v[place(0, n - 2)][..., 7] = INF
+    for t, e in ((0, 2), (lengths[1] - 1, 9)):                    # beside tokens that outweigh them by far, before and behind
+        far(1, t)
+        v[place(1, t)][..., e] = -INF
+    k[place(2, 5)][..., 0] = -INF                                 # a score of -infinity (or infinity): what stands there counts nothing, unless
+    v[place(2, 5)][..., 8] = INF                                  # it is infinite
+    k[place(3, lengths[3] - 1)][..., 0] = math.nan
+    far(5, 0)
+    v[place(5, 0)][..., 1] = INF
+    v[place(5, lengths[5] // 2)][..., d - 1] = INF
+    want = _loose_check(q, k, v, ks, vs, table, lengths, "infinities")
+    assert want.isnan().any() and (want == INF).any() and (want == -INF).any() and want.isfinite().any()
+
+
+@pytest.mark.parametrize("lengths", ROUTES)
+@pytest.mark.parametrize("H,heads,d", [(4, 2, 64), (8, 1, 80), (3, 3, 128), (4, 2, 256)])
+def test_attention_infinite_scales(lengths, H, heads, d):
+    q, k, v, ks, vs, table, place = _loose_cache(d, lengths, H, heads, d, 8)
+
+    def far(s, t):
+        group = q[s].view(heads, H // heads, d).float().mean(1)
+        k[place(s, t)] = (-group / group.abs().amax(1, keepdim=True) * 127).round().to(torch.int8)
+        ks[place(s, t)] = 60.0 * d ** 0.5 * group.abs().amax(1) / 127 / group.square().sum(1)
+    v[place(0, 1)][..., 3:5] = 0                                  # infinity times a code of zero
+    vs[place(0, 1)] = INF
+    far(1, 0)
+    far(1, lengths[1] - 1)
+    vs[place(1, 0)] = INF
+    ks[place(3, lengths[3] - 1)] = math.nan
+    vs[place(4, lengths[4] // 2)] = math.nan
+    far(5, lengths[5] // 2)
+    vs[place(5, lengths[5] // 2)] = INF
+    want = _loose_check(q, k, v, ks, vs, table, lengths, "infinite scales")
+    assert want.isnan().any() and (want == INF).any() and (want == -INF).any() and want.isfinite().any()
