@@ -69,12 +69,6 @@ __device__ __forceinline__ V load(const char *p)
 // weights counts nothing, unless NaN stands there.
 __device__ __forceinline__ float weight_of(float m, float l, float top) { return m == kFloor ? l : fmaxf(exp2_(m - top), 1.1754944e-38f); }
 
-// The halves of a word that are infinite or NaN; the others as 0.
-__device__ __forceinline__ uint32_t not_finite(uint32_t w)
-{
-    return w & ((((w & 0x7c007c00u) + 0x04000400u) >> 15 & 0x00010001u) * 0xffffu);
-}
-
 // How the work is divided.  groups == 0: a workgroup to a sequence and key-value head.  Otherwise `groups` workgroups
 // have equal shares of all steps (kStep tokens of one key-value head, and kBegin steps before the first) in the order
 // sequence, head, step (fewer workgroups where there are fewer steps);
@@ -91,6 +85,43 @@ struct Plan {
 template <int kD>
 constexpr int kHeads = kD == 256 ? 8 : 16;
 
+// The values of tokens t0 to t1 that are infinite or NaN, four dimensions from e on, with weights of 1, or of 0 where the query's score is
+// -infinity: all that counts for a sum in which there is one.  The matrix product makes NaN of it, since the low part of a weight, or all of
+// it, may be 0 in 16 bits; a thread that finds NaN or an infinity goes through the tokens by itself.
+template <bool kInt8>
+__device__ __forceinline__ f32x4 loose_values(const AttendArgs &a, int s, int kvh, int head, int e, int t0, int t1)
+{
+    const int d = a.c.head_dim, shift = a.c.block_shift, mask = (1 << shift) - 1;
+    const _Float16 *const q = a.q + (long long)s * a.ldq + (long long)head * d;
+    f32x4 sum = {};
+    for (int t = t0; t < t1; ++t) {
+        const int page = a.table[(long long)s * a.ld_table + (t >> shift)];
+        if (page < 0 || page >= a.c.n_blocks) continue;
+        const long long row = page * a.c.ld_block + kvh * a.c.ld_head + (t & mask) * a.c.ld_token;
+        const long long at_s = (((long long)page * a.c.n_kv_heads + kvh) << shift) + (t & mask);
+        f32x4 v;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            if constexpr (kInt8)
+                v[x] = (float)((const int8_t *)a.c.v)[row + e + x] * a.c.v_scale[at_s];
+            else
+                v[x] = (float)((const _Float16 *)a.c.v)[row + e + x];
+        }
+        const f32x4 zero = v - v;
+        if (zero[0] == 0.0f && zero[1] == 0.0f && zero[2] == 0.0f && zero[3] == 0.0f) continue;
+        float score = 0.0f;
+        for (int i = 0; i < d; ++i)
+            score += (float)q[i] * (kInt8 ? (float)((const int8_t *)a.c.k)[row + i] : (float)((const _Float16 *)a.c.k)[row + i]);
+        score *= a.scale;
+        if constexpr (kInt8) score *= a.c.k_scale[at_s];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (zero[x] != 0.0f) sum[x] += score == kFloor ? 0.0f * v[x] : v[x];
+        if (sum[0] != sum[0] && sum[1] != sum[1] && sum[2] != sum[2] && sum[3] != sum[3]) break;
+    }
+    return sum;
+}
+
 template <int kD, bool kInt8, bool kFull, int kWaves, bool kShares>
 __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 8 ? 2 : 1) void k_attend(AttendArgs a, Plan plan)
 {
@@ -98,7 +129,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
     constexpr int KW = kInt8 ? NS / 2 : NS, VW = kInt8 ? VE / 4 : VE / 2;      // 16-byte pieces of a key row, words of a value row
     extern __shared__ __align__(16) char lds[];
     __shared__ float sh_m[kWaves][16], sh_l[kWaves][16];
-    __shared__ int sh_bad, sh_sum[kWaves], sh_loose[kWaves];
+    __shared__ int sh_bad, sh_sum[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
     const int subs = (a.group + kHeads<kD> - 1) / kHeads<kD>, pairs = a.c.n_kv_heads * subs;
     const int d = a.c.head_dim, shift = a.c.block_shift, mask = (1 << shift) - 1;
@@ -162,19 +193,14 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
         j = (int)(in - (long long)pair * n);
     }
 
-    // A value that is infinite or NaN makes NaN of its sums, since the low part of its weight, or all of it, may be 0.  Where NaN is found
-    // the piece is gone through a second time for those values alone, at a weight of 1 (0 where the score is -infinity), which is all that
-    // counts there: `again`.
-    bool again = false;
-    for (int piece = 0;;) {
+    for (int piece = 0;; ++piece) {
         const int kvh = pair / subs, sub = pair - kvh * subs;
         const int head0 = kvh * a.group + sub * kHeads<kD>, n_here = min(kHeads<kD>, a.group - sub * kHeads<kD>);
         const int len = length_of(s);
         int t0 = 0, t1 = len;
-        int steps = 0;
         bool whole = true;
         if constexpr (kShares) {
-            steps = (int)min((long long)(n - j), end - at);
+            const int steps = (int)min((long long)(n - j), end - at);
             t0 = min(len, max(0, j - kBegin) * kStep);
             t1 = min(len, max(0, j + steps - kBegin) * kStep);
             whole = steps == n;
@@ -342,16 +368,11 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                 if (__any(top > m + 7.0f)) {                    // rare after the first steps: a new maximum for the head
                     top = fmaxf(top, __shfl_xor(top, 16, 64));
                     top = fmaxf(top, __shfl_xor(top, 32, 64));
-                    const float to = fmaxf(m, top), keep = weight_of(m, 0.0f, to);
+                    const float to = fmaxf(m, top), keep = weight_of(m, l, to);
                     m = to;
                     l *= keep;
 #pragma unroll
                     for (int e = 0; e < VE; ++e) o[e] *= keep;
-                }
-                uint32_t some = 0;
-                if (again) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) some |= p[j] != kFloor ? 1u << j : 0u;
                 }
                 const float off = m == kFloor ? 0.0f : 8.0f - m;
 #pragma unroll
@@ -380,21 +401,6 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                     const fp16x2 r = __builtin_amdgcn_cvt_pkrtz(p[2 * j] - (float)h[0], p[2 * j + 1] - (float)h[1]);
                     hi[j] = __builtin_bit_cast(uint32_t, h);
                     lo[j] = __builtin_bit_cast(uint32_t, r);
-                }
-                if (again) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if constexpr (!kInt8) {
-                            hi[j] = (some >> (2 * j) & 1) * 0x3c00u | (some >> (2 * j + 1) & 1) * 0x3c000000u;
-#pragma unroll
-                            for (int x = 0; x < VW; ++x) v[2 * j][x] = not_finite(v[2 * j][x]), v[2 * j + 1][x] = not_finite(v[2 * j + 1][x]);
-                        } else {
-                            const fp16x2 h = __builtin_amdgcn_cvt_pkrtz(some >> (2 * j) & 1 ? w[2 * j] : 0.0f * w[2 * j],
-                                                                        some >> (2 * j + 1) & 1 ? w[2 * j + 1] : 0.0f * w[2 * j + 1]);
-                            hi[j] = not_finite(__builtin_bit_cast(uint32_t, h));
-                        }
-                        lo[j] = hi[j];
-                    }
                 }
                 const f16x8 ph = half8(hi[0], hi[1], hi[2], hi[3]), pl = half8(lo[0], lo[1], lo[2], lo[3]);
 #pragma unroll
@@ -428,17 +434,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
         if (lane < 16) sh_m[wave][lane] = m, sh_l[wave][lane] = l;
-        float any = 0.0f;                                 // NaN where a sum is infinite or NaN
-#pragma unroll
-        for (int e = 0; e < VE; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) any = __builtin_fmaf(o[e][i], 0.0f, any);
-        const bool wave_loose = __any(any != any && col < n_here);
-        if (lane == 0) sh_loose[wave] = wave_loose;
         __syncthreads();
-        bool loose = false;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) loose |= sh_loose[w] != 0;
         float top = sh_m[0][col];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh_m[w][col]);
@@ -478,32 +474,24 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
             f32x4 sum = {};
 #pragma unroll
             for (int w = 0; w < 4; ++w) sum += *(const f32x4 *)(sh_o + (w * n_here + h) * kD + e);
-            _Float16 *const dst = a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e;
-            const int part = (blockIdx.x * 2 + (piece ? 1 : 0)) * min(a.group, kHeads<kD>) + h;
-            const float inv = most == kFloor ? 0.0f : 1.0f / all;
-            if (again) {
+            const f32x4 zero = sum - sum;
+            if (!(zero[0] + zero[1] + (zero[2] + zero[3]) == 0.0f) && all == all) {
+                const f32x4 loose = loose_values<kInt8>(a, s, kvh, head0 + h, e, t0, t1);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    if (sum[x] - sum[x] == 0.0f) continue;
-                    if (whole)
-                        dst[x] = (_Float16)(sum[x] * inv);
-                    else
-                        plan.o[(long long)part * d + e + x] = sum[x];
-                }
-            } else if (whole) {
+                for (int x = 0; x < 4; ++x)
+                    if (loose[x] - loose[x] != 0.0f) sum[x] = loose[x];
+            }
+            if (whole) {
+                const float inv = most == kFloor ? 0.0f : 1.0f / all;
                 f16x4 r;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) r[x] = (_Float16)(sum[x] * inv);
-                *(f16x4 *)dst = r;
+                *(f16x4 *)(a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e) = r;
             } else {
+                const int part = (blockIdx.x * 2 + (piece ? 1 : 0)) * min(a.group, kHeads<kD>) + h;
                 *(f32x4 *)(plan.o + (long long)part * d + e) = sum;
                 if (e == 0) plan.ml[part] = make_float2(most, all);
             }
-        }
-        if (loose && !again) {
-            again = true;
-            at -= steps;
-            continue;
         }
         if constexpr (!kShares) return;
         if (at >= end) {
@@ -518,8 +506,6 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
         }
         __syncthreads();                                  // (a next piece without tokens goes straight to sh_m)
         // on to the next pair, or the next sequence that has steps
-        again = false;
-        ++piece;
         j = 0;
         if (++pair == pairs) {
             pair = 0;
