@@ -86,8 +86,9 @@ int muxq_kv_gather(const int32_t *slots, int M, const muxq_kv_cache *cache, void
  * the longest sequence is best.
  * Arithmetic: products of fp16 (codes are exact in fp16) with binary32 sums; the scale of a code's key multiplies its score; the
  * softmax weights enter the second product as two 16-bit parts: 22 bits, and a token's weight is cut to whole
- * multiples of 2^-32 of the largest (of its weight times its scale, against the largest of both, with codes).  Values (and scales of
- * values) that are infinite or NaN come out as the formula has them.
+ * multiples of 2^-32 of the largest (with codes weight times scale, to multiples of 2^-31 of the largest weight times the largest scale).
+ * Values (and scales of values) that are infinite or NaN, and a sequence whose scores are all -infinity (0 / 0), come out as the formula has
+ * them.
  * workspace: muxq_paged_attention_workspace_bytes(...) bytes, 256-byte aligned, content undefined on
  * entry; enough for every call with S and max_length no larger; NULL where that is 0.  Calls that share one
  * must not overlap in time. */

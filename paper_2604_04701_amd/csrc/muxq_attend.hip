@@ -66,8 +66,13 @@ __device__ __forceinline__ V load(const char *p)
 }
 
 // 2^(m - top) of a part with maximum m and sum l, never quite 0, so that an infinity among the values stays one; one without
-// weights counts nothing, unless NaN stands there.
+// weights counts nothing, unless NaN stands there.  (Where it has tokens, all of them with a score of -infinity, its sum is kNone: beside a
+// part with weights that is nothing, and where no part has any it says that the softmax is 0 / 0, not an empty row.)
+constexpr float kNone = 0x1p-60f;
 __device__ __forceinline__ float weight_of(float m, float l, float top) { return m == kFloor ? l : fmaxf(exp2_(m - top), 1.1754944e-38f); }
+
+// What the sum of the values is multiplied by in the end.
+__device__ __forceinline__ float factor_of(float m, float l) { return m != kFloor ? 1.0f / l : l == 0.0f ? 0.0f : __builtin_nanf(""); }
 
 // How the work is divided.  groups == 0: a workgroup to a sequence and key-value head.  Otherwise `groups` workgroups
 // have equal shares of all steps (kStep tokens of one key-value head, and kBegin steps before the first) in the order
@@ -433,6 +438,16 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
         // through the lower one's places.
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
+        if (__any(l == 0.0f)) {                           // no weights: are there tokens?
+            bool seen = false;
+            for (int tok = t0 + wave * kTile; tok < t1; tok += kWaves * kTile) {
+                const int kt = tok + (lane & (kTile - 1));
+                if (kt >= t1) break;
+                const int page = a.table[(long long)s * a.ld_table + (kt >> shift)];
+                seen |= page >= 0 && page < a.c.n_blocks;
+            }
+            if (__any(seen) && l == 0.0f) l = kNone;
+        }
         if (lane < 16) sh_m[wave][lane] = m, sh_l[wave][lane] = l;
         __syncthreads();
         float top = sh_m[0][col];
@@ -482,7 +497,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                     if (loose[x] - loose[x] != 0.0f) sum[x] = loose[x];
             }
             if (whole) {
-                const float inv = most == kFloor ? 0.0f : 1.0f / all;
+                const float inv = factor_of(most, all);
                 f16x4 r;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) r[x] = (_Float16)(sum[x] * inv);
@@ -490,7 +505,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
             } else {
                 const int part = (blockIdx.x * 2 + (piece ? 1 : 0)) * min(a.group, kHeads<kD>) + h;
                 *(f32x4 *)(plan.o + (long long)part * d + e) = sum;
-                if (e == 0) plan.ml[part] = make_float2(most, all);
+                if (e == 0) plan.ml[part] = make_float2(most, most == kFloor && all > 0.0f ? kNone : all);
             }
         }
         if constexpr (!kShares) return;
@@ -537,7 +552,7 @@ __global__ __launch_bounds__(512) void k_attend_join(AttendArgs a, Plan plan, in
             all += weight_of(x.x, x.y, top) * x.y;
         }
         for (int x = 1; x < 64; x <<= 1) all += __shfl_xor(all, x, 64);
-        if (lane == 0) sh_top[h] = top, sh_inv[h] = top == kFloor ? 0.0f : 1.0f / all;
+        if (lane == 0) sh_top[h] = top, sh_inv[h] = factor_of(top, all);
     }
     __syncthreads();
     const int lanes = d / 4, items = n_here * lanes, per = items < 512 ? 512 / items : 1;

@@ -177,3 +177,42 @@ def test_attention_infinite_scales(lengths, H, heads, d):
     vs[place(5, lengths[5] // 2)] = INF
     want = _loose_check(q, k, v, ks, vs, table, lengths, "infinite scales")
     assert want.isnan().any() and (want == INF).any() and (want == -INF).any() and want.isfinite().any()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("lengths", ROUTES)
+@pytest.mark.parametrize("H,heads,d", [(4, 2, 64), (8, 1, 80), (3, 3, 128), (4, 2, 256)])
+def test_attention_scores_of_minus_infinity(lengths, H, heads, d, bits):
+    q, k, v, ks, vs, table, place = _loose_cache(d, lengths, H, heads, d, bits)
+    q[:] = q.abs() + 0.01
+    page = k.shape[2]
+
+    def shut(s, tokens):                         # a score of -infinity to every query
+        for t in tokens:
+            if bits == 16:
+                k[place(s, t)][..., 0] = -INF
+            else:
+                k[place(s, t)] = -(k[place(s, t)].int().abs().clamp_min(1)).to(torch.int8)
+                ks[place(s, t)] = INF
+    shut(0, range(lengths[0]))                   # all: 0 / 0
+    shut(1, range(lengths[1] // 2))              # a half, either one: no weight
+    shut(2, range(lengths[2] // 2, lengths[2]))
+    shut(3, [t for t in range(lengths[3]) if t != lengths[3] - 3])           # all but one
+    shut(4, range(0, lengths[4], 2))
+    shut(5, range(lengths[5]))
+    last = lengths[5] - 1
+    if bits == 16:
+        k[place(5, last)][..., 0] = 0.5          # one is left at the very end
+    else:
+        ks[place(5, last)] = 0.01
+    want = _loose_check(q, k, v, ks, vs, table, lengths, "scores of -infinity")
+    assert want[0].isnan().all() and want[1:].isfinite().all()
+    # pages outside the cache leave their tokens out: of the first sequence all of them, zeros; of the second all but shut ones, 0 / 0
+    table = table.clone()
+    table[0] = -1
+    table[1, -(-(lengths[1] // 2) // page):] = k.shape[0]
+    shut(1, range(-(-(lengths[1] // 2) // page) * page))
+    on = [None if x is None else x.to(DEV) for x in (q, k, v, table, ks, vs)]
+    got = B.muxq_paged_attention(*on[:4], ints(lengths), max(lengths), k_scale=on[4], v_scale=on[5])
+    torch.cuda.synchronize()
+    assert (got[0] == 0).all() and got[1].isnan().all() and got[2:].isfinite().all()
