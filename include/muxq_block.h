@@ -108,8 +108,8 @@ int muxq_paged_attention(const void *Q_fp16, int S, int n_heads, int ldq, const 
  * ascending, starts[0] = 0, starts[n_requests] = M) and the adapter adapters[q] (int32; outside
  * [0, n_adapters), e.g. -1: none, its rows are copied from Y).  Rows in no request are not written; bounds
  * are clamped to [0, M].
- * workspace: muxq_lora_workspace_bytes(...) bytes, 16-byte aligned, content undefined on entry; NULL where
- * that is 0.  Calls that share one must not overlap in time.
+ * workspace: muxq_lora_workspace_bytes(...) bytes, 16-byte aligned, content undefined on entry; enough for every call with
+ * M, K, r and n_requests no larger; NULL where that is 0.  Calls that share one must not overlap in time.
  * Rules: K, N, r multiples of 8, r <= 128, K, N <= 2^21, M <= 2^24, row strides <= 2^25, n_adapters >= 1,
  * 1 <= n_requests <= 2^20. */
 size_t muxq_lora_workspace_bytes(int M, int K, int N, int r, int n_requests);   /* 0 on bad shapes, and where none is needed */

@@ -727,7 +727,7 @@ def muxq_paged_attention(q, k_cache, v_cache, block_table, lengths, max_length, 
 
 
 def alloc_lora_workspace(M, K, N, r, n_requests, device="cuda"):
-    """Workspace of a muxq_lora call of these sizes (empty where none is needed)."""
+    """Workspace of muxq_lora, also good for a smaller M, K, r or number of requests (empty where none is needed)."""
     return torch.empty(lib().muxq_lora_workspace_bytes(M, K, N, r, n_requests), dtype=torch.uint8, device=device)
 
 

@@ -14,6 +14,8 @@
 // whatever its size.
 #include "muxq_block_kernels.h"
 
+#include <algorithm>
+
 namespace muxq {
 namespace {
 
@@ -431,10 +433,13 @@ hipError_t launch(const LoraArgs &g, const Shape &p, hipStream_t s)
 
 }  // namespace
 
+// Enough for every call with M and n_requests no larger: fewer tiles have more pieces, so that a call's own parts of H would not be.  Pieces are
+// at most the steps of K, and less than 512 / tiles + 1, where there are more than M / 32 tiles.
 size_t lora_workspace_bytes(int M, int K, int N, int r, int n_requests)
 {
-    const Shape p = shape_of(M, K, N, r, n_requests);
-    return p.two_launches ? (size_t)p.k_pieces * M * r * 4 : 0;
+    if (!shape_of(M, K, N, r, n_requests).two_launches) return 0;
+    const long long steps = (K + kDeep - 1) / kDeep;
+    return (size_t)std::min(steps * M, 512ll * 32 + M) * r * 4;
 }
 
 hipError_t lora_prepare()

@@ -216,3 +216,45 @@ def test_attention_scores_of_minus_infinity(lengths, H, heads, d, bits):
     got = B.muxq_paged_attention(*on[:4], ints(lengths), max(lengths), k_scale=on[4], v_scale=on[5])
     torch.cuda.synchronize()
     assert (got[0] == 0).all() and got[1].isnan().all() and got[2:].isfinite().all()
+
+
+# ---- one workspace for many calls --------------------------------------------------------------
+
+
+def test_adapters_share_the_workspace_of_the_largest_batch():
+    g = gen(21)
+    K, N, r, n = 4096, 264, 32, 3
+    M, requests = 1600, 40
+    X, Y = normal(g, M, K), normal(g, M, N)
+    A, Bm = (normal(g, n, r, K, dtype=torch.float32) / 64).half(), normal(g, n, N, r)
+    scales = torch.rand(n, generator=g, device=DEV)
+    size = B.alloc_lora_workspace(M, K, N, r, requests).numel()
+    room = torch.full((size + 4096,), 0x7f, dtype=torch.uint8, device=DEV)
+    for m, q in ((M, requests), (M - 5, 1), (1300, 1), (900, 3), (511, 40), (200, 7), (33, 1), (16, 16), (1, 1)):
+        starts = [m * i // q for i in range(q + 1)]
+        adapters = [i % n for i in range(q)]
+        say(f"[lora] workspace of {M} rows for {m} of {q} requests")
+        got = B.muxq_lora(X[:m], A, Bm, scales, ints(starts), ints(adapters), Y[:m], workspace=room[:size])
+        torch.cuda.synchronize()
+        want, tol = lora64(X[:m], A, Bm, scales, starts, adapters, Y[:m])
+        check(got, want, tol, "adapters")
+        assert (room[size:] == 0x7f).all()
+
+
+def test_attention_shares_the_workspace_of_the_largest_batch():
+    # with shares, with fewer sequences and longer ones, and calls that need none
+    g = gen(22)
+    H, heads, d, page, most = 8, 4, 64, 16, 6000
+    k, v, ks, vs = make_cache(g, 2000, heads, page, d, 16)
+    size = B.attention_workspace_bytes(64, H, heads, d, most)
+    assert size > 0
+    room = torch.full((size + 4096,), 0x7f, dtype=torch.uint8, device=DEV)
+    for lengths in ([500] * 63 + [most], [most, 1, 3000], [1300], [2600, 2400], [100] * 64, [700, 0], [0], [most]):
+        table = torch.randint(0, 2000, (len(lengths), max(1, -(-max(lengths) // page))), generator=g, device=DEV).int()     # pages in common
+        q = normal(g, len(lengths), H, d)
+        say(f"[attend] workspace of 64 x {most} for {len(lengths)} to {max(lengths)}")
+        got = B.muxq_paged_attention(q, k, v, table, ints(lengths), max(max(lengths), 1), workspace=room[:size])
+        torch.cuda.synchronize()
+        want, tol = attend64(q, k, v, None, None, table, lengths, d ** -0.5)
+        check(got, want, tol, "attention")
+        assert (room[size:] == 0x7f).all()
