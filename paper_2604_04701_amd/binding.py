@@ -590,7 +590,9 @@ def _call(entry, args, workspace, stream, alloc, what):
     """entry(*args, workspace, its bytes, stream).  Without a workspace the call goes out with none: it is refused for a NULL
     pointer, with nothing enqueued, where one is needed, and only then is one allocated."""
     if workspace is not None:
-        status = entry(*args, workspace.data_ptr(), workspace.numel(), stream)
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            _refuse(f"{what}: the workspace is a contiguous GPU tensor")
+        status = entry(*args, workspace.data_ptr(), workspace.nbytes, stream)
     else:
         status = entry(*args, None, 0, stream)
         if status == 1:

@@ -56,3 +56,29 @@ def test_gates_of_rows(calls, M, of, stride):
     B.muxq_norm(**norm_args(M, 64), gate=gate)
     (name, args), = calls
     assert name == "muxq_norm" and args[9] == gate.data_ptr() and args[10] == stride
+
+
+def lora_args():
+    return dict(X=gpu(4, 64), A=gpu(2, 8, 64), B=gpu(2, 32, 8), scales=gpu(2, dtype=torch.float32), starts=gpu(3, dtype=torch.int32),
+                adapters=gpu(2, dtype=torch.int32), Y=gpu(4, 32), out=gpu(4, 32))
+
+
+def attend_args():
+    return dict(q=gpu(3, 4, 64), k_cache=gpu(4, 2, 16, 64), v_cache=gpu(4, 2, 16, 64), block_table=gpu(3, 2, dtype=torch.int32),
+                lengths=gpu(3, dtype=torch.int32), max_length=32, out=gpu(3, 4, 64))
+
+
+ROOMS = [(B.muxq_lora, lora_args, "workspace"), (B.muxq_paged_attention, attend_args, "workspace"), (B.muxq_norm, lambda: norm_args(70, 64), "scratch")]
+
+
+@pytest.mark.parametrize("call,args,name", ROOMS, ids=[c.__name__ for c, _, _ in ROOMS])
+def test_workspaces_that_are_refused(calls, call, args, name):
+    for what, room in (("host memory", torch.empty(512, dtype=torch.uint8)), ("every second byte", gpu(1024, dtype=torch.uint8)[::2])):
+        with pytest.raises(B.MuxqError, match="workspace"):
+            call(**args(), **{name: room})
+        assert calls == [], what
+    for room in (gpu(512, dtype=torch.uint8), gpu(128, dtype=torch.float32)):
+        calls.clear()
+        call(**args(), **{name: room})
+        (_, given), = calls
+        assert given[-3:] == (room.data_ptr(), 512, None)
