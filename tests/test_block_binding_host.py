@@ -82,3 +82,21 @@ def test_workspaces_that_are_refused(calls, call, args, name):
         call(**args(), **{name: room})
         (_, given), = calls
         assert given[-3:] == (room.data_ptr(), 512, None)
+
+
+def test_mfma_probe_does_not_time_the_loading_of_its_kernel(calls, monkeypatch):
+    class Event:
+        def __init__(self, **_):
+            pass
+
+        def record(self):
+            calls.append(("record", ()))
+
+        def elapsed_time(self, _):
+            return 1.0
+    monkeypatch.setattr(torch.cuda, "Event", Event)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda: None)
+    codes = torch.zeros(64, dtype=torch.int8)
+    tops, _ = B.muxq_probe_mfma_rate(codes, codes, iters=200, n_workgroups=256)
+    assert [name for name, _ in calls] == ["muxq_probe_mfma_rate", "record", "muxq_probe_mfma_rate", "record"]
+    assert calls[0][1][3] == 1 and calls[2][1][3] == 200 and tops == pytest.approx(256 * 4 * 200 * 8 * 65536.0 / 1e-3 / 1e12)
