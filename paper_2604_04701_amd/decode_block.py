@@ -75,6 +75,8 @@ class Batch:
     def __init__(self, g, S, lengths, max_tokens, page, d, adapters, rotated):
         per = -(-max_tokens // page)
         self.max_tokens, self.page, self.n_pages = max_tokens, page, S * per
+        self.longest = 0                                 # of the lengths, known on the host
+        self._grow(max(lengths) + 1)
         self.table = torch.randperm(self.n_pages, generator=g, device=DEV).int().view(S, per)
         self.positions = torch.tensor(lengths, dtype=torch.int32, device=DEV)       # of the new tokens
         self.lengths, self.slots = self.positions + 1, torch.empty_like(self.positions)
@@ -86,11 +88,17 @@ class Batch:
             self.cos_sin = torch.cat([angle.cos(), angle.sin()], 1).float().contiguous()
         self._place()
 
+    def _grow(self, longest):
+        if longest > self.max_tokens:
+            raise ValueError(f"a sequence of {longest} tokens, where the tables and angles hold {self.max_tokens}")
+        self.longest = longest
+
     def _place(self):
         at = self.positions.long()
         self.slots.copy_(self.table.gather(1, (at // self.page)[:, None])[:, 0] * self.page + at % self.page)
 
     def next_token(self):
+        self._grow(self.longest + 1)
         self.positions += 1
         self.lengths += 1
         self._place()
@@ -123,10 +131,12 @@ def main():
     ap.add_argument("--blocks", type=int, default=4)
     ap.add_argument("--batch", type=int, default=24)
     ap.add_argument("--context", type=int, default=512)
-    ap.add_argument("--tokens", type=int, default=32)
+    ap.add_argument("--tokens", type=int, default=32, help="half of them eager, half replayed")
     ap.add_argument("--fp16-cache", action="store_true")
     ap.add_argument("--rotated", action="store_true")
     args = ap.parse_args()
+    if args.tokens < 2:
+        ap.error("--tokens is 2 at least")
     B.muxq_init()
     stack, batch, x = make(args.width, args.heads, args.blocks, args.batch, args.context, args.tokens + 2,
                            kv_dtype=torch.float16 if args.fp16_cache else torch.int8, rotated=args.rotated)
