@@ -50,7 +50,7 @@ typedef struct {
  * (NULL: no queries).  Typically three column ranges of one projection's output.
  * slots: int32 [M], slot = page * block_size + token of the page.  A token whose slot lies outside
  * [0, n_blocks * block_size) is not stored (-1 for the padding of a batch); two tokens with the same slot
- * leave one of the two there.
+ * leave parts of both there.
  * Rotation: cos_sin float [n_positions][rot_dim], a row holds rot_dim / 2 cosines, then as many sines;
  * rot_dim a multiple of 8, 0 (no rotation, cos_sin and positions may be NULL) to head_dim.  Pair j of
  * a head is (x[j], x[j + rot_dim / 2]), with interleaved != 0 (x[2j], x[2j + 1]):
@@ -76,7 +76,7 @@ int muxq_kv_gather(const int32_t *slots, int M, const muxq_kv_cache *cache, void
 /* Attention of one new token of each of S sequences over the cache:
  *   O[s][h] = sum_t softmax_t(scale * Q[s][h] . K[t][h / g]) V[t][h / g],  t < lengths[s],
  * g = n_heads / n_kv_heads queries to each key-value head (n_heads % n_kv_heads == 0).  Q, O: S rows
- * of n_heads * head_dim fp16, row strides ldq, ldo.  Token t of sequence s is token t % block_size of
+ * of n_heads * head_dim fp16, row strides ldq, ldo; O may be Q itself (same stride).  Token t of sequence s is token t % block_size of
  * page block_table[s * ld_table + t / block_size]; table entries are int32.  lengths: int32 [S].
  * A length below 1 (an idle place of the batch) gives a row of zeros, one above max_length counts as
  * max_length.  Tokens of a page outside [0, n_blocks) are left out as if masked.  What the cache holds

@@ -496,6 +496,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                 for (int x = 0; x < 4; ++x)
                     if (loose[x] - loose[x] != 0.0f) sum[x] = loose[x];
             }
+            __builtin_amdgcn_wave_barrier();              // (O may be Q: a head's lanes are of one wave, and have read its query before one writes)
             if (whole) {
                 const float inv = factor_of(most, all);
                 f16x4 r;

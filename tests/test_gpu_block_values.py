@@ -124,6 +124,9 @@ def _loose_check(q, k, v, ks, vs, table, lengths, what):
     got = B.muxq_paged_attention(*on[:4], ints(lengths), max(lengths), scale=scale, k_scale=on[4], v_scale=on[5])
     torch.cuda.synchronize()
     check_places(got, want, tol, what)
+    B.muxq_paged_attention(*on[:4], ints(lengths), max(lengths), scale=scale, k_scale=on[4], v_scale=on[5], out=on[0])
+    torch.cuda.synchronize()
+    assert torch.equal(on[0].view(torch.int16), got.view(torch.int16)), "in place"
     return want
 
 
