@@ -68,7 +68,7 @@ int muxq_kv_append(const void *K_fp16, const void *V_fp16, int M, int ldk, int l
                    int interleaved, const muxq_kv_cache *cache, void *stream);
 
 /* The other way: rows of the cache as fp16 (codes times scale in binary32, rounded once), e.g. the
- * cached prefix of a prompt for an attention that wants it dense.  K_out, V_out: M rows of
+ * cached prefix of a prompt for a caller's own attention over it (there is none for prompts here).  K_out, V_out: M rows of
  * n_kv_heads * head_dim, row strides ldk, ldv.  Rows of slots outside the cache are zeros. */
 int muxq_kv_gather(const int32_t *slots, int M, const muxq_kv_cache *cache, void *K_out_fp16, int ldk,
                    void *V_out_fp16, int ldv, void *stream);

@@ -16,9 +16,11 @@
 //
 // How it is divided (Plan below): short or many sequences have a workgroup of 8 waves each and key-value head, and no second
 // launch; otherwise as many workgroups as the chip holds have equal shares, and a second launch joins what they cut through.
-// Measured: 64 sequences of 131 to 8192 tokens, 8 key-value heads of 128, fp16, 1.09 GB: 181 us, 6.0 TB/s; one of 131071 tokens
-// 95 us, 5.7 TB/s; 24 sequences to 1024, 20 heads of 64, 8-bit codes, 34 MB: 15.5 us, latency of 4 steps and of what comes
-// before and after them; one of 37 tokens 4.4 us.
+// Measured: 64 sequences of 131 to 8192 tokens, 8 key-value heads of 128, fp16, 1.09 GB: 183 us, 6.0 TB/s; one of 131071 tokens
+// 95 us, 5.7 TB/s; 64 of 4096 to 8192, 8 heads of 128, 8-bit codes, 0.83 GB: 152 us, 5.5 TB/s; 24 sequences to 1024, 20 heads of 64, codes,
+// 34 MB: 15.3 us, where a wave has 32 tokens on its way at a time, of 128 bytes in codes, and four such steps one after the other; one of
+// 37 tokens 5.2 us (kernel trace).  Heads of 144 to 256 in fp16 without shares keep arrays in scratch memory: 64 sequences to 1000, 4
+// heads of 256, 157 us, in codes 25.
 #include "muxq_block_kernels.h"
 
 #include <algorithm>

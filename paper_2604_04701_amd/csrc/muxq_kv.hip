@@ -5,7 +5,8 @@
 // the second run is the partners of the first, so that no value crosses lanes.  P lanes, a power of two, stand for
 // a head, and with many tokens each goes through four heads of its token with the sines it has loaded once (the table is binary32: for
 // 8 + 8 values of a head it is twice the head's bytes).  The abs-max of a head for its codes is a reduction over its P lanes.
-// Measured: 8192 tokens of 32 + 8 + 8 heads of 128, rotated, 206 MB: 39.8 us, 5.2 TB/s; 64 of them to codes 3.6 us.
+// Measured: 8192 tokens of 32 + 8 + 8 heads of 128, rotated, 206 MB: 39.9 us, 5.2 TB/s; 64 of them to codes 3.6 us (kernel trace).  In a graph,
+// inputs in the memory-side cache: the 8192 to fp16 32 us, to codes 32 us, read back as fp16 11.4 us from either.
 #include "muxq_block_kernels.h"
 
 namespace muxq {
@@ -206,7 +207,7 @@ hipError_t launch_kv_append(const AppendArgs &a, bool int8, bool interleaved, hi
     const int E = interleaved || a.rot_dim % 16 == 0 ? 8 : 4;
     int P = 1;
     while (P * 2 * E < a.c.head_dim) P *= 2;
-    // one head to a lane while that does not fill the chip (64 tokens of 48 heads with 8-bit codes: 5.2 us with the read-back,
+    // one head to a lane while that does not fill the chip (64 tokens of 48 heads with 8-bit codes: 5.4 us with the read-back,
     // 6.9 with four), then four (8192 tokens: 40.3 us, 50.3 with one)
     const bool many = (long long)a.M * (a.n_heads + 2 * a.c.n_kv_heads) * P > 1 << 18;
     if (E == 8) return many ? launch_append<8, 4>(a, P, int8, interleaved, s) : launch_append<8, 1>(a, P, int8, interleaved, s);

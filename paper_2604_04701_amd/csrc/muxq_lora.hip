@@ -8,8 +8,8 @@
 // H is what several strips of a tile compute again: it costs reads of X and A from the L2s, and saves a second
 // launch and the way of H through memory.  Where it would cost more than that, two launches: the first
 // divides K over workgroups too and leaves its parts of H in the workspace, binary32, the second adds them.
-// One token 768 -> 2304 at rank 8 4.6 us, 64 requests 1280 -> 3840 at rank 16 9.2 us, 8192 rows 4096 -> 4096 at rank 32 57 us (22 + 35
-// in two launches, 3.5 TB/s of what has to move).
+// One token 768 -> 2304 at rank 8 4.9 us, 64 requests 1280 -> 3840 at rank 16 9.6 us (kernel trace; each of its 8 strips reads its request's
+// A whole, 41 KB, for a row of a tile of 16), 8192 rows 4096 -> 4096 at rank 32 57 us (23 + 35 in two launches, 3.5 TB/s of what has to move).
 // H is binary32; the second product takes it as two fp16 parts (22 bits) of the row over a power of two,
 // whatever its size.
 #include "muxq_block_kernels.h"

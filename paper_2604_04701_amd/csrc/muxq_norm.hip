@@ -7,7 +7,7 @@
 // elements and its loads go out together.
 // Column maxima: every wave keeps those of the rows it writes; a workgroup's go to the scratch and a second launch folds
 // them.  Up to 64 rows their magnitudes are the maxima, and there is one launch.
-// Measured: 24 x 1280 3.1 us, 16384 x 1280 with both norms, a gate and the maxima 41 us, of which the rows take 36 (4.6 TB/s).
+// Measured (kernel trace): 24 x 1280 3.4 us, 16384 x 1280 with both norms, a gate and the maxima 41 us, of which the rows take 36 (4.6 TB/s).
 #include "muxq_block_kernels.h"
 
 namespace muxq {
@@ -196,8 +196,8 @@ __global__ __launch_bounds__(256) void k_norm_fold(const uint16_t *maxima, int r
     }
 }
 
-// Waves to a row.  us, one and four: 24 x 1280 3.7 / 2.8, 64 x 768 3.2 / 2.8, 256 x 1280 6.3 / 6.5, 1024 x 768 6.5 / 9.4,
-// 16384 x 1280 41.9 / 71.3, 4096 x 2048 (32 channels a lane) 19.9 / 18.0.
+// Waves to a row.  us in a graph, inputs in the memory-side cache, one and four: 24 x 1280 3.5 / 2.6, 64 x 768 3.0 / 2.6, 256 x 1280
+// 6.2 / 6.3, 1024 x 768 6.3 / 9.1, 16384 x 1280 33.3 / 54.5, 4096 x 1536 14.7 / 18.1, 4096 x 2048 (32 channels a lane) 20.4 / 19.2.
 int waves_of(int M, int K) { return K > 8192 ? 16 : K > 1536 || M <= 64 ? 4 : 1; }
 
 int groups_of(int M, int K)

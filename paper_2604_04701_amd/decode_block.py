@@ -4,7 +4,7 @@
 
 Each block is  norm -> c_attn (+ the request's adapter) -> keys and values to the paged cache, queries and keys
 rotated if asked -> attention over the cache -> c_proj -> norm with the residual stream -> MLP,  all of it through
-`binding`, with the channel maxima going from each norm to the quantised layer behind it.  Weights are random, of GPT-2's
+`binding`, with the channel maxima going from the first norm to c_attn (the MLP takes its own).  Weights are random, of GPT-2's
 shapes; every sequence starts with a random cached context of its own length.  The step is captured in a HIP graph once and
 replayed per token, the way a serving loop runs it; positions, lengths and slots are counted on up the device.
 """
