@@ -2,7 +2,9 @@
  * muxq_block.h -- C ABI of what stands between the quantised projections of muxq.h when a block
  * of a decoder serves requests: the paged key-value cache and the attention of one new token that
  * reads it, low-rank adapters beside a projection that many requests share, and the norms around
- * the residual stream, which hand the channel maxima to the next quantised layer.
+ * the residual stream, which hand the channel maxima to the next quantised layer; and what a sequence with several new
+ * tokens needs: attention of prompts, within a sliding window if asked, attention of the nodes of a drafted tree, the
+ * verification of drafted tokens, and pages and tokens moved within the cache.
  *
  * Conventions are those of muxq.h: DEVICE pointers owned by the caller; nothing is allocated, freed
  * or synchronised; every call only enqueues kernels on `stream` and may be captured into a graph (the first
@@ -141,6 +143,77 @@ int muxq_norm(const void *X_fp16, int M, int K, int ldx, const void *R_fp16, int
               const void *post_w, const void *post_b, const void *gate, int ldg, const void *w, const void *b,
               int kind, float eps, void *R_out_fp16, int ldro, void *Y_fp16, int ldy, void *slabs,
               void *scratch, size_t scratch_bytes, void *stream);
+
+/* ---- several new tokens of a sequence --------------------------------------------------------
+ * The rows of sequence s are starts[s] <= m < starts[s + 1] (int32 [S + 1], ascending, clamped to [0, M]); n of them are its
+ * n new tokens, which stand in the cache already, as the last n of its lengths[s] tokens: row starts[s] + i is token
+ * lengths[s] - n + i.  A length above max_length counts as max_length.  A sequence with more rows than max_new (max_nodes)
+ * counts as one without rows.  Rows in no sequence are not written.  S <= 65535, M <= 2^24.
+ *
+ * Attention of these tokens over the cache:
+ *   O[m][h] = sum_t softmax_t(scale * Q[m][h] . K[t][h / g]) V[t][h / g]   over the tokens t that m sees,
+ * g = n_heads / n_kv_heads (n_heads % n_kv_heads == 0).  Q, O: M rows of n_heads * head_dim fp16, row strides ldq, ldo, which share
+ * no memory.  Cache, table and pages as for muxq_paged_attention; tokens of a page outside [0, n_blocks) are left out.
+ * muxq_window_attention: token p = lengths[s] - n + i sees t <= p; with window > 0 of these t > p - window and t < sinks.
+ *   (window 0: all; sinks counts only with a window.)  One row a sequence is the form for decoding.
+ * muxq_tree_attention: the rows are the nodes of a tree (or forest), parents (int32 [M]) the parent of each as its number within the
+ *   sequence, smaller than its own; anything else (-1) marks a root.  Node i sees all tokens before the
+ *   tree (t < lengths[s] - n), itself and the nodes above it.  max_nodes <= 64.
+ * A row that sees nothing (a length below 1, pages outside the cache) is zeros.  What stands in places that a row
+ * does not see, NaN and infinity included, has no influence on it; infinite and NaN values in places that it sees
+ * come out as the formula has them, with weights that are never quite 0, and scores that are all -infinity give NaN (0 / 0).
+ * Arithmetic: products of fp16 with binary32 sums; scales of codes multiply scores and weights; statistics of the softmax are
+ * binary32; the weights enter the second product rounded to fp16 (11 bits, and whole multiples of 2^-32 of a row's largest, with
+ * codes 2^-31 of the largest weight times the largest scale).
+ * max_length: the host's bound on lengths[], 1 <= max_length <= ld_table * block_size, at most 2^26; max_new and max_nodes: the
+ * host's bound on the rows of a sequence.  The work is divided by them.
+ * workspace: ..._workspace_bytes(...) bytes, 256-byte aligned, content undefined on entry; enough for every call with S, max_new
+ * (max_nodes), max_length, window and sinks no larger (a window of 0 is the largest); NULL where that is 0.  Calls that share one must
+ * not overlap in time. */
+size_t muxq_window_attention_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length,
+                                             int window, int sinks);
+int muxq_window_attention(const void *Q_fp16, int M, int n_heads, int ldq, const muxq_kv_cache *cache,
+                          const int32_t *block_table, int ld_table, const int32_t *starts, const int32_t *lengths, int S,
+                          int max_new, int max_length, int window, int sinks, float scale, void *O_fp16, int ldo,
+                          void *workspace, size_t workspace_bytes, void *stream);
+size_t muxq_tree_attention_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_nodes, int max_length);
+int muxq_tree_attention(const void *Q_fp16, int M, int n_heads, int ldq, const muxq_kv_cache *cache,
+                        const int32_t *block_table, int ld_table, const int32_t *starts, const int32_t *lengths,
+                        const int32_t *parents, int S, int max_nodes, int max_length, float scale, void *O_fp16, int ldo,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* Drafted tokens against the target's probabilities.  Each sequence has a tree of n <= max_nodes <= 64 nodes (starts, parents as
+ * above; a chain is a tree), whose node 0 is its last token and stands already; tokens[m] (int32 [M]) is the token of node m.  target: float
+ * [M][V] (row stride ldt), row m what the target says after node m; draft: float [M][V] (ldd), row m what the children of
+ * node m were drawn from, NULL: they were chosen without drawing (a probability of 1).  uniforms: float [M] in [0, 1).
+ * From v = 0, r = target[v], Z = 1 the children c of v, ascending, are tried:
+ *   accepted if uniforms[c] * draft[v][x_c] * Z < r[x_c]: then v = c, and on with its children;
+ *   otherwise r = max(r / Z - draft[v], 0), Z = sum r, and on with the next one.  If Z is 0, no other child is accepted and r = target[v].
+ * Where no child is left the next token is the smallest t with r_0 + ... + r_t > uniforms[node 0] * (sum of r) (the last one with
+ * r_t > 0 if there is none, -1 if the sum is not positive).  All in binary64, so that the order of sums does not matter.
+ * uniforms NULL (draft is not read): the child whose token is the largest of target[v], the lowest index of equal ones (NaN counts as -infinity),
+ * is accepted, the first of several; where there is none that token is the next.
+ * A drafted token outside [0, V) is not accepted and leaves r as it is.  Probabilities need not sum to 1; infinite, NaN or
+ * negative ones give unspecified tokens within [-1, V).
+ * path: int32 [M], the accepted nodes of sequence s, as numbers within it, at starts[s] + j (0 first), -1 behind them; counts: int32 [S], how
+ * many; next_token: int32 [S].  A sequence without rows gives a count of 0 and a token of -1.  1 <= V <= 2^22, strides
+ * below 2^31. */
+int muxq_verify_tree(const float *target, int ldt, const float *draft, int ldd, int M, int V, const int32_t *tokens,
+                     const int32_t *parents, const float *uniforms, const int32_t *starts, int S, int max_nodes,
+                     int32_t *path, int32_t *counts, int32_t *next_token, void *stream);
+
+/* Pages dst[i] of the cache become copies of pages src[i] (int32 [n], n <= 2^24): keys, values and scales.  A pair with a page outside
+ * [0, n_blocks) is left out.  A page that two pairs write, or that one pair writes and another reads, has unspecified content. */
+int muxq_kv_copy(const int32_t *src, const int32_t *dst, int n, const muxq_kv_cache *cache, void *stream);
+
+/* The accepted nodes of each tree become the first of its new tokens in the cache: token lengths[s] - n + j becomes what token
+ * lengths[s] - n + path[starts[s] + j] was, for j < counts[s] (at most n <= max_nodes <= 64), keys, values and scales, as if
+ * all were read before any is written.  The sequence is then lengths[s] - n + counts[s] tokens long.  Arguments as
+ * muxq_verify_tree and the attention take and give them.  Numbers outside [0, n), tokens outside the table (ld_table * block_size
+ * tokens) and pages outside the cache are left out.  No two sequences may share the pages of their new tokens. */
+int muxq_kv_compact(const int32_t *path, const int32_t *counts, const int32_t *starts, const int32_t *lengths,
+                    const int32_t *block_table, int ld_table, int M, int S, int max_nodes, const muxq_kv_cache *cache,
+                    void *stream);
 
 #ifdef __cplusplus
 }

@@ -27,7 +27,9 @@ EXPORTS = ["muxq_version", "muxq_status_string", "muxq_k_pad", "muxq_wq_bytes",
            "muxq_probe_mfma_rate", "muxq_gemm_kernel", "muxq_code_kernel", "muxq_static_bytes", "muxq_static_layout_of",
            "muxq_prepare_static", "muxq_linear_static", "muxq_gelu_absmax",
            "muxq_kv_append", "muxq_kv_gather", "muxq_paged_attention", "muxq_paged_attention_workspace_bytes",
-           "muxq_lora", "muxq_lora_workspace_bytes", "muxq_norm", "muxq_norm_slabs", "muxq_norm_scratch_bytes"]
+           "muxq_lora", "muxq_lora_workspace_bytes", "muxq_norm", "muxq_norm_slabs", "muxq_norm_scratch_bytes",
+           "muxq_window_attention", "muxq_window_attention_workspace_bytes", "muxq_tree_attention",
+           "muxq_tree_attention_workspace_bytes", "muxq_verify_tree", "muxq_kv_copy", "muxq_kv_compact"]
 
 
 class MuxqError(RuntimeError):
@@ -164,6 +166,20 @@ def lib():
         L.muxq_norm_scratch_bytes.argtypes = [i, i]
         L.muxq_norm.restype = i
         L.muxq_norm.argtypes = [vp, i, i, i, vp, i, f, vp, vp, vp, i, vp, vp, i, f, vp, i, vp, i, vp, vp, sz, vp]
+        L.muxq_window_attention_workspace_bytes.restype = sz
+        L.muxq_window_attention_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
+        L.muxq_window_attention.restype = i
+        L.muxq_window_attention.argtypes = [vp, i, i, i, kv, vp, i, vp, vp, i, i, i, i, i, f, vp, i, vp, sz, vp]
+        L.muxq_tree_attention_workspace_bytes.restype = sz
+        L.muxq_tree_attention_workspace_bytes.argtypes = [i, i, i, i, i, i]
+        L.muxq_tree_attention.restype = i
+        L.muxq_tree_attention.argtypes = [vp, i, i, i, kv, vp, i, vp, vp, vp, i, i, i, f, vp, i, vp, sz, vp]
+        L.muxq_verify_tree.restype = i
+        L.muxq_verify_tree.argtypes = [vp, i, vp, i, i, i, vp, vp, vp, vp, i, i, vp, vp, vp, vp]
+        L.muxq_kv_copy.restype = i
+        L.muxq_kv_copy.argtypes = [vp, vp, i, kv, vp]
+        L.muxq_kv_compact.restype = i
+        L.muxq_kv_compact.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, kv, vp]
         _lib = L
     return _lib
 
@@ -818,3 +834,120 @@ def muxq_norm(x, weight, bias=None, residual=None, residual_scale=1.0, post_weig
             None if bias is None else _flat(bias, K, _F16, "bias"), _NORM[kind], eps, r_out_at, ldro, out.data_ptr(), os[0], _p(slabs))
     _call(lib().muxq_norm, args, scratch, _stream(), lambda: alloc_norm_scratch(M, K, x.device), "muxq_norm")
     return out, residual_out
+
+
+# ---- several new tokens of a sequence ----------------------------------------------------------
+
+def alloc_window_attention_workspace(S, n_heads, n_kv_heads, head_dim, max_new, max_length, window=0, sinks=0, device="cuda"):
+    """Workspace of muxq_window_attention, also good for fewer sequences and tokens and smaller windows (empty where none is needed)."""
+    n = lib().muxq_window_attention_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_new, max_length, window, sinks)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_tree_attention_workspace(S, n_heads, n_kv_heads, head_dim, max_nodes, max_length, device="cuda"):
+    """Workspace of muxq_tree_attention, also good for fewer sequences, nodes and tokens (empty where none is needed)."""
+    n = lib().muxq_tree_attention_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_nodes, max_length)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale, v_scale, out):
+    """The checks that both attentions of several new tokens share: (descriptor of the cache, out, arguments up to lengths)."""
+    M, n_heads, d = q.shape
+    c = _kv(k_cache, v_cache, k_scale, v_scale)
+    S = lengths.numel()
+    if out is None:
+        out = torch.empty((M, n_heads, d), dtype=torch.float16, device=q.device)
+    qs, os, ts = q.stride(), out.stride(), block_table.stride()
+    if not (q.dtype is out.dtype is _F16 and block_table.dtype is lengths.dtype is starts.dtype is _I32 and q.is_cuda and out.is_cuda and
+            block_table.is_cuda and lengths.is_cuda and starts.is_cuda and d == c.head_dim and out.shape == q.shape and
+            qs[2] == os[2] == 1 and (n_heads == 1 or qs[1] == os[1] == d) and block_table.dim() == 2 and block_table.shape[0] == S and
+            ts[1] == 1 and lengths.is_contiguous() and starts.is_contiguous() and starts.numel() == S + 1 and
+            max_length <= block_table.shape[1] * c.block_size):
+        _rows(q, "q"), _rows(out, "out"), _flat(lengths, S, _I32, "lengths"), _flat(starts, S + 1, _I32, "starts")
+        _refuse(f"{what}: q, out and the cache differ in head size, starts has not one entry more than lengths, or block_table is no "
+                "int32 GPU tensor [S, pages] with contiguous rows of max_length tokens")
+    return c, out, os[0], S, (q.data_ptr(), M, n_heads, qs[0], C.byref(c), block_table.data_ptr(),
+                              ts[0] if S > 1 else block_table.shape[1], starts.data_ptr(), lengths.data_ptr())
+
+
+def muxq_window_attention(q, k_cache, v_cache, block_table, starts, lengths, max_new, max_length, window=0, sinks=0, scale=None,
+                          k_scale=None, v_scale=None, out=None, workspace=None):
+    """Causal attention of the new tokens of each sequence, q [M, n_heads, d], over the cache, where they stand already: rows
+    starts[s]..starts[s + 1] (int32 [S + 1]) are the last of lengths[s] tokens (int32 [S]).  window: how many tokens a row sees, its own the
+    last of them (0: all), with the first `sinks` of the sequence beside them.  max_new, max_length: bounds on the rows and tokens of a
+    sequence known on the host.  scale: 1 / sqrt(d) when not given."""
+    c, out, ldo, S, args = _rows_args("muxq_window_attention", q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale,
+                                      v_scale, out)
+    args += (S, max_new, max_length, window, sinks, c.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), ldo)
+    _call(lib().muxq_window_attention, args, workspace, _stream(),
+          lambda: alloc_window_attention_workspace(S, q.shape[1], c.n_kv_heads, c.head_dim, max_new, max_length, window, sinks, q.device),
+          "muxq_window_attention")
+    return out
+
+
+def muxq_tree_attention(q, k_cache, v_cache, block_table, starts, lengths, parents, max_nodes, max_length, scale=None, k_scale=None,
+                        v_scale=None, out=None, workspace=None):
+    """Attention of the nodes of a drafted tree of each sequence, as muxq_window_attention without a window, but a node sees of the
+    new tokens only itself and the nodes above it; parents (int32 [M]): the number of each node's parent within its
+    sequence, -1 for a root.  max_nodes: a bound on the nodes of a tree, at most 64."""
+    c, out, ldo, S, args = _rows_args("muxq_tree_attention", q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale,
+                                      v_scale, out)
+    args += (_flat(parents, q.shape[0], _I32, "parents"), S, max_nodes, max_length, c.head_dim ** -0.5 if scale is None else scale,
+             out.data_ptr(), ldo)
+    _call(lib().muxq_tree_attention, args, workspace, _stream(),
+          lambda: alloc_tree_attention_workspace(S, q.shape[1], c.n_kv_heads, c.head_dim, max_nodes, max_length, q.device),
+          "muxq_tree_attention")
+    return out
+
+
+def muxq_verify_tree(target, tokens, starts, parents, max_nodes, draft=None, uniforms=None, path=None, counts=None, next_token=None):
+    """Drafted trees against the target's probabilities, target [M, V] float, row m what comes after node m: (path int32 [M], counts
+    int32 [S], next_token int32 [S]).  tokens, parents: int32 [M]; starts: int32 [S + 1]; draft [M, V] float: what each
+    node's children were drawn from (None: chosen without drawing); uniforms float [M] in [0, 1), None: greedy."""
+    M, V = target.shape
+    S = starts.numel() - 1
+    device = target.device
+    path = torch.empty(M, dtype=torch.int32, device=device) if path is None else path
+    counts = torch.empty(S, dtype=torch.int32, device=device) if counts is None else counts
+    next_token = torch.empty(S, dtype=torch.int32, device=device) if next_token is None else next_token
+    for name, t in (("target", target), ("draft", draft)):
+        if t is not None and (t.dtype is not _F32 or not t.is_cuda or t.dim() != 2 or t.shape != (M, V) or (t.stride(1) != 1 and V > 1)):
+            _refuse(f"{name}: a GPU tensor of float [{M}, {V}] with contiguous rows is expected")
+    # (a dimension of one element may carry any stride)
+    ldt = target.stride(0) if M > 1 else V
+    ldd = 0 if draft is None else draft.stride(0) if M > 1 else V
+    for name, t, n in (("path", path, M), ("counts", counts, S), ("next_token", next_token, S)):
+        if t.numel() != n:
+            _refuse(f"{name}: {n} entries are expected")
+    status = lib().muxq_verify_tree(target.data_ptr(), ldt, _p(draft), ldd, M, V, _flat(tokens, M, _I32, "tokens"),
+                                    _flat(parents, M, _I32, "parents"), _flat(uniforms, M, _F32, "uniforms"),
+                                    _flat(starts, S + 1, _I32, "starts"), S, max_nodes, _flat(path, M, _I32, "path"),
+                                    _flat(counts, S, _I32, "counts"), _flat(next_token, S, _I32, "next_token"), _stream())
+    if status != 0:
+        _check(status, "muxq_verify_tree")
+    return path, counts, next_token
+
+
+def muxq_kv_copy(src, dst, k_cache, v_cache, k_scale=None, v_scale=None):
+    """Pages dst[i] of the cache become copies of pages src[i] (int32 [n]; pairs with a page outside it are left out)."""
+    c = _kv(k_cache, v_cache, k_scale, v_scale)
+    n = src.numel()
+    if dst.numel() != n:
+        _refuse("muxq_kv_copy: src and dst differ in length")
+    status = lib().muxq_kv_copy(_flat(src, n, _I32, "src"), _flat(dst, n, _I32, "dst"), n, C.byref(c), _stream())
+    if status != 0:
+        _check(status, "muxq_kv_copy")
+
+
+def muxq_kv_compact(path, counts, starts, lengths, block_table, k_cache, v_cache, max_nodes, k_scale=None, v_scale=None):
+    """The accepted nodes of each tree (path, counts as muxq_verify_tree gives them) become the first of its new tokens in the
+    cache; starts, lengths (the nodes among them) and block_table as muxq_tree_attention takes them."""
+    c = _kv(k_cache, v_cache, k_scale, v_scale)
+    S, M = counts.numel(), path.numel()
+    if block_table.dtype is not _I32 or not block_table.is_cuda or block_table.dim() != 2 or block_table.shape[0] != S or block_table.stride(1) != 1:
+        _refuse("muxq_kv_compact: block_table is no int32 GPU tensor [S, pages] with contiguous rows")
+    status = lib().muxq_kv_compact(_flat(path, M, _I32, "path"), _flat(counts, S, _I32, "counts"), _flat(starts, S + 1, _I32, "starts"),
+                                   _flat(lengths, S, _I32, "lengths"), block_table.data_ptr(),
+                                   block_table.stride(0) if S > 1 else block_table.shape[1], M, S, max_nodes, C.byref(c), _stream())
+    if status != 0:
+        _check(status, "muxq_kv_compact")

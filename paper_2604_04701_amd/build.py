@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmuxq.so")
 SOURCES = ["muxq_api.hip", "muxq_scan.hip", "muxq_gemm.hip", "muxq_gemm_own.hip",
            "muxq_gemm_gelu.hip", "muxq_gemm_codes.hip", "muxq_few.hip", "muxq_act.hip", "muxq_probe.hip",
-           "muxq_block_api.hip", "muxq_kv.hip", "muxq_attend.hip", "muxq_lora.hip", "muxq_norm.hip"]
+           "muxq_block_api.hip", "muxq_kv.hip", "muxq_attend.hip", "muxq_lora.hip", "muxq_norm.hip",
+           "muxq_rows.hip", "muxq_verify.hip", "muxq_pages.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "--offload-arch=gfx950"
 FLAGS = [

@@ -374,6 +374,9 @@ int muxq_init(void)
     MUXQ_TRY(muxq::attend_prepare());
     MUXQ_TRY(muxq::lora_prepare());
     MUXQ_TRY(muxq::norm_prepare());
+    MUXQ_TRY(muxq::rows_prepare());
+    MUXQ_TRY(muxq::verify_prepare());
+    MUXQ_TRY(muxq::pages_prepare());
     void *p = nullptr;
     MUXQ_TRY(noalloc_scratch_ptr(&p));
     return MUXQ_OK;

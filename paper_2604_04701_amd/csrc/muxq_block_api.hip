@@ -68,6 +68,15 @@ int check_attend(int S, int n_heads, int n_kv_heads, int head_dim, int max_lengt
     return MUXQ_OK;
 }
 
+// Sizes of an attention call of several new tokens without its cache.
+int check_rows(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length, int window, int sinks, bool tree)
+{
+    const int st = check_attend(S, n_heads, n_kv_heads, head_dim, max_length);
+    if (st) return st;
+    if (max_new < 1 || max_new > (tree ? muxq::kMaxNodes : kMaxRows)) return MUXQ_ERR_SHAPE;
+    return window < 0 || sinks < 0 ? MUXQ_ERR_PARAM : MUXQ_OK;
+}
+
 #define MUXQ_TRY(expr)                          \
     do {                                        \
         if ((expr) != hipSuccess) return MUXQ_ERR_HIP; \
@@ -268,6 +277,139 @@ int muxq_norm(const void *X, int M, int K, int ldx, const void *R, int ldr, floa
     n.slabs = (uint16_t *)slabs;
     n.scratch = (uint16_t *)scratch;
     MUXQ_TRY(muxq::launch_norm(n, kind == MUXQ_NORM_RMS, (hipStream_t)stream));
+    return MUXQ_OK;
+}
+
+static int rows_attention(const void *Q, int M, int n_heads, int ldq, const muxq_kv_cache *cache, const int32_t *block_table,
+                          int ld_table, const int32_t *starts, const int32_t *lengths, const int32_t *parents, bool tree, int S,
+                          int max_new, int max_length, int window, int sinks, float scale, void *O, int ldo, void *workspace,
+                          size_t workspace_bytes, void *stream)
+{
+    if (!Q || !O || !block_table || !starts || !lengths || (tree && !parents)) return MUXQ_ERR_NULL;
+    muxq::RowsArgs a{};
+    int st = check_cache(cache, &a.c);
+    if (st) return st;
+    const int d = a.c.head_dim;
+    if ((st = check_rows(S, n_heads, a.c.n_kv_heads, d, max_new, max_length, window, sinks, tree))) return st;
+    const long long width = (long long)n_heads * d;
+    if (M < 1 || M > kMaxRows || bad_ld(ldq, width) || bad_ld(ldo, width)) return MUXQ_ERR_SHAPE;
+    if (ld_table < 1 || (long long)max_length > ((long long)ld_table << a.c.block_shift)) return MUXQ_ERR_SHAPE;
+    if (!(fabsf(scale) <= 3.4e38f)) return MUXQ_ERR_PARAM;
+    if (!aligned(Q, 16) || !aligned(O, 16) || !aligned(block_table, 4) || !aligned(starts, 4) || !aligned(lengths, 4) || !aligned(parents, 4))
+        return MUXQ_ERR_ALIGN;
+    if (share(Q, ldq, width, O, ldo, width, M)) return MUXQ_ERR_PARAM;
+    const size_t need = muxq::rows_workspace_need(S, n_heads, a.c.n_kv_heads, d, max_new, max_length, window, sinks, tree);
+    if (need > 0) {
+        if (!workspace) return MUXQ_ERR_NULL;
+        if (!aligned(workspace, 256)) return MUXQ_ERR_ALIGN;
+        if (workspace_bytes < need) return MUXQ_ERR_WORKSPACE;
+    }
+    a.q = (const _Float16 *)Q;
+    a.o = (_Float16 *)O;
+    a.table = block_table;
+    a.starts = starts;
+    a.lengths = lengths;
+    a.parents = tree ? parents : nullptr;
+    a.M = M; a.S = S;
+    a.n_heads = n_heads; a.group = n_heads / a.c.n_kv_heads;
+    a.ldq = ldq; a.ldo = ldo; a.ld_table = ld_table;
+    a.max_new = max_new; a.max_length = max_length;
+    a.window = window;
+    a.sinks = window ? sinks : 0;
+    a.scale = scale;
+    a.workspace = workspace;
+    MUXQ_TRY(muxq::launch_rows(a, cache->type == MUXQ_KV_INT8, (hipStream_t)stream));
+    return MUXQ_OK;
+}
+
+size_t muxq_window_attention_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length,
+                                             int window, int sinks)
+{
+    if (check_rows(S, n_heads, n_kv_heads, head_dim, max_new, max_length, window, sinks, false)) return 0;
+    return muxq::rows_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_new, max_length, window, window ? sinks : 0, false);
+}
+
+int muxq_window_attention(const void *Q, int M, int n_heads, int ldq, const muxq_kv_cache *cache, const int32_t *block_table,
+                          int ld_table, const int32_t *starts, const int32_t *lengths, int S, int max_new, int max_length,
+                          int window, int sinks, float scale, void *O, int ldo, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return rows_attention(Q, M, n_heads, ldq, cache, block_table, ld_table, starts, lengths, nullptr, false, S, max_new, max_length,
+                          window, sinks, scale, O, ldo, workspace, workspace_bytes, stream);
+}
+
+size_t muxq_tree_attention_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_nodes, int max_length)
+{
+    if (check_rows(S, n_heads, n_kv_heads, head_dim, max_nodes, max_length, 0, 0, true)) return 0;
+    return muxq::rows_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_nodes, max_length, 0, 0, true);
+}
+
+int muxq_tree_attention(const void *Q, int M, int n_heads, int ldq, const muxq_kv_cache *cache, const int32_t *block_table,
+                        int ld_table, const int32_t *starts, const int32_t *lengths, const int32_t *parents, int S, int max_nodes,
+                        int max_length, float scale, void *O, int ldo, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return rows_attention(Q, M, n_heads, ldq, cache, block_table, ld_table, starts, lengths, parents, true, S, max_nodes, max_length,
+                          0, 0, scale, O, ldo, workspace, workspace_bytes, stream);
+}
+
+int muxq_verify_tree(const float *target, int ldt, const float *draft, int ldd, int M, int V, const int32_t *tokens,
+                     const int32_t *parents, const float *uniforms, const int32_t *starts, int S, int max_nodes, int32_t *path,
+                     int32_t *counts, int32_t *next_token, void *stream)
+{
+    if (!target || !tokens || !parents || !starts || !path || !counts || !next_token) return MUXQ_ERR_NULL;
+    if (M < 1 || M > kMaxRows || S < 1 || S > 65535 || V < 1 || V > (1 << 22) || ldt < V || (draft && uniforms && ldd < V) ||
+        max_nodes < 1 || max_nodes > muxq::kMaxNodes)
+        return MUXQ_ERR_SHAPE;
+    for (const void *p : {(const void *)target, (const void *)draft, (const void *)tokens, (const void *)parents, (const void *)uniforms,
+                          (const void *)starts, (const void *)path, (const void *)counts, (const void *)next_token})
+        if (!aligned(p, 4)) return MUXQ_ERR_ALIGN;
+    muxq::VerifyArgs a{};
+    a.target = target;
+    a.draft = uniforms ? draft : nullptr;
+    a.uniforms = uniforms;
+    a.tokens = tokens;
+    a.parents = parents;
+    a.starts = starts;
+    a.path = path;
+    a.counts = counts;
+    a.next = next_token;
+    a.ldt = ldt; a.ldd = ldd;
+    a.M = M; a.V = V; a.S = S; a.max_nodes = max_nodes;
+    MUXQ_TRY(muxq::launch_verify(a, (hipStream_t)stream));
+    return MUXQ_OK;
+}
+
+int muxq_kv_copy(const int32_t *src, const int32_t *dst, int n, const muxq_kv_cache *cache, void *stream)
+{
+    if (!src || !dst) return MUXQ_ERR_NULL;
+    muxq::KvView c;
+    const int st = check_cache(cache, &c);
+    if (st) return st;
+    if (n < 1 || n > kMaxRows || c.n_kv_heads > kMaxCols / c.head_dim) return MUXQ_ERR_SHAPE;
+    if (!aligned(src, 4) || !aligned(dst, 4)) return MUXQ_ERR_ALIGN;
+    MUXQ_TRY(muxq::launch_kv_copy(src, dst, n, c, cache->type == MUXQ_KV_INT8, (hipStream_t)stream));
+    return MUXQ_OK;
+}
+
+int muxq_kv_compact(const int32_t *path, const int32_t *counts, const int32_t *starts, const int32_t *lengths,
+                    const int32_t *block_table, int ld_table, int M, int S, int max_nodes, const muxq_kv_cache *cache, void *stream)
+{
+    if (!path || !counts || !starts || !lengths || !block_table) return MUXQ_ERR_NULL;
+    muxq::CompactArgs a{};
+    const int st = check_cache(cache, &a.c);
+    if (st) return st;
+    if (M < 1 || M > kMaxRows || S < 1 || S > 65535 || ld_table < 1 || max_nodes < 1 || max_nodes > muxq::kMaxNodes ||
+        a.c.n_kv_heads > kMaxCols / a.c.head_dim)
+        return MUXQ_ERR_SHAPE;
+    for (const void *p : {path, counts, starts, lengths, block_table})
+        if (!aligned(p, 4)) return MUXQ_ERR_ALIGN;
+    a.path = path;
+    a.counts = counts;
+    a.starts = starts;
+    a.lengths = lengths;
+    a.table = block_table;
+    a.ld_table = ld_table;
+    a.M = M; a.S = S; a.max_nodes = max_nodes;
+    MUXQ_TRY(muxq::launch_kv_compact(a, cache->type == MUXQ_KV_INT8, (hipStream_t)stream));
     return MUXQ_OK;
 }
 

@@ -61,10 +61,46 @@ int norm_slab_rows(int M);                        // rows of maxima a call leave
 size_t norm_scratch_bytes(int M, int K, int k_pad);
 hipError_t launch_norm(const NormArgs &a, bool rms, hipStream_t s);
 
+constexpr int kMaxNodes = 64;           // nodes of a drafted tree: the bits of a word
+
+// Attention of several new tokens a sequence; parents: of a tree's nodes, NULL: causal, with a window.
+struct RowsArgs {
+    const _Float16 *q;
+    _Float16 *o;
+    const int32_t *table, *starts, *lengths, *parents;
+    int M, S, n_heads, group, ldq, ldo, ld_table, max_new, max_length, window, sinks;
+    float scale;
+    void *workspace;
+    KvView c;
+};
+size_t rows_workspace_need(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length, int window, int sinks, bool tree);
+size_t rows_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length, int window, int sinks, bool tree);
+hipError_t launch_rows(const RowsArgs &a, bool int8, hipStream_t s);
+
+struct VerifyArgs {
+    const float *target, *draft, *uniforms;
+    const int32_t *tokens, *parents, *starts;
+    int32_t *path, *counts, *next;
+    long long ldt, ldd;
+    int M, V, S, max_nodes;
+};
+hipError_t launch_verify(const VerifyArgs &a, hipStream_t s);
+
+hipError_t launch_kv_copy(const int32_t *src, const int32_t *dst, int n, const KvView &c, bool int8, hipStream_t s);
+struct CompactArgs {
+    const int32_t *path, *counts, *starts, *lengths, *table;
+    int ld_table, M, S, max_nodes;
+    KvView c;
+};
+hipError_t launch_kv_compact(const CompactArgs &a, bool int8, hipStream_t s);
+
 // Load a file's kernels on the current device, so that a first call may be captured.
 hipError_t attend_prepare();
 hipError_t kv_prepare();
 hipError_t lora_prepare();
 hipError_t norm_prepare();
+hipError_t rows_prepare();
+hipError_t verify_prepare();
+hipError_t pages_prepare();
 
 }  // namespace muxq
