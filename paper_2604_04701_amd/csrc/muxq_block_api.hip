@@ -298,7 +298,10 @@ static int rows_attention(const void *Q, int M, int n_heads, int ldq, const muxq
     if (!aligned(Q, 16) || !aligned(O, 16) || !aligned(block_table, 4) || !aligned(starts, 4) || !aligned(lengths, 4) || !aligned(parents, 4))
         return MUXQ_ERR_ALIGN;
     if (share(Q, ldq, width, O, ldo, width, M)) return MUXQ_ERR_PARAM;
-    const size_t need = muxq::rows_workspace_need(S, n_heads, a.c.n_kv_heads, d, max_new, max_length, window, sinks, tree);
+    a.window = window;
+    a.sinks = window ? sinks : 0;
+    a.max_new = max_new < M ? max_new : M;
+    const size_t need = muxq::rows_workspace_need(S, n_heads, a.c.n_kv_heads, d, a.max_new, max_length, a.window, a.sinks, tree);
     if (need > 0) {
         if (!workspace) return MUXQ_ERR_NULL;
         if (!aligned(workspace, 256)) return MUXQ_ERR_ALIGN;
@@ -313,9 +316,7 @@ static int rows_attention(const void *Q, int M, int n_heads, int ldq, const muxq
     a.M = M; a.S = S;
     a.n_heads = n_heads; a.group = n_heads / a.c.n_kv_heads;
     a.ldq = ldq; a.ldo = ldo; a.ld_table = ld_table;
-    a.max_new = max_new; a.max_length = max_length;
-    a.window = window;
-    a.sinks = window ? sinks : 0;
+    a.max_length = max_length;
     a.scale = scale;
     a.workspace = workspace;
     MUXQ_TRY(muxq::launch_rows(a, cache->type == MUXQ_KV_INT8, (hipStream_t)stream));

@@ -2,7 +2,19 @@
 // visible, or the nodes of a drafted tree.
 //
 // O = sum_t p_t V_t / sum_t p_t, p_t = 2^(s_t - m), s_t = scale log2(e) q . K_t, over the tokens that a row sees, with the running
-// maximum and sum of the softmax.  A wave has a row and head: a lane scores a token of 64, then the lanes have the dimensions.
+// maximum and sum of the softmax, so that keys and values are read once for all rows of a workgroup.  Rows are (token, head) pairs of the
+// heads that share a key-value head, in this order: many rows make it a matrix product (4 d operations for a row and token, bound by the matrix
+// pipes), few rows a stream through the cache (bound by memory).
+//
+// Keys and values of a tile of tokens go through LDS as fp16, 8-bit codes converted on the way (exactly).  Both products are
+// 32 x 32 x 16 steps with the tokens, or the dimensions, as rows of the left operand and 32 rows of the problem as the columns of the right one: scores
+// come out with a row per lane column, which is where the weights of the second product have to stand, so that they never leave their
+// lanes.  The second product's left operand is the transposed values, which LDS turns while it reads (16 lanes, 4 tokens of 16 dimensions).
+// 16-byte pieces of a token's row are permuted by its number, so that neither kind of read meets the same banks twice.
+//
+// Weights are 2^(s - m + 8), rounded to fp16, and m follows the maximum only when a score is 7 above it, which is rare: up to
+// 2^15, so that small ones keep their bits.  The scale of a key goes to its score, the scale of a value to its
+// weight, over a running power of two.
 #include "muxq_block_kernels.h"
 
 #include <algorithm>
@@ -10,105 +22,675 @@
 namespace muxq {
 namespace {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef s16x4 __attribute__((address_space(3))) *LdsQuad;
+
+constexpr int kChunk = 32;                    // tiles whose pages stand in LDS at a time
+constexpr int kLoose = 32;                    // tiles with infinite or NaN values that are remembered one by one
 constexpr float kFloor = -__builtin_inff();
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <bool kInt8>
-__global__ __launch_bounds__(64) void k_rows(RowsArgs a)
+// Four codes of a word as fp16 values, exactly: code + 128 in the low byte of 0x64.. is 1024 + code + 128.
+__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t &lo, uint32_t &hi)
 {
-    __shared__ float sh_p[64];
-    __shared__ long long sh_row[64], sh_scale[64];
-    const int s = blockIdx.y, i = blockIdx.x, lane = threadIdx.x, d = a.c.head_dim;
-    const int first = max(0, min(a.starts[s], a.M)), n = max(0, min(a.starts[s + 1], a.M)) - first;
-    if (n > a.max_new || i >= n) return;
-    const int len = max(0, min(a.lengths[s], a.max_length)), shift = a.c.block_shift, ctx = len - n, m0 = first + i;
-    uint64_t above = 0;                  // the nodes that a node sees
-    if (a.parents)
-        for (int x = i; x >= 0 && x < n;) {
-            above |= 1ull << x;
-            const int up = a.parents[first + x];
-            x = up < x ? up : -1;
+    const uint32_t u = w ^ 0x80808080u;
+    const uint32_t a = __builtin_amdgcn_perm(0x64646464u, u, 0x07010700u), b = __builtin_amdgcn_perm(0x64646464u, u, 0x07030702u);
+    const f16x2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+    lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, a) - bias);
+    hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, b) - bias);
+}
+
+// 2^(m - top) of a part with maximum m and sum l, never quite 0, so that an infinity among the values stays one; one without
+// weights counts nothing, unless NaN stands there.  (Where it has tokens, all of them with a score of -infinity, its sum is kNone: beside a
+// part with weights that is nothing, and where no part has any it says that the softmax is 0 / 0, not an empty row.)
+constexpr float kNone = 0x1p-60f;
+__device__ __forceinline__ float weight_of(float m, float l, float top) { return m == kFloor ? l : fmaxf(exp2_(m - top), 1.1754944e-38f); }
+
+// What the sum of the values is multiplied by in the end.
+__device__ __forceinline__ float factor_of(float m, float l) { return m != kFloor ? 1.0f / l : l == 0.0f ? 0.0f : __builtin_nanf(""); }
+
+// How the work is divided: a workgroup to a sequence, key-value head, tile of rows and piece of `tiles` tiles of tokens.  Rows that
+// see no more tiles than that are finished by their first piece; the others leave parts in the workspace.
+struct Plan {
+    int row_tiles, pieces, tiles;         // (the last piece has what is left)
+    float *o;           // [row tile of all][piece][rows of a tile][d], unnormalised
+    float2 *ml;         // [row tile of all][piece][rows of a tile]: m and the sum
+};
+
+// What one workgroup's rows are and see.
+template <int kTT>
+struct Span {
+    int s, kvh, first, n, len, ctx;           // rows first..first + n of the call, tokens before the first
+    long long row0;                           // of the sequence's rows (token, head)
+    int i_lo, i_hi, t1;                       // its tokens, and the first token that none of its rows sees
+    int sink_tiles, window_from, count;       // tiles that they see: the first ones, then from window_from on
+
+    __device__ __forceinline__ bool find(const RowsArgs &a, int x, int seq, int row_tiles, int rows)
+    {
+        s = seq;
+        const int tile = x / a.c.n_kv_heads;
+        kvh = x - tile * a.c.n_kv_heads;
+        first = max(0, min(a.starts[s], a.M));
+        n = max(0, min(a.starts[s + 1], a.M)) - first;
+        if (n < 1 || n > a.max_new) return false;
+        row0 = (long long)(row_tiles - 1 - tile) * rows;          // the last tokens see most: they come first
+        if (row0 >= (long long)n * a.group) return false;
+        len = max(0, min(a.lengths[s], a.max_length));
+        ctx = len - n;
+        i_lo = (int)(row0 / a.group);
+        i_hi = min(n - 1, (int)((row0 + rows - 1) / a.group));
+        t1 = a.parents ? len : max(0, min(len, ctx + i_hi + 1));
+        sink_tiles = window_from = 0;
+        count = (t1 + kTT - 1) / kTT;
+        if (a.window) {
+            const int from = max(0, (int)max(-1ll, (long long)ctx + i_lo - a.window) + 1) / kTT, sinks = (min(a.sinks, t1) + kTT - 1) / kTT;
+            if (from > sinks) sink_tiles = sinks, window_from = from, count = max(0, count - from) + sinks;
         }
-    for (int h = 0; h < a.n_heads; ++h) {
-        const int kvh = h / a.group;
-        const _Float16 *const q = a.q + (long long)m0 * a.ldq + (long long)h * d;
-        float m = kFloor, l = 0.0f, o[4] = {}, loose[4] = {};
-        bool any = false;
-        for (int t0 = 0; t0 < len; t0 += 64) {
-            const int t = t0 + lane;
-            bool there = t < len;
-            if (a.parents)
-                there = there && (t < ctx || (t - ctx >= 0 && t - ctx < n && (above >> (t - ctx) & 1)));
-            else
-                there = there && t <= ctx + i && (a.window == 0 || t > (long long)ctx + i - a.window || t < a.sinks);
-            int page = -1;
-            if (there) page = a.table[(long long)s * a.ld_table + (t >> shift)];
-            there = there && page >= 0 && page < a.c.n_blocks;
-            float score = kFloor, vs = 1.0f;
-            const long long row = there ? page * a.c.ld_block + kvh * a.c.ld_head + (t & ((1 << shift) - 1)) * a.c.ld_token : -1;
-            if (there) {
-                float sum = 0.0f;
-                for (int e = 0; e < d; ++e)
-                    sum += (float)q[e] * (kInt8 ? (float)((const int8_t *)a.c.k)[row + e] : (float)((const _Float16 *)a.c.k)[row + e]);
-                if (kInt8) {
-                    const long long at = (((long long)page * a.c.n_kv_heads + kvh) << shift) + (t & ((1 << shift) - 1));
-                    sum *= a.c.k_scale[at];
-                    vs = a.c.v_scale[at];
-                }
-                score = sum * (a.scale * 1.44269504088896f);
+        return true;
+    }
+    __device__ __forceinline__ int tile_of(int j) const { return j < sink_tiles ? j : window_from + j - sink_tiles; }
+};
+
+// A row: its place in the sequence, its head, and what it sees.
+struct Row {
+    int i, head, p, sinks;
+    uint32_t window;
+    uint64_t above;           // of a tree's nodes
+    int ctx;
+
+    __device__ __forceinline__ void find(const RowsArgs &a, int kvh, int n, int ctx_, int i_lo, int local)
+    {
+        i = min(n - 1, i_lo + local / a.group);
+        head = kvh * a.group + local % a.group;
+        ctx = ctx_;
+        p = ctx + i;
+        window = a.window ? a.window : 0x80000000u;
+        sinks = min(a.sinks, p + 1);
+    }
+    __device__ __forceinline__ bool sees(bool tree, int t) const
+    {
+        if (!tree) return (uint32_t)(p - t) < window || t < sinks;
+        const int x = t - ctx;
+        return t < ctx || ((uint32_t)x < 64u && (above >> x & 1));
+    }
+};
+
+// The nodes above node i and itself.
+__device__ __forceinline__ uint64_t nodes_above(const int32_t *parents, int i)
+{
+    uint64_t above = 0;
+    for (;;) {
+        above |= 1ull << i;
+        const int up = parents[i];
+        if (up < 0 || up >= i) return above;
+        i = up;
+    }
+}
+
+// Infinite and NaN values that the rows of a workgroup see, with weights of 1, or of 0 where the row's score is -infinity: all that counts for
+// a sum in which there is one.  The tiles' values went into the products without them; here they decide what they stand for.
+template <bool kInt8, int kTT>
+__device__ void put_loose(const RowsArgs &a, const Span<kTT> &w, int rows, int j0, int j1, const int *tiles, int n_tiles,
+                                                    const int32_t *parents, _Float16 *o, float *part)
+{
+    const int d = a.c.head_dim, quads = d / 4, shift = a.c.block_shift, mask = (1 << shift) - 1;
+    const int local0 = (int)(w.row0 - (long long)w.i_lo * a.group);
+    const int n_rows = (int)min((long long)rows, (long long)w.n * a.group - w.row0);
+    for (int item = threadIdx.x; item < n_rows * quads; item += blockDim.x) {
+        const int r = item / quads, e = (item - r * quads) * 4;
+        Row row;
+        row.find(a, w.kvh, w.n, w.ctx, w.i_lo, local0 + r);
+        row.above = a.parents ? nodes_above(parents, row.i) : 0;
+        const _Float16 *const q = a.q + (long long)(w.first + row.i) * a.ldq + (long long)row.head * d;
+        f32x4 sum = {};
+        const int n = n_tiles > kLoose ? j1 - j0 : n_tiles;
+        for (int x = 0; x < n; ++x) {
+            const int t0 = w.tile_of(n_tiles > kLoose ? j0 + x : tiles[x]) * kTT;
+            for (int t = t0; t < min(t0 + kTT, w.t1); ++t) {
+                if (!row.sees(a.parents != nullptr, t)) continue;
+                const int page = a.table[(long long)w.s * a.ld_table + (t >> shift)];
+                if (page < 0 || page >= a.c.n_blocks) continue;
+                const long long at = page * a.c.ld_block + w.kvh * a.c.ld_head + (t & mask) * a.c.ld_token;
+                const long long at_s = (((long long)page * a.c.n_kv_heads + w.kvh) << shift) + (t & mask);
+                f32x4 v;
+                for (int y = 0; y < 4; ++y)
+                    v[y] = kInt8 ? (float)((const int8_t *)a.c.v)[at + e + y] * a.c.v_scale[at_s] : (float)((const _Float16 *)a.c.v)[at + e + y];
+                const f32x4 zero = v - v;
+                if (zero[0] == 0.0f && zero[1] == 0.0f && zero[2] == 0.0f && zero[3] == 0.0f) continue;
+                float score = 0.0f;
+                for (int y = 0; y < d; ++y)
+                    score += (float)q[y] * (kInt8 ? (float)((const int8_t *)a.c.k)[at + y] : (float)((const _Float16 *)a.c.k)[at + y]);
+                score *= a.scale;
+                if (kInt8) score *= a.c.k_scale[at_s];
+                for (int y = 0; y < 4; ++y)
+                    if (zero[y] != 0.0f) sum[y] += score == kFloor ? 0.0f * v[y] : v[y];
             }
-            if (!__any(there)) continue;
-            any = true;
-            float top = score;
-            for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-            const float to = fmaxf(m, top), keep = m == kFloor ? 0.0f : exp2_(m - to);
-            m = to;
-            const float p = !there || score == kFloor ? 0.0f : exp2_(score - m);
-            float sum = p;
-            for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
-            l = l * keep + sum;
-            __syncthreads();
-            sh_p[lane] = p * vs;
-            sh_row[lane] = row;
-            sh_scale[lane] = score == kFloor ? 0 : 1;
-            __syncthreads();
-            for (int x = 0; x < 4; ++x) o[x] *= keep;
-            for (int j = 0; j < 64; ++j) {
-                if (sh_row[j] < 0) continue;
+        }
+        for (int y = 0; y < 4; ++y)
+            if (sum[y] - sum[y] != 0.0f) {
+                if (part)
+                    part[(long long)r * d + e + y] = sum[y];
+                else
+                    o[(long long)(w.first + row.i) * a.ldo + (long long)row.head * d + e + y] = (_Float16)sum[y];
+            }
+    }
+}
+
+// kD: the head's dimensions, padded; kWaves, kWR of them along the rows, 32 each, the others divide a tile's tokens; kTT: tokens of a tile.
+template <int kD, bool kInt8, int kWaves, int kWR, int kTT>
+__global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void k_rows(RowsArgs a, Plan plan)
+{
+    constexpr int kThreads = 64 * kWaves, kWT = kWaves / kWR, kR = 32 * kWR, kNB = kTT / kWT / 32;          // waves along tokens; rows; blocks of 32 tokens of a wave
+    constexpr int kPieces = kD / 8;                                                 // 16-byte pieces of a row in LDS
+    constexpr int kCH = kInt8 ? kD / 16 : kD / 8, kTPP = kThreads / kCH, kP = kTT / kTPP;      // loads of a row, rows of a pass, passes
+    static_assert(kNB >= 1 && kP >= 1, "tile");
+    __shared__ __align__(16) u32x4 sh_k[2 * kTT * kPieces];
+    u32x4 *const sh_v = sh_k + kTT * kPieces;
+    __shared__ long long sh_off[kChunk * (kTT / 8)];          // where the pages stand, in elements; -1: not in the cache
+    __shared__ int sh_page[kInt8 ? kChunk * (kTT / 8) : 1];
+    __shared__ __align__(16) float sh_ks[kInt8 ? kTT : 4], sh_vs[kInt8 ? kTT : 4];
+    __shared__ float sh_m[kWaves][32], sh_l[kWaves][32];
+    __shared__ int sh_bad, sh_found, sh_n_loose, sh_loose[kLoose], sh_parents[kMaxNodes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wr = wave % kWR, wt = wave / kWR, col = lane & 31, half = lane >> 5;
+    const int d = a.c.head_dim, shift = a.c.block_shift, mask = (1 << shift) - 1;
+    const bool tree = a.parents != nullptr;
+
+    Span<kTT> w;
+    if (!w.find(a, blockIdx.x, blockIdx.y, plan.row_tiles, kR)) return;
+    const int piece = blockIdx.z;
+    const bool whole = w.count <= plan.tiles || plan.pieces == 1;
+    const int j0 = whole ? 0 : piece * plan.tiles, j1 = whole || piece == plan.pieces - 1 ? w.count : min(w.count, j0 + plan.tiles);
+    if (piece > 0 && (whole || j0 >= j1)) return;
+
+    if (tree && tid < w.n) sh_parents[tid] = a.parents[w.first + tid];
+    if (tid == 0) sh_found = sh_n_loose = 0;
+    __syncthreads();
+    const int local0 = (int)(w.row0 - (long long)w.i_lo * a.group);
+    const int n_rows = (int)min((long long)kR, (long long)w.n * a.group - w.row0);
+    Row row;
+    row.find(a, w.kvh, w.n, w.ctx, w.i_lo, local0 + min(wr * 32 + col, n_rows - 1));
+    row.above = tree ? nodes_above(sh_parents, row.i) : 0;
+    // what the wave's rows see, from the first to the last of them
+    const int p_lo = __builtin_amdgcn_readfirstlane(row.p), p_hi = __builtin_amdgcn_readlane(row.p, 31);
+    const _Float16 *const q_row = a.q + (long long)(w.first + row.i) * a.ldq + (long long)row.head * d;
+
+    // queries: the right operand of the first product; a negative scale turns their signs, one of 0 makes them 0
+    f16x8 q[kD / 16];
+#pragma unroll
+    for (int x = 0; x < kD / 16; ++x) {
+        const int e = 16 * x + 8 * half;
+        q[x] = f16x8{};
+        if (e < d) q[x] = *(const f16x8 *)(q_row + e);
+        if (a.scale < 0.0f) q[x] = -q[x];
+        if (a.scale == 0.0f) q[x] = q[x] * (_Float16)0.0f;
+    }
+    const float c = a.scale == 0.0f ? 1.0f : fminf(fabsf(a.scale) * 1.44269504088896f, 3.0e38f);
+
+    float m = kFloor, l = 0.0f, cap = 0.0f, cap_inv = 0.0f;
+    f32x16 o[kD / 32] = {};
+
+    // what a thread loads of a tile: of rows kTPP apart the same 16 bytes, of keys and of values
+    const int lane_row = tid / kCH, piece_of = tid % kCH;
+    const bool live = piece_of * (kInt8 ? 16 : 8) < d;
+    const long long lane_at = (long long)(lane_row & mask) * a.c.ld_token + piece_of * (kInt8 ? 16 : 8);
+    const int e_shift = max(0, __builtin_ctz(kTT) - shift);         // pages of a tile: 1 << e_shift
+    u32x4 k[kP], v[kP];
+    float scale_k = 0.0f, scale_v = 0.0f;
+    uint32_t gone = 0;               // passes whose row is not there
+    bool bad = false;
+    int jc = j0;
+
+    auto load = [&](int j) {
+        const int t0 = w.tile_of(j) * kTT, slot = (j - jc) << e_shift;
+        const bool masked = bad || t0 + kTT > w.t1;
+        gone = 0;
+#pragma unroll
+        for (int x = 0; x < kP; ++x) {
+            const int in = x * kTPP + lane_row;
+            long long at = sh_off[slot + (e_shift ? in >> shift : 0)];
+            if (masked && (at < 0 || t0 + in >= w.t1)) {
+                gone |= 1u << x;
+                at = 0;
+            } else {
+                at += lane_at + (long long)((t0 + x * kTPP) & mask) * a.c.ld_token;
+            }
+            k[x] = v[x] = u32x4{};
+            if (live && !(gone >> x & 1)) {
+                k[x] = *(const u32x4 *)(a.c.k + at * (kInt8 ? 1 : 2));
+                v[x] = *(const u32x4 *)(a.c.v + at * (kInt8 ? 1 : 2));
+            }
+        }
+        if (kInt8 && tid < kTT) {
+            const int page = sh_page[slot + (e_shift ? tid >> shift : 0)];
+            scale_k = scale_v = 0.0f;
+            if (page >= 0 && t0 + tid < w.t1) {
+                const long long at = (((long long)page * a.c.n_kv_heads + w.kvh) << shift) + ((t0 + tid) & mask);
+                scale_k = a.c.k_scale[at];
+                scale_v = a.c.v_scale[at];
+            }
+        }
+    };
+    // the tile that is on its way to LDS, without infinite and NaN values
+    auto store = [&]() {
+        bool found = false;
+#pragma unroll
+        for (int x = 0; x < kP; ++x) {
+            const int r = x * kTPP + lane_row, turn_k = r & 7, turn_v = (r & 3) << 1;
+            if constexpr (kInt8) {
+                u32x4 lo, hi;
+                uint32_t y[8];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) codes_to_half(k[x][z], y[2 * z], y[2 * z + 1]);
+                lo = u32x4{y[0], y[1], y[2], y[3]}, hi = u32x4{y[4], y[5], y[6], y[7]};
+                sh_k[r * kPieces + ((2 * piece_of) ^ turn_k)] = lo;
+                sh_k[r * kPieces + ((2 * piece_of + 1) ^ turn_k)] = hi;
+#pragma unroll
+                for (int z = 0; z < 4; ++z) codes_to_half(v[x][z], y[2 * z], y[2 * z + 1]);
+                lo = u32x4{y[0], y[1], y[2], y[3]}, hi = u32x4{y[4], y[5], y[6], y[7]};
+                sh_v[r * kPieces + ((2 * piece_of) ^ turn_v)] = lo;
+                sh_v[r * kPieces + ((2 * piece_of + 1) ^ turn_v)] = hi;
+            } else {
+                uint32_t some = 0;
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    const f16x2 y = __builtin_bit_cast(f16x2, v[x][z]);
+                    some |= __builtin_bit_cast(uint32_t, y - y);          // 0, or NaN
+                }
+                if (some & 0x7fff7fffu) {
+                    found = true;
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        if ((v[x][z] & 0x7c00u) == 0x7c00u) v[x][z] &= 0xffff0000u;
+                        if ((v[x][z] & 0x7c000000u) == 0x7c000000u) v[x][z] &= 0xffffu;
+                    }
+                }
+                sh_k[r * kPieces + (piece_of ^ turn_k)] = k[x];
+                sh_v[r * kPieces + (piece_of ^ turn_v)] = v[x];
+            }
+        }
+        if (kInt8 && tid < kTT) {
+            if (!(scale_v - scale_v == 0.0f)) found = true, scale_v = 0.0f;
+            sh_ks[tid] = scale_k * c;
+            sh_vs[tid] = scale_v;
+        }
+        if (__any(found)) sh_found = 1;
+    };
+
+    auto compute = [&](int j) {
+        const int t0 = w.tile_of(j) * kTT + wt * (32 * kNB), slot = (j - jc) << e_shift;
+        // nothing, or all of it, to be seen by the wave's rows
+        const int t9 = t0 + 32 * kNB - 1;
+        if (t0 >= w.t1 || wr * 32 >= n_rows) return;
+        bool all = t9 < w.t1 && !bad;
+        if (tree) {
+            all = all && t9 < w.ctx;
+        } else {
+            if (t0 > p_hi || (a.window && (long long)t9 <= (long long)p_lo - a.window && t0 >= a.sinks)) return;
+            all = all && t9 <= p_lo && (!a.window || (long long)t0 > (long long)p_hi - a.window || t9 < a.sinks);
+        }
+        f32x16 acc[kNB] = {};
+#pragma unroll
+        for (int x = 0; x < kD / 16; ++x)
+#pragma unroll
+            for (int b = 0; b < kNB; ++b) {
+                const int r = (wt * kNB + b) * 32 + col;
+                const f16x8 y = __builtin_bit_cast(f16x8, sh_k[r * kPieces + ((2 * x + half) ^ (r & 7))]);
+                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(y, q[x], acc[b], 0, 0, 0);
+            }
+        if constexpr (kInt8) {
+#pragma unroll
+            for (int b = 0; b < kNB; ++b)
+#pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const int e = lane + 64 * x;
-                    if (e >= d) break;
-                    const float v = kInt8 ? (float)((const int8_t *)a.c.v)[sh_row[j] + e] : (float)((const _Float16 *)a.c.v)[sh_row[j] + e];
-                    if (v - v == 0.0f && sh_p[j] - sh_p[j] == 0.0f)
-                        o[x] += sh_p[j] * v;
-                    else                    // weights are never quite 0
-                        loose[x] += sh_scale[j] ? (kInt8 ? sh_p[j] * v : v) : 0.0f * v;
+                    const f32x4 y = *(const f32x4 *)(sh_ks + (wt * kNB + b) * 32 + 8 * x + 4 * half);
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) acc[b][4 * x + z] *= y[z];
+                }
+        }
+        if (!all) {
+#pragma unroll
+            for (int b = 0; b < kNB; ++b)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    const int in = 32 * b + 8 * (x >> 2) + 4 * half + (x & 3), t = t0 + in;
+                    bool there = t < w.t1 && row.sees(tree, t);
+                    if (bad && there) there = sh_off[slot + (e_shift ? (wt * 32 * kNB + in) >> shift : 0)] >= 0;
+                    if (!there) acc[b][x] = kFloor;
+                }
+        }
+        float top = kFloor;
+#pragma unroll
+        for (int b = 0; b < kNB; ++b)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) top = fmaxf(top, acc[b][x]);
+        if (!kInt8) top *= c;
+        if (__any(top > m + 7.0f)) {                    // rare after the first tiles: a new maximum for the row
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float to = fmaxf(m, top), keep = weight_of(m, l, to);
+            m = to;
+            l *= keep;
+#pragma unroll
+            for (int x = 0; x < kD / 32; ++x) o[x] *= keep;
+        }
+        const float off = m == kFloor ? 0.0f : 8.0f - m;
+        float sum = 0.0f;
+#pragma unroll
+        for (int b = 0; b < kNB; ++b)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                acc[b][x] = exp2_(kInt8 ? acc[b][x] + off : __builtin_fmaf(acc[b][x], c, off));
+                sum += acc[b][x];
+            }
+        l += sum;
+        if constexpr (kInt8) {
+            float most = 0.0f;
+            f32x4 vs[kNB][4];
+#pragma unroll
+            for (int b = 0; b < kNB; ++b)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    vs[b][x] = *(const f32x4 *)(sh_vs + (wt * kNB + b) * 32 + 8 * x + 4 * half);
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) most = fmaxf(most, fabsf(vs[b][x][z]));
+                }
+            if (__any(most > cap)) {                    // scales of values over a power of two
+                most = fmaxf(most, __shfl_xor(most, 32, 64));
+                const uint32_t ex = min(__float_as_uint(most) >> 23, 252u) + 1;
+                const float was = cap;
+                cap = fmaxf(cap, __uint_as_float(ex << 23));
+                cap_inv = __uint_as_float((254u - (__float_as_uint(cap) >> 23)) << 23);
+                const float keep = was * cap_inv;
+#pragma unroll
+                for (int x = 0; x < kD / 32; ++x) o[x] *= keep;
+            }
+#pragma unroll
+            for (int b = 0; b < kNB; ++b)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) acc[b][x] *= vs[b][x >> 2][x & 3] * cap_inv;
+        }
+        // the second product: 16 tokens a step, the lanes' own, in the order of the scores
+#pragma unroll
+        for (int b = 0; b < kNB; ++b)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                u32x4 p;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    p[x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[b][8 * y + 2 * x], acc[b][8 * y + 2 * x + 1]}, f16x2));
+                const f16x8 weights = __builtin_bit_cast(f16x8, p);
+                const int r = (wt * kNB + b) * 32 + 16 * y + 4 * half + ((lane & 15) >> 2);          // and 8 rows on
+#pragma unroll
+                for (int x = 0; x < kD / 32; ++x) {
+                    const int e = 32 * x + (lane & 16) + 4 * (lane & 3), at = r * kPieces + ((e >> 3) ^ ((r & 3) << 1));
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)((char *)&sh_v[at] + (e & 4) * 2));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)((char *)&sh_v[at + 8 * kPieces] + (e & 4) * 2));
+                    typedef short s16x8 __attribute__((ext_vector_type(8)));
+                    const s16x8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, t), weights, o[x], 0, 0, 0);
                 }
             }
+    };
+
+    for (; jc < j1; jc += kChunk) {
+        const int j9 = min(j1, jc + kChunk);
+        __syncthreads();                              // readers of the pages before
+        if (tid == 0) sh_bad = 0;
+        __syncthreads();
+        for (int x = tid; x < (j9 - jc) << e_shift; x += kThreads) {
+            const int t = w.tile_of(jc + (x >> e_shift)) * kTT + ((x & ((1 << e_shift) - 1)) << shift);
+            int page = -1;
+            if (t < w.t1) {
+                page = a.table[(long long)w.s * a.ld_table + (t >> shift)];
+                if (page < 0 || page >= a.c.n_blocks) page = -1, sh_bad = 1;
+            }
+            sh_off[x] = page < 0 ? -1 : page * a.c.ld_block + w.kvh * a.c.ld_head;
+            if (kInt8) sh_page[x] = page;
         }
-        for (int x = 0; x < 4; ++x) {
-            const int e = lane + 64 * x;
-            if (e < d) a.o[(long long)m0 * a.ldo + (long long)h * d + e] = (_Float16)(any ? (o[x] + loose[x]) / l : 0.0f);
+        __syncthreads();
+        bad = sh_bad != 0;
+        load(jc);
+        for (int j = jc; j < j9; ++j) {
+            __syncthreads();                          // readers of the tile before
+            store();
+            __syncthreads();
+            if (tid == 0 && sh_found) {
+                if (sh_n_loose < kLoose) sh_loose[sh_n_loose] = j;
+                ++sh_n_loose;
+                sh_found = 0;
+            }
+            if (j + 1 < j9) load(j + 1);
+            compute(j);
         }
     }
+
+    // The parts of the waves that have the same rows: m and the sum by row, then the values through LDS, lane by lane.
+    l += __shfl_xor(l, 32, 64);
+    if (l == 0.0f && row.p >= 0) {                    // no weights: are there tokens?
+        bool seen = false;
+        for (int j = j0; j < j1 && !seen; ++j) {
+            const int t0 = w.tile_of(j) * kTT + wt * (32 * kNB);
+            for (int t = t0; t < min(t0 + 32 * kNB, w.t1) && !seen; ++t)
+                if (row.sees(tree, t)) {
+                    const int page = a.table[(long long)w.s * a.ld_table + (t >> shift)];
+                    seen = page >= 0 && page < a.c.n_blocks;
+                }
+        }
+        if (seen) l = kNone;
+    }
+    float top = m, total = l;
+    if constexpr (kWT > 1) {
+        if (half == 0) sh_m[wave][col] = m, sh_l[wave][col] = l;
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < kWT; ++x) top = fmaxf(top, sh_m[x * kWR + wr][col]);
+        total = 0.0f;
+#pragma unroll
+        for (int x = 0; x < kWT; ++x) {
+            const float y = sh_m[x * kWR + wr][col], z = sh_l[x * kWR + wr][col];
+            total += weight_of(y, z, top) * z;
+        }
+        const float f = weight_of(m, l, top) * (kInt8 ? cap : 1.0f);
+#pragma unroll
+        for (int x = 0; x < kD / 32; ++x) o[x] *= f;
+        // the upper half of the waves gives, the lower half takes
+        f32x4 *const sh = (f32x4 *)sh_k;
+        static_assert(kD / 32 * 16 * 64 * 4 * (kWaves / 2) <= sizeof(sh_k), "the join fits the tile");
+#pragma unroll
+        for (int give = kWT / 2; give >= 1; give /= 2) {
+            const int to = (wt - give) * kWR + wr, from = wt * kWR + wr;
+#pragma unroll
+            for (int x = 0; x < kD / 8; ++x) {
+                if (wt >= give && wt < 2 * give) {
+                    sh[(to * (kD / 8) + x) * 64 + lane] = f32x4{o[x >> 2][4 * (x & 3)], o[x >> 2][4 * (x & 3) + 1], o[x >> 2][4 * (x & 3) + 2], o[x >> 2][4 * (x & 3) + 3]};
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < kD / 8; ++x) {
+                if (wt < give) {
+                    const f32x4 y = sh[(from * (kD / 8) + x) * 64 + lane];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) o[x >> 2][4 * (x & 3) + z] += y[z];
+                }
+            }
+            if (give > 1) __syncthreads();
+        }
+    } else if constexpr (kInt8) {
+#pragma unroll
+        for (int x = 0; x < kD / 32; ++x) o[x] *= cap;
+    }
+    const long long part = ((((long long)w.s * a.c.n_kv_heads + w.kvh) * plan.row_tiles + blockIdx.x / a.c.n_kv_heads) * plan.pieces + piece) * kR;
+    float *const part_o = whole ? nullptr : plan.o + part * d;
+    if (wt == 0 && wr * 32 + col < n_rows) {
+        const int r = wr * 32 + col;
+        const float inv = factor_of(top, total);
+        _Float16 *const o_row = a.o + (long long)(w.first + row.i) * a.ldo + (long long)row.head * d;
+#pragma unroll
+        for (int x = 0; x < kD / 32; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int e = 32 * x + 8 * y + 4 * half;
+                const f32x4 z = {o[x][4 * y], o[x][4 * y + 1], o[x][4 * y + 2], o[x][4 * y + 3]};
+                if (e >= d) continue;
+                if (whole)
+                    *(f16x4 *)(o_row + e) = __builtin_convertvector(z * inv, f16x4);
+                else
+                    *(f32x4 *)(part_o + (long long)r * d + e) = z;
+            }
+        if (!whole && half == 0) plan.ml[part + r] = make_float2(top, top == kFloor && total > 0.0f ? kNone : total);
+    }
+    __syncthreads();
+    if (sh_n_loose > 0) {
+        __threadfence_block();
+        put_loose<kInt8, kTT>(a, w, kR, j0, j1, sh_loose, sh_n_loose, sh_parents, a.o, part_o);
+    }
+}
+
+// The parts of rows that several workgroups have, joined by weights 2^(m - max m): a workgroup to a tile of rows, a thread four
+// dimensions of a row.
+constexpr int kJoinThreads = 256;
+
+template <int kTT>
+__global__ __launch_bounds__(kJoinThreads) void k_rows_join(RowsArgs a, Plan plan, int rows)
+{
+    Span<kTT> w;
+    if (!w.find(a, blockIdx.x, blockIdx.y, plan.row_tiles, rows) || w.count <= plan.tiles) return;
+    const int d = a.c.head_dim, quads = d / 4, pieces = min(plan.pieces, (w.count + plan.tiles - 1) / plan.tiles);
+    const int local0 = (int)(w.row0 - (long long)w.i_lo * a.group);
+    const int n_rows = (int)min((long long)rows, (long long)w.n * a.group - w.row0);
+    const long long part = (((long long)w.s * a.c.n_kv_heads + w.kvh) * plan.row_tiles + blockIdx.x / a.c.n_kv_heads) * plan.pieces * rows;
+    for (int item = threadIdx.x + kJoinThreads * blockIdx.z; item < n_rows * quads; item += kJoinThreads * gridDim.z) {
+        const int r = item / quads, e = (item - r * quads) * 4;
+        float top = kFloor, total = 0.0f;
+        for (int x = 0; x < pieces; ++x) top = fmaxf(top, plan.ml[part + (long long)x * rows + r].x);
+        f32x4 sum = {};
+        for (int x = 0; x < pieces; ++x) {
+            const long long at = part + (long long)x * rows + r;
+            const float2 ml = plan.ml[at];
+            const float f = weight_of(ml.x, ml.y, top);
+            total += f * ml.y;
+            sum += f * *(const f32x4 *)(plan.o + at * d + e);
+        }
+        const int i = w.i_lo + (local0 + r) / a.group, head = w.kvh * a.group + (local0 + r) % a.group;
+        *(f16x4 *)(a.o + (long long)(w.first + i) * a.ldo + (long long)head * d + e) = __builtin_convertvector(sum * factor_of(top, total), f16x4);
+    }
+}
+
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+// How a call is divided.
+struct Form {
+    int rows, tile;                 // rows of a workgroup, tokens of a tile
+    long long row_tiles, groups;    // of a sequence and head, and of all
+    int pieces, tiles;
+};
+
+constexpr int kFill = 512, kLeast = 4;        // workgroups that fill the chip; tiles of a piece, at least
+
+// Tiles of `tile` tokens that a workgroup's rows see at most, `span` tokens being its own.
+long long tiles_seen(int max_length, int window, int sinks, long long span, int tile)
+{
+    const long long all = ((long long)max_length + tile - 1) / tile;
+    return window ? std::min(all, ((long long)window + sinks + span + tile - 1) / tile + 4) : all;
+}
+
+Form form_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length, int window, int sinks, bool tree)
+{
+    Form f;
+    const int group = n_heads / n_kv_heads;
+    const long long most = (long long)max_new * group, all = (long long)S * n_kv_heads;
+    // the widest tile of rows that the rows fill, and that fills the chip; of a tree's keys and values each is read once
+    f.rows = 32;
+    for (int r : {128, 64})
+        if (most > r / 2 && (tree || all * ((most + r - 1) / r) >= kFill)) {
+            f.rows = r;
+            break;
+        }
+    if (head_dim > 128) f.rows = 128;
+    f.tile = head_dim > 128 ? 32 : f.rows == 32 && head_dim <= 64 ? 128 : 64;
+    f.row_tiles = (most + f.rows - 1) / f.rows;
+    f.groups = all * f.row_tiles;
+    const long long tiles = tiles_seen(max_length, window, sinks, std::min((long long)max_new, (long long)f.rows / group + 2), f.tile);
+    f.pieces = 1;
+    f.tiles = (int)tiles;
+    if (f.groups < kFill && tiles >= 2 * kLeast) {
+        const long long want = std::min((kFill + f.groups - 1) / f.groups, tiles / kLeast);
+        f.tiles = (int)((tiles + want - 1) / want);
+        f.pieces = (int)((tiles + f.tiles - 1) / f.tiles);
+    }
+    return f;
+}
+
+size_t bytes_of(size_t parts, int head_dim) { return up256(parts * head_dim * 4) + up256(parts * 8); }
+
+template <int kD, bool kInt8>
+hipError_t launch_d(const RowsArgs &a, const Plan &plan, const Form &f, hipStream_t s)
+{
+    const dim3 grid((unsigned)(f.row_tiles * a.c.n_kv_heads), a.S, f.pieces);
+    hipError_t e;
+    if constexpr (kD == 256) {
+        e = launch_kernel(k_rows<kD, kInt8, 4, 4, 32>, grid, dim3(256), 0, s, a, plan);
+    } else {
+        if (f.rows == 128)
+            e = launch_kernel(k_rows<kD, kInt8, 4, 4, 64>, grid, dim3(256), 0, s, a, plan);
+        else if (f.rows == 64)
+            e = launch_kernel(k_rows<kD, kInt8, 4, 2, 64>, grid, dim3(256), 0, s, a, plan);
+        else if constexpr (kD == 64)
+            e = launch_kernel(k_rows<kD, kInt8, 4, 1, 128>, grid, dim3(256), 0, s, a, plan);
+        else
+            e = launch_kernel(k_rows<kD, kInt8, 2, 1, 64>, grid, dim3(128), 0, s, a, plan);
+    }
+    if (e != hipSuccess || f.pieces == 1) return e;
+    const dim3 join((unsigned)(f.row_tiles * a.c.n_kv_heads), a.S, std::max(1, std::min(f.rows * a.c.head_dim / 4 / kJoinThreads, 8)));
+    if (f.tile == 32) return launch_kernel(k_rows_join<32>, join, dim3(kJoinThreads), 0, s, a, plan, f.rows);
+    if (f.tile == 64) return launch_kernel(k_rows_join<64>, join, dim3(kJoinThreads), 0, s, a, plan, f.rows);
+    return launch_kernel(k_rows_join<128>, join, dim3(kJoinThreads), 0, s, a, plan, f.rows);
 }
 
 }  // namespace
 
-size_t rows_workspace_need(int, int, int, int, int, int, int, int, bool) { return 0; }
-size_t rows_workspace_bytes(int, int, int, int, int, int, int, int, bool) { return 0; }
+size_t rows_workspace_need(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length, int window, int sinks, bool tree)
+{
+    const Form f = form_of(S, n_heads, n_kv_heads, head_dim, max_new, max_length, window, sinks, tree);
+    return f.pieces > 1 ? bytes_of((size_t)f.groups * f.pieces * f.rows, head_dim) : 0;
+}
+
+// Enough for every smaller call: where a call is cut, all its workgroups are fewer than 2 kFill.
+size_t rows_workspace_bytes(int, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length, int window, int sinks, bool)
+{
+    const long long most = (long long)max_new * (n_heads / n_kv_heads);
+    const int rows = head_dim > 128 || most > 64 ? 128 : most > 32 ? 64 : 32;
+    if (tiles_seen(max_length, window, sinks, std::min(max_new, 130), head_dim > 128 ? 32 : 64) < 2 * kLeast) return 0;
+    return bytes_of((size_t)2 * kFill * rows, head_dim);
+}
 
 hipError_t rows_prepare()
 {
     hipFuncAttributes at;
-    return hipFuncGetAttributes(&at, (const void *)k_rows<false>);
+    return hipFuncGetAttributes(&at, (const void *)k_rows<64, false, 4, 1, 128>);
 }
 
 hipError_t launch_rows(const RowsArgs &a, bool int8, hipStream_t s)
 {
-    const dim3 grid(std::min(a.max_new, a.M), a.S);
-    return int8 ? launch_kernel(k_rows<true>, grid, dim3(64), 0, s, a) : launch_kernel(k_rows<false>, grid, dim3(64), 0, s, a);
+    const int d = a.c.head_dim;
+    const Form f = form_of(a.S, a.n_heads, a.c.n_kv_heads, d, a.max_new, a.max_length, a.window, a.sinks, a.parents != nullptr);
+    if (f.row_tiles * a.c.n_kv_heads > 1 << 23) return hipErrorInvalidValue;
+    Plan plan{(int)f.row_tiles, f.pieces, f.tiles, nullptr, nullptr};
+    if (f.pieces > 1) {
+        const size_t parts = (size_t)f.groups * f.pieces * f.rows;
+        plan.o = (float *)a.workspace;
+        plan.ml = (float2 *)((char *)a.workspace + up256(parts * d * 4));
+    }
+    if (d <= 64) return int8 ? launch_d<64, true>(a, plan, f, s) : launch_d<64, false>(a, plan, f, s);
+    if (d <= 128) return int8 ? launch_d<128, true>(a, plan, f, s) : launch_d<128, false>(a, plan, f, s);
+    return int8 ? launch_d<256, true>(a, plan, f, s) : launch_d<256, false>(a, plan, f, s);
 }
 
 }  // namespace muxq
