@@ -10,7 +10,7 @@
 // 32 x 32 x 16 steps with the tokens, or the dimensions, as rows of the left operand and 32 rows of the problem as the columns of the right one: scores
 // come out with a row per lane column, which is where the weights of the second product have to stand, so that they never leave their
 // lanes.  The second product's left operand is the transposed values, which LDS turns while it reads (16 lanes, 4 tokens of 16 dimensions).
-// 16-byte pieces of a token's row are permuted by its number, so that neither kind of read meets the same banks twice.
+// Rows in LDS are 16 bytes longer for keys and 32 for values, so that neither kind of read meets the same banks twice.
 //
 // Weights are 2^(s - m + 8), rounded to fp16, and m follows the maximum only when a score is 7 above it, which is rare: up to
 // 2^15, so that small ones keep their bits.  The scale of a key goes to its score, the scale of a value to its
@@ -114,6 +114,21 @@ struct Row {
         window = a.window ? a.window : 0x80000000u;
         sinks = min(a.sinks, p + 1);
     }
+    // which of the tokens t0..t0 + 31 it sees, a bit to each
+    __device__ __forceinline__ uint32_t sees32(bool tree, int t0, int t1) const
+    {
+        uint32_t word;
+        if (tree) {
+            const int x = t0 - ctx;                   // the node of the first one
+            word = below(-x);
+            if (x > -32 && x < 64) word |= (uint32_t)(x < 0 ? above << -x : above >> x);
+        } else {
+            word = below(p + 1 - t0) & ~below((int)max((long long)p - window + 1 - t0, -1ll)) | below(sinks - t0);
+        }
+        return word & below(t1 - t0);
+    }
+    // the n lowest bits
+    static __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
     __device__ __forceinline__ bool sees(bool tree, int t) const
     {
         if (!tree) return (uint32_t)(p - t) < window || t < sinks;
@@ -188,17 +203,17 @@ template <int kD, bool kInt8, int kWaves, int kWR, int kTT>
 __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void k_rows(RowsArgs a, Plan plan)
 {
     constexpr int kThreads = 64 * kWaves, kWT = kWaves / kWR, kR = 32 * kWR, kNB = kTT / kWT / 32;          // waves along tokens; rows; blocks of 32 tokens of a wave
-    constexpr int kPieces = kD / 8;                                                 // 16-byte pieces of a row in LDS
+    constexpr int kKeyRow = 2 * kD + 16, kValueRow = 2 * kD + 32;                   // bytes of a row in LDS
     constexpr int kCH = kInt8 ? kD / 16 : kD / 8, kTPP = kThreads / kCH, kP = kTT / kTPP;      // loads of a row, rows of a pass, passes
     static_assert(kNB >= 1 && kP >= 1, "tile");
-    __shared__ __align__(16) u32x4 sh_k[2 * kTT * kPieces];
-    u32x4 *const sh_v = sh_k + kTT * kPieces;
+    __shared__ __align__(16) char sh_k[kTT * (kKeyRow + kValueRow)];
+    char *const sh_v = sh_k + kTT * kKeyRow;
     __shared__ long long sh_off[kChunk * (kTT / 8)];          // where the pages stand, in elements; -1: not in the cache
     __shared__ int sh_page[kInt8 ? kChunk * (kTT / 8) : 1];
     __shared__ __align__(16) float sh_ks[kInt8 ? kTT : 4], sh_vs[kInt8 ? kTT : 4];
     __shared__ float sh_m[kWaves][32], sh_l[kWaves][32];
     __shared__ int sh_bad, sh_found, sh_n_loose, sh_loose[kLoose], sh_parents[kMaxNodes];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wr = wave % kWR, wt = wave / kWR, col = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave % kWR, wt = wave / kWR, col = lane & 31, half = lane >> 5;
     const int d = a.c.head_dim, shift = a.c.block_shift, mask = (1 << shift) - 1;
     const bool tree = a.parents != nullptr;
 
@@ -233,8 +248,9 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     }
     const float c = a.scale == 0.0f ? 1.0f : fminf(fabsf(a.scale) * 1.44269504088896f, 3.0e38f);
 
-    float m = kFloor, l = 0.0f, cap = 0.0f, cap_inv = 0.0f;
-    f32x16 o[kD / 32] = {};
+    float m, l, cap, cap_inv;
+    f32x16 o[kD / 32];
+    bool careful = false;
 
     // what a thread loads of a tile: of rows kTPP apart the same 16 bytes, of keys and of values
     const int lane_row = tid / kCH, piece_of = tid % kCH;
@@ -277,50 +293,41 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
             }
         }
     };
-    // the tile that is on its way to LDS, without infinite and NaN values
+    // the tile that is on its way to LDS; where care is taken without its infinite and NaN values
     auto store = [&]() {
         bool found = false;
 #pragma unroll
         for (int x = 0; x < kP; ++x) {
-            const int r = x * kTPP + lane_row, turn_k = r & 7, turn_v = (r & 3) << 1;
+            u32x4 *const to_k = (u32x4 *)(sh_k + (x * kTPP + lane_row) * kKeyRow + piece_of * (kInt8 ? 32 : 16));
+            u32x4 *const to_v = (u32x4 *)(sh_v + (x * kTPP + lane_row) * kValueRow + piece_of * (kInt8 ? 32 : 16));
             if constexpr (kInt8) {
-                u32x4 lo, hi;
                 uint32_t y[8];
 #pragma unroll
                 for (int z = 0; z < 4; ++z) codes_to_half(k[x][z], y[2 * z], y[2 * z + 1]);
-                lo = u32x4{y[0], y[1], y[2], y[3]}, hi = u32x4{y[4], y[5], y[6], y[7]};
-                sh_k[r * kPieces + ((2 * piece_of) ^ turn_k)] = lo;
-                sh_k[r * kPieces + ((2 * piece_of + 1) ^ turn_k)] = hi;
+                to_k[0] = u32x4{y[0], y[1], y[2], y[3]}, to_k[1] = u32x4{y[4], y[5], y[6], y[7]};
 #pragma unroll
                 for (int z = 0; z < 4; ++z) codes_to_half(v[x][z], y[2 * z], y[2 * z + 1]);
-                lo = u32x4{y[0], y[1], y[2], y[3]}, hi = u32x4{y[4], y[5], y[6], y[7]};
-                sh_v[r * kPieces + ((2 * piece_of) ^ turn_v)] = lo;
-                sh_v[r * kPieces + ((2 * piece_of + 1) ^ turn_v)] = hi;
+                to_v[0] = u32x4{y[0], y[1], y[2], y[3]}, to_v[1] = u32x4{y[4], y[5], y[6], y[7]};
             } else {
-                uint32_t some = 0;
-#pragma unroll
-                for (int z = 0; z < 4; ++z) {
-                    const f16x2 y = __builtin_bit_cast(f16x2, v[x][z]);
-                    some |= __builtin_bit_cast(uint32_t, y - y);          // 0, or NaN
-                }
-                if (some & 0x7fff7fffu) {
-                    found = true;
+                if (careful) {
 #pragma unroll
                     for (int z = 0; z < 4; ++z) {
-                        if ((v[x][z] & 0x7c00u) == 0x7c00u) v[x][z] &= 0xffff0000u;
-                        if ((v[x][z] & 0x7c000000u) == 0x7c000000u) v[x][z] &= 0xffffu;
+                        const uint32_t was = v[x][z];
+                        if ((was & 0x7c00u) == 0x7c00u) v[x][z] &= 0xffff0000u;
+                        if ((was & 0x7c000000u) == 0x7c000000u) v[x][z] &= 0xffffu;
+                        found |= v[x][z] != was;
                     }
                 }
-                sh_k[r * kPieces + (piece_of ^ turn_k)] = k[x];
-                sh_v[r * kPieces + (piece_of ^ turn_v)] = v[x];
+                *to_k = k[x];
+                *to_v = v[x];
             }
         }
         if (kInt8 && tid < kTT) {
-            if (!(scale_v - scale_v == 0.0f)) found = true, scale_v = 0.0f;
+            if (careful && !(scale_v - scale_v == 0.0f)) found = true, scale_v = 0.0f;
             sh_ks[tid] = scale_k * c;
             sh_vs[tid] = scale_v;
         }
-        if (__any(found)) sh_found = 1;
+        if (careful && __any(found)) sh_found = 1;
     };
 
     auto compute = [&](int j) {
@@ -336,14 +343,31 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
             all = all && t9 <= p_lo && (!a.window || (long long)t0 > (long long)p_hi - a.window || t9 < a.sinks);
         }
         f32x16 acc[kNB] = {};
+        const char *const keys = sh_k + (wt * kNB * 32 + col) * kKeyRow + half * 16;
+        const char *const values = sh_v + (wt * kNB * 32 + 4 * half + ((lane & 15) >> 2)) * kValueRow + ((lane & 16) + 4 * (lane & 3)) * 2;
+        // (In the compiler's own order each matrix instruction waits for the read in front of it: the barriers keep the next four reads
+        // in front of four of them, and below the exponentials of a step behind the products of the one before.)
+        constexpr int kAhead = 4, kSteps = kD / 16 * kNB / kAhead;
+        f16x8 y[2][kAhead];
+        auto ask_keys = [&](int g) {
 #pragma unroll
-        for (int x = 0; x < kD / 16; ++x)
-#pragma unroll
-            for (int b = 0; b < kNB; ++b) {
-                const int r = (wt * kNB + b) * 32 + col;
-                const f16x8 y = __builtin_bit_cast(f16x8, sh_k[r * kPieces + ((2 * x + half) ^ (r & 7))]);
-                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(y, q[x], acc[b], 0, 0, 0);
+            for (int x = 0; x < kAhead; ++x) {
+                const int at = g * kAhead + x;
+                y[g & 1][x] = *(const f16x8 *)(keys + at % kNB * 32 * kKeyRow + at / kNB * 32);
             }
+        };
+        ask_keys(0);
+#pragma unroll
+        for (int g = 0; g < kSteps; ++g) {
+            if (g + 1 < kSteps) ask_keys(g + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < kAhead; ++x) {
+                const int at = g * kAhead + x;
+                acc[at % kNB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(y[g & 1][x], q[at / kNB], acc[at % kNB], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
         if constexpr (kInt8) {
 #pragma unroll
             for (int b = 0; b < kNB; ++b)
@@ -356,14 +380,17 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
         }
         if (!all) {
 #pragma unroll
-            for (int b = 0; b < kNB; ++b)
+            for (int b = 0; b < kNB; ++b) {
+                uint32_t word = row.sees32(tree, t0 + 32 * b, w.t1);
+                if (bad)                              // pages are 8 tokens at least
 #pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    const int in = 32 * b + 8 * (x >> 2) + 4 * half + (x & 3), t = t0 + in;
-                    bool there = t < w.t1 && row.sees(tree, t);
-                    if (bad && there) there = sh_off[slot + (e_shift ? (wt * 32 * kNB + in) >> shift : 0)] >= 0;
-                    if (!there) acc[b][x] = kFloor;
-                }
+                    for (int x = 0; x < 4; ++x)
+                        if (sh_off[slot + (e_shift ? (wt * 32 * kNB + 32 * b + 8 * x) >> shift : 0)] < 0) word &= ~(255u << 8 * x);
+                word >>= 4 * half;
+#pragma unroll
+                for (int x = 0; x < 16; ++x)
+                    if (!(word >> (8 * (x >> 2) + (x & 3)) & 1)) acc[b][x] = kFloor;
+            }
         }
         float top = kFloor;
 #pragma unroll
@@ -380,18 +407,9 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
             for (int x = 0; x < kD / 32; ++x) o[x] *= keep;
         }
         const float off = m == kFloor ? 0.0f : 8.0f - m;
-        float sum = 0.0f;
-#pragma unroll
-        for (int b = 0; b < kNB; ++b)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                acc[b][x] = exp2_(kInt8 ? acc[b][x] + off : __builtin_fmaf(acc[b][x], c, off));
-                sum += acc[b][x];
-            }
-        l += sum;
+        f32x4 vs[kInt8 ? kNB : 1][4];
         if constexpr (kInt8) {
             float most = 0.0f;
-            f32x4 vs[kNB][4];
 #pragma unroll
             for (int b = 0; b < kNB; ++b)
 #pragma unroll
@@ -410,64 +428,97 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
 #pragma unroll
                 for (int x = 0; x < kD / 32; ++x) o[x] *= keep;
             }
-#pragma unroll
-            for (int b = 0; b < kNB; ++b)
-#pragma unroll
-                for (int x = 0; x < 16; ++x) acc[b][x] *= vs[b][x >> 2][x & 3] * cap_inv;
         }
         // the second product: 16 tokens a step, the lanes' own, in the order of the scores
+        u32x4 weights[2];
+        f32x4 sums = {};
+        auto weigh = [&](int step) {
+            const int b = step >> 1;
+            float p[8];
 #pragma unroll
-        for (int b = 0; b < kNB; ++b)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                u32x4 p;
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    p[x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{acc[b][8 * y + 2 * x], acc[b][8 * y + 2 * x + 1]}, f16x2));
-                const f16x8 weights = __builtin_bit_cast(f16x8, p);
-                const int r = (wt * kNB + b) * 32 + 16 * y + 4 * half + ((lane & 15) >> 2);          // and 8 rows on
-#pragma unroll
-                for (int x = 0; x < kD / 32; ++x) {
-                    const int e = 32 * x + (lane & 16) + 4 * (lane & 3), at = r * kPieces + ((e >> 3) ^ ((r & 3) << 1));
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)((char *)&sh_v[at] + (e & 4) * 2));
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)((char *)&sh_v[at + 8 * kPieces] + (e & 4) * 2));
-                    typedef short s16x8 __attribute__((ext_vector_type(8)));
-                    const s16x8 t = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, t), weights, o[x], 0, 0, 0);
-                }
+            for (int x = 0; x < 8; ++x) {
+                const int at = 8 * (step & 1) + x;
+                p[x] = exp2_(kInt8 ? acc[b][at] + off : __builtin_fmaf(acc[b][at], c, off));
+                sums[x & 3] += p[x];
+                if constexpr (kInt8) p[x] *= vs[b][at >> 2][at & 3] * cap_inv;
             }
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                weights[step & 1][x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[2 * x], p[2 * x + 1]}, f16x2));
+        };
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        s16x8 t[2][kD / 32];
+        auto ask_values = [&](int step) {
+            // rows 4 half + 0..3 of the step's tokens, and 8 rows on
+            const char *const at = values + step * 16 * kValueRow;
+#pragma unroll
+            for (int x = 0; x < kD / 32; ++x) {
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(at + 64 * x));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(at + 64 * x + 8 * kValueRow));
+                t[step & 1][x] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+        };
+        ask_values(0);
+        weigh(0);
+#pragma unroll
+        for (int step = 0; step < 2 * kNB; ++step) {
+            if (step + 1 < 2 * kNB) ask_values(step + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < kD / 32; ++x)
+                o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, t[step & 1][x]), __builtin_bit_cast(f16x8, weights[step & 1]),
+                                                              o[x], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (step + 1 < 2 * kNB) weigh(step + 1);
+        }
+        l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
     };
 
-    for (; jc < j1; jc += kChunk) {
-        const int j9 = min(j1, jc + kChunk);
-        __syncthreads();                              // readers of the pages before
-        if (tid == 0) sh_bad = 0;
-        __syncthreads();
-        for (int x = tid; x < (j9 - jc) << e_shift; x += kThreads) {
-            const int t = w.tile_of(jc + (x >> e_shift)) * kTT + ((x & ((1 << e_shift) - 1)) << shift);
-            int page = -1;
-            if (t < w.t1) {
-                page = a.table[(long long)w.s * a.ld_table + (t >> shift)];
-                if (page < 0 || page >= a.c.n_blocks) page = -1, sh_bad = 1;
-            }
-            sh_off[x] = page < 0 ? -1 : page * a.c.ld_block + w.kvh * a.c.ld_head;
-            if (kInt8) sh_page[x] = page;
-        }
-        __syncthreads();
-        bad = sh_bad != 0;
-        load(jc);
-        for (int j = jc; j < j9; ++j) {
-            __syncthreads();                          // readers of the tile before
-            store();
+    // An infinite or NaN value makes all rows of a tile NaN, also those that do not see it (0 times infinity): where a sum is, the
+    // workgroup begins again, takes such values out and remembers where they are.
+    for (;;) {
+        m = kFloor, l = cap = cap_inv = 0.0f;
+#pragma unroll
+        for (int x = 0; x < kD / 32; ++x) o[x] = f32x16{};
+        for (jc = j0; jc < j1; jc += kChunk) {
+            const int j9 = min(j1, jc + kChunk);
+            __syncthreads();                              // readers of the pages before
+            if (tid == 0) sh_bad = 0;
             __syncthreads();
-            if (tid == 0 && sh_found) {
-                if (sh_n_loose < kLoose) sh_loose[sh_n_loose] = j;
-                ++sh_n_loose;
-                sh_found = 0;
+            for (int x = tid; x < (j9 - jc) << e_shift; x += kThreads) {
+                const int t = w.tile_of(jc + (x >> e_shift)) * kTT + ((x & ((1 << e_shift) - 1)) << shift);
+                int page = -1;
+                if (t < w.t1) {
+                    page = a.table[(long long)w.s * a.ld_table + (t >> shift)];
+                    if (page < 0 || page >= a.c.n_blocks) page = -1, sh_bad = 1;
+                }
+                sh_off[x] = page < 0 ? -1 : page * a.c.ld_block + w.kvh * a.c.ld_head;
+                if (kInt8) sh_page[x] = page;
             }
-            if (j + 1 < j9) load(j + 1);
-            compute(j);
+            __syncthreads();
+            bad = sh_bad != 0;
+            load(jc);
+            for (int j = jc; j < j9; ++j) {
+                __syncthreads();                          // readers of the tile before
+                store();
+                __syncthreads();
+                if (careful && tid == 0 && sh_found) {
+                    if (sh_n_loose < kLoose) sh_loose[sh_n_loose] = j;
+                    ++sh_n_loose;
+                    sh_found = 0;
+                }
+                if (j + 1 < j9) load(j + 1);
+                compute(j);
+            }
         }
+        if (careful) break;
+        float sum = 0.0f;
+#pragma unroll
+        for (int x = 0; x < kD / 32; ++x)
+#pragma unroll
+            for (int y = 0; y < 16; ++y) sum += fabsf(o[x][y]);
+        careful = __syncthreads_or(!(sum <= 3.4e38f));
+        if (!careful) break;
     }
 
     // The parts of the waves that have the same rows: m and the sum by row, then the values through LDS, lane by lane.
