@@ -208,8 +208,8 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     static_assert(kNB >= 1 && kP >= 1, "tile");
     __shared__ __align__(16) char sh_k[kTT * (kKeyRow + kValueRow)];
     char *const sh_v = sh_k + kTT * kKeyRow;
-    __shared__ long long sh_off[kChunk * (kTT / 8)];          // where the pages stand, in elements; -1: not in the cache
-    __shared__ int sh_page[kInt8 ? kChunk * (kTT / 8) : 1];
+    __shared__ long long sh_at[kChunk * (kTT / 8)];           // where runs of rows stand, in bytes; 0 for those that are nowhere
+    __shared__ int sh_page[kChunk * (kTT / 8)];               // their pages; -1: not in the cache, or behind all tokens
     __shared__ __align__(16) float sh_ks[kInt8 ? kTT : 4], sh_vs[kInt8 ? kTT : 4];
     __shared__ float sh_m[kWaves][32], sh_l[kWaves][32];
     __shared__ int sh_bad, sh_found, sh_n_loose, sh_loose[kLoose], sh_parents[kMaxNodes];
@@ -255,47 +255,53 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     // what a thread loads of a tile: of rows kTPP apart the same 16 bytes, of keys and of values
     const int lane_row = tid / kCH, piece_of = tid % kCH;
     const bool live = piece_of * (kInt8 ? 16 : 8) < d;
-    const long long lane_at = (long long)(lane_row & mask) * a.c.ld_token + piece_of * (kInt8 ? 16 : 8);
-    const int e_shift = max(0, __builtin_ctz(kTT) - shift);         // pages of a tile: 1 << e_shift
+    // (rows of a run stand in one page and belong to one pass)
+    const int run_shift = min(shift, __builtin_ctz(kTPP)), e_shift = __builtin_ctz(kTT) - run_shift;      // runs of a tile: 1 << e_shift
+    const long long lane_at = ((long long)(lane_row & ((1 << run_shift) - 1)) * a.c.ld_token + (live ? piece_of : 0) * (kInt8 ? 16 : 8)) * (kInt8 ? 1 : 2);
     u32x4 k[kP], v[kP];
     float scale_k = 0.0f, scale_v = 0.0f;
-    uint32_t gone = 0;               // passes whose row is not there
-    bool bad = false;
-    int jc = j0;
+    bool bad = false, edge = false;
+    int jc = j0, t_next = 0, slot_next = 0;
 
+    // Every lane loads, from the first page where its row is nowhere: such rows become zeros in store().
     auto load = [&](int j) {
-        const int t0 = w.tile_of(j) * kTT, slot = (j - jc) << e_shift;
-        const bool masked = bad || t0 + kTT > w.t1;
-        gone = 0;
+        t_next = w.tile_of(j) * kTT, slot_next = (j - jc) << e_shift;
+        edge = bad || t_next + kTT > w.t1;
 #pragma unroll
         for (int x = 0; x < kP; ++x) {
-            const int in = x * kTPP + lane_row;
-            long long at = sh_off[slot + (e_shift ? in >> shift : 0)];
-            if (masked && (at < 0 || t0 + in >= w.t1)) {
-                gone |= 1u << x;
-                at = 0;
-            } else {
-                at += lane_at + (long long)((t0 + x * kTPP) & mask) * a.c.ld_token;
-            }
-            k[x] = v[x] = u32x4{};
-            if (live && !(gone >> x & 1)) {
-                k[x] = *(const u32x4 *)(a.c.k + at * (kInt8 ? 1 : 2));
-                v[x] = *(const u32x4 *)(a.c.v + at * (kInt8 ? 1 : 2));
-            }
+            const long long at = sh_at[slot_next + ((x * kTPP + lane_row) >> run_shift)] + lane_at;
+            k[x] = *(const u32x4 *)(a.c.k + at);
+            v[x] = *(const u32x4 *)(a.c.v + at);
         }
         if (kInt8 && tid < kTT) {
-            const int page = sh_page[slot + (e_shift ? tid >> shift : 0)];
-            scale_k = scale_v = 0.0f;
-            if (page >= 0 && t0 + tid < w.t1) {
-                const long long at = (((long long)page * a.c.n_kv_heads + w.kvh) << shift) + ((t0 + tid) & mask);
-                scale_k = a.c.k_scale[at];
-                scale_v = a.c.v_scale[at];
-            }
+            const int page = max(0, sh_page[slot_next + (tid >> run_shift)]);
+            const long long at = (((long long)page * a.c.n_kv_heads + w.kvh) << shift) + ((t_next + tid) & mask);
+            scale_k = a.c.k_scale[at];
+            scale_v = a.c.v_scale[at];
         }
     };
     // the tile that is on its way to LDS; where care is taken without its infinite and NaN values
     auto store = [&]() {
         bool found = false;
+        if (edge || d != kD) {
+#pragma unroll
+            for (int x = 0; x < kP; ++x) {
+                const int in = x * kTPP + lane_row;
+                if (!live || t_next + in >= w.t1 || sh_page[slot_next + (in >> run_shift)] < 0) k[x] = v[x] = u32x4{};
+            }
+            if (kInt8 && tid < kTT && (t_next + tid >= w.t1 || sh_page[slot_next + (tid >> run_shift)] < 0)) scale_k = scale_v = 0.0f;
+        }
+        if (!kInt8 && careful) {
+#pragma unroll
+            for (int x = 0; x < kP; ++x)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    const uint32_t was = v[x][z];
+                    if ((was & 0x7c00u) == 0x7c00u) v[x][z] &= 0xffff0000u;
+                    if ((was & 0x7c000000u) == 0x7c000000u) v[x][z] &= 0xffffu;
+                    found |= v[x][z] != was;
+                }
+        }
 #pragma unroll
         for (int x = 0; x < kP; ++x) {
             u32x4 *const to_k = (u32x4 *)(sh_k + (x * kTPP + lane_row) * kKeyRow + piece_of * (kInt8 ? 32 : 16));
@@ -309,15 +315,6 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
                 for (int z = 0; z < 4; ++z) codes_to_half(v[x][z], y[2 * z], y[2 * z + 1]);
                 to_v[0] = u32x4{y[0], y[1], y[2], y[3]}, to_v[1] = u32x4{y[4], y[5], y[6], y[7]};
             } else {
-                if (careful) {
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) {
-                        const uint32_t was = v[x][z];
-                        if ((was & 0x7c00u) == 0x7c00u) v[x][z] &= 0xffff0000u;
-                        if ((was & 0x7c000000u) == 0x7c000000u) v[x][z] &= 0xffffu;
-                        found |= v[x][z] != was;
-                    }
-                }
                 *to_k = k[x];
                 *to_v = v[x];
             }
@@ -385,7 +382,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
                 if (bad)                              // pages are 8 tokens at least
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        if (sh_off[slot + (e_shift ? (wt * 32 * kNB + 32 * b + 8 * x) >> shift : 0)] < 0) word &= ~(255u << 8 * x);
+                        if (sh_page[slot + ((wt * 32 * kNB + 32 * b + 8 * x) >> run_shift)] < 0) word &= ~(255u << 8 * x);
                 word >>= 4 * half;
 #pragma unroll
                 for (int x = 0; x < 16; ++x)
@@ -439,12 +436,18 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
             for (int x = 0; x < 8; ++x) {
                 const int at = 8 * (step & 1) + x;
                 p[x] = exp2_(kInt8 ? acc[b][at] + off : __builtin_fmaf(acc[b][at], c, off));
-                sums[x & 3] += p[x];
-                if constexpr (kInt8) p[x] *= vs[b][at >> 2][at & 3] * cap_inv;
+                if constexpr (kInt8) {
+                    sums[x & 3] += p[x];
+                    p[x] *= vs[b][at >> 2][at & 3] * cap_inv;
+                }
             }
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-                weights[step & 1][x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[2 * x], p[2 * x + 1]}, f16x2));
+            for (int x = 0; x < 4; ++x) {
+                const f16x2 y = __builtin_convertvector(f32x2{p[2 * x], p[2 * x + 1]}, f16x2);
+                weights[step & 1][x] = __builtin_bit_cast(uint32_t, y);
+                // the weights' sum as they were rounded, two at a time
+                if constexpr (!kInt8) sums[x] = __builtin_amdgcn_fdot2(y, f16x2{(_Float16)1.0f, (_Float16)1.0f}, sums[x], false);
+            }
         };
         typedef short s16x8 __attribute__((ext_vector_type(8)));
         s16x8 t[2][kD / 32];
@@ -486,17 +489,17 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
             if (tid == 0) sh_bad = 0;
             __syncthreads();
             for (int x = tid; x < (j9 - jc) << e_shift; x += kThreads) {
-                const int t = w.tile_of(jc + (x >> e_shift)) * kTT + ((x & ((1 << e_shift) - 1)) << shift);
+                const int t = w.tile_of(jc + (x >> e_shift)) * kTT + ((x & ((1 << e_shift) - 1)) << run_shift);
                 int page = -1;
                 if (t < w.t1) {
                     page = a.table[(long long)w.s * a.ld_table + (t >> shift)];
                     if (page < 0 || page >= a.c.n_blocks) page = -1, sh_bad = 1;
                 }
-                sh_off[x] = page < 0 ? -1 : page * a.c.ld_block + w.kvh * a.c.ld_head;
-                if (kInt8) sh_page[x] = page;
+                sh_at[x] = page < 0 ? 0 : (page * a.c.ld_block + w.kvh * a.c.ld_head + (t & mask) * a.c.ld_token) * (kInt8 ? 1 : 2);
+                sh_page[x] = page;
             }
             __syncthreads();
-            bad = sh_bad != 0;
+            bad = __builtin_amdgcn_readfirstlane(sh_bad) != 0;
             load(jc);
             for (int j = jc; j < j9; ++j) {
                 __syncthreads();                          // readers of the tile before
@@ -517,7 +520,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
         for (int x = 0; x < kD / 32; ++x)
 #pragma unroll
             for (int y = 0; y < 16; ++y) sum += fabsf(o[x][y]);
-        careful = __syncthreads_or(!(sum <= 3.4e38f));
+        careful = __builtin_amdgcn_readfirstlane(__syncthreads_or(!(sum <= 3.4e38f))) != 0;
         if (!careful) break;
     }
 
