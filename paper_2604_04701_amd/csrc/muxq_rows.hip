@@ -13,8 +13,8 @@
 // Rows in LDS are 16 bytes longer for keys and 32 for values, so that neither kind of read meets the same banks twice.
 //
 // Weights are 2^(s - m + 8), rounded to fp16, and m follows the maximum only when a score is 7 above it, which is rare: up to
-// 2^15, so that small ones keep their bits.  The scale of a key goes to its score, the scale of a value to its
-// weight, over a running power of two.
+// 2^15, so that small ones keep their bits.  The scale of a key goes to its score, the scale of a value to its weight; weights and
+// their sum are over a running power of two that the scales do not pass.
 #include "muxq_block_kernels.h"
 
 #include <algorithm>
@@ -123,7 +123,7 @@ struct Row {
             word = below(-x);
             if (x > -32 && x < 64) word |= (uint32_t)(x < 0 ? above << -x : above >> x);
         } else {
-            word = below(p + 1 - t0) & ~below((int)max((long long)p - window + 1 - t0, -1ll)) | below(sinks - t0);
+            word = (below(p + 1 - t0) & ~below((int)max((long long)p - window + 1 - t0, -1ll))) | below(sinks - t0);
         }
         return word & below(t1 - t0);
     }
@@ -248,7 +248,9 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     }
     const float c = a.scale == 0.0f ? 1.0f : fminf(fabsf(a.scale) * 1.44269504088896f, 3.0e38f);
 
-    float m, l, cap, cap_inv;
+    float m;
+    int cap;                         // of codes: weights and their sum are over 2^cap, which scales of values do not pass
+    f32x4 l;                         // the weights' sum, in four parts
     f32x16 o[kD / 32];
     bool careful = false;
 
@@ -342,42 +344,85 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
         f32x16 acc[kNB] = {};
         const char *const keys = sh_k + (wt * kNB * 32 + col) * kKeyRow + half * 16;
         const char *const values = sh_v + (wt * kNB * 32 + 4 * half + ((lane & 15) >> 2)) * kValueRow + ((lane & 16) + 4 * (lane & 3)) * 2;
-        // (In the compiler's own order each matrix instruction waits for the read in front of it: the barriers keep the next four reads
-        // in front of four of them, and below the exponentials of a step behind the products of the one before.)
-        constexpr int kAhead = 4, kSteps = kD / 16 * kNB / kAhead;
-        f16x8 y[2][kAhead];
-        auto ask_keys = [&](int g) {
-#pragma unroll
-            for (int x = 0; x < kAhead; ++x) {
-                const int at = g * kAhead + x;
-                y[g & 1][x] = *(const f16x8 *)(keys + at % kNB * 32 * kKeyRow + at / kNB * 32);
-            }
+        // A block is 32 tokens: kQ products with its keys, kQ with its values, and 16 weights of a lane between them.  While a block is
+        // weighed, the products with the keys of the next one and with the values of the last one go on; reads of LDS are kAhead products in
+        // front of theirs.  (In the compiler's own order each product waits for its read, and the weights for all of them.)
+        constexpr int kQ = kD / 16, kAhead = 4;
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        f16x8 key[kAhead];
+        s16x8 value[kAhead];
+        uint32_t weights[2][8];
+        f32x4 vs[4];
+        auto ask_key = [&](int b, int x) { key[x % kAhead] = *(const f16x8 *)(keys + b * 32 * kKeyRow + x * 32); };
+        auto ask_value = [&](int b, int x) {
+            // rows 4 half + 0..3 of 16 tokens, and 8 rows on, 32 dimensions
+            const char *const at = values + (b * 32 + x / (kD / 32) * 16) * kValueRow + x % (kD / 32) * 64;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(at + 8 * kValueRow));
+            value[x % kAhead] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
-        ask_keys(0);
+        auto score = [&](int b, int x) {
+            acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key[x % kAhead], q[x], acc[b], 0, 0, 0);
+            if (x + kAhead < kQ) ask_key(b, x + kAhead);
+        };
+        auto add = [&](int b, int x) {
+            const uint32_t *const p = weights[b & 1] + x / (kD / 32) * 4;
+            o[x % (kD / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, value[x % kAhead]), __builtin_bit_cast(f16x8, u32x4{p[0], p[1], p[2], p[3]}),
+                                                                     o[x % (kD / 32)], 0, 0, 0);
+            if (x + kAhead < kQ) ask_value(b, x + kAhead);
+        };
+        float off = 0.0f;
+        auto weigh = [&](int b, int x) {              // two of them
+            float p[2];
 #pragma unroll
-        for (int g = 0; g < kSteps; ++g) {
-            if (g + 1 < kSteps) ask_keys(g + 1);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int x = 0; x < kAhead; ++x) {
-                const int at = g * kAhead + x;
-                acc[at % kNB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(y[g & 1][x], q[at / kNB], acc[at % kNB], 0, 0, 0);
+            for (int y = 0; y < 2; ++y) {
+                const int at = 2 * x + y;
+                p[y] = exp2_(kInt8 ? acc[b][at] + off : __builtin_fmaf(acc[b][at], c, off));
+                if constexpr (kInt8) {
+                    l[at & 3] += p[y];
+                    p[y] *= vs[at >> 2][at & 3];
+                }
             }
+            const f16x2 y = __builtin_convertvector(f32x2{p[0], p[1]}, f16x2);
+            weights[b & 1][x] = __builtin_bit_cast(uint32_t, y);
+            asm volatile("" : "+v"(weights[b & 1][x]));              // (here, not where the weight is needed)
+            // their sum as they were rounded
+            if constexpr (!kInt8) l[x & 3] = __builtin_amdgcn_fdot2(y, f16x2{(_Float16)1.0f, (_Float16)1.0f}, l[x & 3], false);
+        };
+        // everything so far times a power of two
+        auto scale_all = [&](int b, float keep) {
+            l *= keep;
+#pragma unroll
+            for (int x = 0; x < kD / 32; ++x) o[x] *= keep;
+            if (b > 0)
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    weights[(b - 1) & 1][x] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, weights[(b - 1) & 1][x]) * f16x2{(_Float16)keep, (_Float16)keep});
+        };
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x) ask_key(0, x);
+#pragma unroll
+        for (int x = 0; x < kQ; ++x) {
+            score(0, x);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (kInt8) {
 #pragma unroll
-            for (int b = 0; b < kNB; ++b)
+        for (int b = 0; b < kNB; ++b) {
+            const bool last = b == kNB - 1;
+            if (!last)
+#pragma unroll
+                for (int x = 0; x < kAhead; ++x) ask_key(b + 1, x);
+            if (b > 0 || last)
+#pragma unroll
+                for (int x = 0; x < kAhead; ++x) ask_value(b > 0 ? b - 1 : b, x);
+            if constexpr (kInt8) {
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const f32x4 y = *(const f32x4 *)(sh_ks + (wt * kNB + b) * 32 + 8 * x + 4 * half);
 #pragma unroll
                     for (int z = 0; z < 4; ++z) acc[b][4 * x + z] *= y[z];
                 }
-        }
-        if (!all) {
-#pragma unroll
-            for (int b = 0; b < kNB; ++b) {
+            }
+            if (!all) {
                 uint32_t word = row.sees32(tree, t0 + 32 * b, w.t1);
                 if (bad)                              // pages are 8 tokens at least
 #pragma unroll
@@ -388,99 +433,75 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
                 for (int x = 0; x < 16; ++x)
                     if (!(word >> (8 * (x >> 2) + (x & 3)) & 1)) acc[b][x] = kFloor;
             }
-        }
-        float top = kFloor;
-#pragma unroll
-        for (int b = 0; b < kNB; ++b)
+            float top = kFloor;
 #pragma unroll
             for (int x = 0; x < 16; ++x) top = fmaxf(top, acc[b][x]);
-        if (!kInt8) top *= c;
-        if (__any(top > m + 7.0f)) {                    // rare after the first tiles: a new maximum for the row
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float to = fmaxf(m, top), keep = weight_of(m, l, to);
-            m = to;
-            l *= keep;
-#pragma unroll
-            for (int x = 0; x < kD / 32; ++x) o[x] *= keep;
-        }
-        const float off = m == kFloor ? 0.0f : 8.0f - m;
-        f32x4 vs[kInt8 ? kNB : 1][4];
-        if constexpr (kInt8) {
-            float most = 0.0f;
-#pragma unroll
-            for (int b = 0; b < kNB; ++b)
+            if (!kInt8) top *= c;
+            if (__any(top > m + 7.0f)) {                    // rare after the first tiles: a new maximum for the row, a whole number
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float to = fmaxf(m, __builtin_ceilf(top)), keep = weight_of(m, l[0] + l[1] + (l[2] + l[3]), to);
+                m = to;
+                scale_all(b, keep);
+            }
+            if constexpr (kInt8) {
+                float most = 0.0f;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    vs[b][x] = *(const f32x4 *)(sh_vs + (wt * kNB + b) * 32 + 8 * x + 4 * half);
+                    vs[x] = *(const f32x4 *)(sh_vs + (wt * kNB + b) * 32 + 8 * x + 4 * half);
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) most = fmaxf(most, fabsf(vs[b][x][z]));
+                    for (int z = 0; z < 4; ++z) most = fmaxf(most, fabsf(vs[x][z]));
                 }
-            if (__any(most > cap)) {                    // scales of values over a power of two
-                most = fmaxf(most, __shfl_xor(most, 32, 64));
-                const uint32_t ex = min(__float_as_uint(most) >> 23, 252u) + 1;
-                const float was = cap;
-                cap = fmaxf(cap, __uint_as_float(ex << 23));
-                cap_inv = __uint_as_float((254u - (__float_as_uint(cap) >> 23)) << 23);
-                const float keep = was * cap_inv;
-#pragma unroll
-                for (int x = 0; x < kD / 32; ++x) o[x] *= keep;
-            }
-        }
-        // the second product: 16 tokens a step, the lanes' own, in the order of the scores
-        u32x4 weights[2];
-        f32x4 sums = {};
-        auto weigh = [&](int step) {
-            const int b = step >> 1;
-            float p[8];
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const int at = 8 * (step & 1) + x;
-                p[x] = exp2_(kInt8 ? acc[b][at] + off : __builtin_fmaf(acc[b][at], c, off));
-                if constexpr (kInt8) {
-                    sums[x & 3] += p[x];
-                    p[x] *= vs[b][at >> 2][at & 3] * cap_inv;
+                if (__any(most > __uint_as_float((uint32_t)(cap + 127) << 23))) {          // rare: scales of values beyond 2^cap
+                    most = fmaxf(most, __shfl_xor(most, 32, 64));
+                    const int to = max(cap, (int)(min(__float_as_uint(most) >> 23, 252u) + 1) - 127);
+                    scale_all(b, exp2_((float)(cap - to)));
+                    cap = to;
                 }
             }
+            off = m == kFloor ? 0.0f : 8.0f - m - (kInt8 ? (float)cap : 0.0f);
+            // two weights after each product; the last block's second half beside the products with its first half
+            if (!last) {
+                const int n = b > 0 ? 2 * kQ : kQ;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const f16x2 y = __builtin_convertvector(f32x2{p[2 * x], p[2 * x + 1]}, f16x2);
-                weights[step & 1][x] = __builtin_bit_cast(uint32_t, y);
-                // the weights' sum as they were rounded, two at a time
-                if constexpr (!kInt8) sums[x] = __builtin_amdgcn_fdot2(y, f16x2{(_Float16)1.0f, (_Float16)1.0f}, sums[x], false);
+                for (int x = 0; x < n; ++x) {
+                    if (x < kQ) score(b + 1, x);
+                    else add(b - 1, x - kQ);
+#pragma unroll
+                    for (int y = x * 8 / n; y < (x + 1) * 8 / n; ++y) weigh(b, y);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                if (b > 0) {
+#pragma unroll
+                    for (int x = 0; x < kQ; ++x) {
+                        add(b - 1, x);
+#pragma unroll
+                        for (int y = x * 8 / kQ; y < (x + 1) * 8 / kQ; ++y) weigh(b, y);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int x = 0; x < kAhead; ++x) ask_value(b, x);
+                } else {
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) weigh(b, y);
+                }
+#pragma unroll
+                for (int x = 0; x < kQ; ++x) {
+                    add(b, x);
+                    if (b == 0 && x < kQ / 2)
+#pragma unroll
+                        for (int y = 4 + x * 4 / (kQ / 2); y < 4 + (x + 1) * 4 / (kQ / 2); ++y) weigh(b, y);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-        };
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
-        s16x8 t[2][kD / 32];
-        auto ask_values = [&](int step) {
-            // rows 4 half + 0..3 of the step's tokens, and 8 rows on
-            const char *const at = values + step * 16 * kValueRow;
-#pragma unroll
-            for (int x = 0; x < kD / 32; ++x) {
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(at + 64 * x));
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(at + 64 * x + 8 * kValueRow));
-                t[step & 1][x] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            }
-        };
-        ask_values(0);
-        weigh(0);
-#pragma unroll
-        for (int step = 0; step < 2 * kNB; ++step) {
-            if (step + 1 < 2 * kNB) ask_values(step + 1);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int x = 0; x < kD / 32; ++x)
-                o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, t[step & 1][x]), __builtin_bit_cast(f16x8, weights[step & 1]),
-                                                              o[x], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-            if (step + 1 < 2 * kNB) weigh(step + 1);
         }
-        l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
     };
 
     // An infinite or NaN value makes all rows of a tile NaN, also those that do not see it (0 times infinity): where a sum is, the
     // workgroup begins again, takes such values out and remembers where they are.
     for (;;) {
-        m = kFloor, l = cap = cap_inv = 0.0f;
+        m = kFloor, cap = -80;
+        l = f32x4{};
 #pragma unroll
         for (int x = 0; x < kD / 32; ++x) o[x] = f32x16{};
         for (jc = j0; jc < j1; jc += kChunk) {
@@ -525,8 +546,15 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     }
 
     // The parts of the waves that have the same rows: m and the sum by row, then the values through LDS, lane by lane.
-    l += __shfl_xor(l, 32, 64);
-    if (l == 0.0f && row.p >= 0) {                    // no weights: are there tokens?
+    float total = (l[0] + l[1]) + (l[2] + l[3]);
+    total += __shfl_xor(total, 32, 64);
+    if constexpr (kInt8) {
+        const float up = __uint_as_float((uint32_t)(cap + 127) << 23);
+        total *= up;
+#pragma unroll
+        for (int x = 0; x < kD / 32; ++x) o[x] *= up;
+    }
+    if (total == 0.0f && row.p >= 0) {                    // no weights: are there tokens?
         bool seen = false;
         for (int j = j0; j < j1 && !seen; ++j) {
             const int t0 = w.tile_of(j) * kTT + wt * (32 * kNB);
@@ -536,21 +564,21 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
                     seen = page >= 0 && page < a.c.n_blocks;
                 }
         }
-        if (seen) l = kNone;
+        if (seen) total = kNone;
     }
-    float top = m, total = l;
+    float top = m;
     if constexpr (kWT > 1) {
-        if (half == 0) sh_m[wave][col] = m, sh_l[wave][col] = l;
+        if (half == 0) sh_m[wave][col] = m, sh_l[wave][col] = total;
         __syncthreads();
 #pragma unroll
         for (int x = 0; x < kWT; ++x) top = fmaxf(top, sh_m[x * kWR + wr][col]);
+        const float f = weight_of(m, total, top);
         total = 0.0f;
 #pragma unroll
         for (int x = 0; x < kWT; ++x) {
             const float y = sh_m[x * kWR + wr][col], z = sh_l[x * kWR + wr][col];
             total += weight_of(y, z, top) * z;
         }
-        const float f = weight_of(m, l, top) * (kInt8 ? cap : 1.0f);
 #pragma unroll
         for (int x = 0; x < kD / 32; ++x) o[x] *= f;
         // the upper half of the waves gives, the lower half takes
@@ -576,9 +604,6 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
             }
             if (give > 1) __syncthreads();
         }
-    } else if constexpr (kInt8) {
-#pragma unroll
-        for (int x = 0; x < kD / 32; ++x) o[x] *= cap;
     }
     const long long part = ((((long long)w.s * a.c.n_kv_heads + w.kvh) * plan.row_tiles + blockIdx.x / a.c.n_kv_heads) * plan.pieces + piece) * kR;
     float *const part_o = whole ? nullptr : plan.o + part * d;
