@@ -12,16 +12,40 @@
 namespace muxq {
 namespace {
 
+constexpr long long kAtOnce = 8 << 20;          // numbers of a target whose rows are looked at all at once
 constexpr int kThreads = 1024, kWaves = kThreads / 64, kBlock = 1024, kMaxBlocks = (1 << 22) / kBlock;
 
 typedef float Four __attribute__((ext_vector_type(4), aligned(4)));        // rows of an odd vocabulary begin anywhere
 
-__device__ __forceinline__ double wave_sum(double v)
+// v plus the value of another lane: lanes of a row of 16 to the right, or the last lane of a row to the rows in kRows.
+template <int kWhere, int kRows>
+__device__ __forceinline__ double plus(double v)
 {
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) v += __shfl_xor(v, x, 64);
-    return v;
+    typedef int Two __attribute__((ext_vector_type(2)));
+    const Two x = __builtin_bit_cast(Two, v);
+    return v + __builtin_bit_cast(double, Two{__builtin_amdgcn_update_dpp(0, x[0], kWhere, kRows, 0xf, false),
+                                              __builtin_amdgcn_update_dpp(0, x[1], kWhere, kRows, 0xf, false)});
 }
+
+// The sums up to each lane, without LDS.
+__device__ __forceinline__ double wave_scan(double v)
+{
+    v = plus<0x111, 0xf>(v);
+    v = plus<0x112, 0xf>(v);
+    v = plus<0x114, 0xf>(v);
+    v = plus<0x118, 0xf>(v);
+    v = plus<0x142, 0xa>(v);
+    return plus<0x143, 0xc>(v);
+}
+
+__device__ __forceinline__ double lane_of(double v, int lane)
+{
+    typedef int Two __attribute__((ext_vector_type(2)));
+    const Two x = __builtin_bit_cast(Two, v);
+    return __builtin_bit_cast(double, Two{__builtin_amdgcn_readlane(x[0], lane), __builtin_amdgcn_readlane(x[1], lane)});
+}
+
+__device__ __forceinline__ double wave_sum(double v) { return lane_of(wave_scan(v), 63); }
 
 // Where a node's children are tried: p, q (NULL: 1 for the child's token) and the rejections so far.
 struct Rest {
@@ -45,26 +69,89 @@ __device__ __forceinline__ double less(const Rest &r, double x, double q, int t)
     return x;
 }
 
-// Four tokens from t on.
-__device__ __forceinline__ void four(const Rest &r, int t, int V, double out[4])
+// A lane's tokens of a block: four runs of four, 256 tokens apart.
+struct Tokens {
+    Four p[4], q[4];
+};
+
+__device__ __forceinline__ void ask(const Rest &r, int block, int V, Tokens &x)
 {
-    Four p = {}, q = {};
-    if (t + 4 <= V) {
-        p = *(const Four *)(r.p + t);
-        if (r.q && r.rejected) q = *(const Four *)(r.q + t);
-    } else {
+    const int t0 = block * kBlock + (threadIdx.x & 63) * 4;
+    const bool two = r.q && r.rejected;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (t + i < V) {
-                p[i] = r.p[t + i];
-                if (r.q && r.rejected) q[i] = r.q[t + i];
-            }
+    for (int i = 0; i < 4; ++i) {
+        const int t = t0 + i * 256;
+        x.p[i] = x.q[i] = Four{};
+        if (t + 4 <= V) {
+            x.p[i] = *(const Four *)(r.p + t);
+            if (two) x.q[i] = *(const Four *)(r.q + t);
+        } else {
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                if (t + y < V) {
+                    x.p[i][y] = r.p[t + y];
+                    if (two) x.q[i][y] = r.q[t + y];
+                }
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = less(r, p[i], q[i], t + i);
 }
 
-__global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
+// The largest of a row, the lowest index of equal ones, for all threads of a workgroup.
+__device__ int largest(const float *p, int V, float *sh_most, int *sh_best)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int kEach = 8;                            // loads on their way
+    float most = -__builtin_inff();
+    int best = 0x7fffffff;
+    auto look = [&](float x, int t) {
+        if (x > most) most = x, best = t;
+    };
+    for (int t0 = tid * 4; t0 < V; t0 += 4 * kThreads * kEach) {
+        Four x[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int t = t0 + i * 4 * kThreads;
+            x[i] = Four{};
+            if (t + 4 <= V) x[i] = *(const Four *)(p + t);
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int t = t0 + i * 4 * kThreads;
+            if (t + 4 <= V) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) look(x[i][y], t + y);
+            } else {
+                for (int y = t; y < V; ++y) look(p[y], y);
+            }
+        }
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+        const float other = __shfl_xor(most, x, 64);
+        const int at = __shfl_xor(best, x, 64);
+        if (other > most || (other == most && at < best)) most = other, best = at;
+    }
+    __syncthreads();                        // the last row's readers
+    if (lane == 0) sh_most[wave] = most, sh_best[wave] = best;
+    __syncthreads();
+    most = sh_most[0], best = sh_best[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w)
+        if (sh_most[w] > most || (sh_most[w] == most && sh_best[w] < best)) most = sh_most[w], best = sh_best[w];
+    return best == 0x7fffffff ? 0 : best;       // nothing above -infinity
+}
+
+// The largest of each row, left in path, which is not yet needed for anything else.
+__global__ __launch_bounds__(kThreads) void k_largest(VerifyArgs a)
+{
+    __shared__ float sh_most[kWaves];
+    __shared__ int sh_best[kWaves];
+    if ((int)blockIdx.x < a.starts[0] || (int)blockIdx.x >= a.starts[a.S]) return;       // a row of no sequence
+    const int best = largest(a.target + blockIdx.x * a.ldt, a.V, sh_most, sh_best);
+    if (threadIdx.x == 0) a.path[blockIdx.x] = best;
+}
+
+__global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a, bool known)
 {
     extern __shared__ __align__(16) double sh_block[];         // [blocks of the vocabulary]
     __shared__ double sh_inv[kMaxNodes + 1], sh_total;
@@ -83,6 +170,7 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
         sh_token[tid] = token;
         sh_parent[tid] = up;
         float p = 0.0f, q = 1.0f;
+        if (known) sh_gone[tid] = a.path[first + tid];        // the largest of the node's row
         if (a.uniforms) {
             sh_u[tid] = a.uniforms[first + tid];
             if (up >= 0 && up < tid && token >= 0 && token < V) {
@@ -109,36 +197,7 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
 
     if (!a.uniforms) {
         for (;;) {
-            // the largest of target[v], the lowest of equal ones
-            const float *const p = a.target + (first + v) * a.ldt;
-            float most = -__builtin_inff();
-            int best = 0x7fffffff;
-            auto look = [&](float x, int t) {
-                if (x > most) most = x, best = t;
-            };
-            for (int t = tid * 4; t < V; t += 4 * kThreads) {
-                if (t + 4 <= V) {
-                    const Four x = *(const Four *)(p + t);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) look(x[i], t + i);
-                } else {
-                    for (int i = t; i < V; ++i) look(p[i], i);
-                }
-            }
-#pragma unroll
-            for (int x = 1; x < 64; x <<= 1) {
-                const float other = __shfl_xor(most, x, 64);
-                const int at = __shfl_xor(best, x, 64);
-                if (other > most || (other == most && at < best)) most = other, best = at;
-            }
-            __syncthreads();                        // the last row's readers
-            if (lane == 0) sh_most[wave] = most, sh_best[wave] = best;
-            __syncthreads();
-            most = sh_most[0], best = sh_best[0];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w)
-                if (sh_most[w] > most || (sh_most[w] == most && sh_best[w] < best)) most = sh_most[w], best = sh_best[w];
-            if (best == 0x7fffffff) best = 0;       // nothing above -infinity
+            const int best = known ? sh_gone[v] : largest(a.target + (first + v) * a.ldt, V, sh_most, sh_best);
             int taken = -1;
             for (int c = v + 1; c < n; ++c)
                 if (sh_parent[c] == v && sh_token[c] == best) {
@@ -161,18 +220,27 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
         Z = 1.0;
     };
     // the sum of r, and of its blocks
+    auto values = [&](const Tokens &y, int b, int i, double x[4]) {
+        const int t = b * kBlock + i * 256 + lane * 4;
+#pragma unroll
+        for (int z = 0; z < 4; ++z) x[z] = less(r, y.p[i][z], y.q[i][z], t + z);
+    };
     auto pass = [&]() {
-        for (int b = wave; b < blocks; b += kWaves) {
+        Tokens y[2];
+        int b = wave;
+        if (b < blocks) ask(r, b, V, y[0]);
+        for (; b < blocks; b += kWaves) {
+            if (b + kWaves < blocks) ask(r, b + kWaves, V, y[1]);
             double sum = 0.0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int t = b * kBlock + i * 256 + lane * 4;
-                double x[4] = {};
-                if (t < V) four(r, t, V, x);
+                double x[4];
+                values(y[0], b, i, x);
                 sum += (x[0] + x[1]) + (x[2] + x[3]);
             }
             sum = wave_sum(sum);
             if (lane == 0) sh_block[b] = sum;
+            y[0] = y[1];
         }
         __syncthreads();
         if (wave == 0) {
@@ -229,51 +297,44 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
         for (int b0 = 0; b0 < blocks && found < 0; b0 += 64) {
             const int b = b0 + lane;
             const double mine = b < blocks ? sh_block[b] : 0.0;
-            double up = mine;
-#pragma unroll
-            for (int x = 1; x < 64; x <<= 1) {
-                const double y = __shfl_up(up, x, 64);
-                if (lane >= x) up += y;
-            }
+            const double up = wave_scan(mine);
             const unsigned long long past = __ballot(before + up > to && mine > 0.0), some = __ballot(mine > 0.0);
             if (past) {
                 const int l = __ffsll((long long)past) - 1;
                 found = b0 + l;
-                at_found = before + __shfl(up - mine, l, 64);
+                at_found = before + lane_of(up - mine, l);
             } else if (some) {
                 const int l = 63 - __clzll((long long)some);
                 last = b0 + l;
-                at_last = before + __shfl(up - mine, l, 64);
+                at_last = before + lane_of(up - mine, l);
             }
-            before += __shfl(up, 63, 64);
+            before += lane_of(up, 63);
         }
         if (found < 0) found = last, at_found = at_last;
         int token = -1, positive = -1;
-        for (int i = 0; i < 4 && token < 0; ++i) {
-            const int t = found * kBlock + i * 256 + lane * 4;
-            double x[4] = {};
-            if (t < V) four(r, t, V, x);
-            const double mine = (x[0] + x[1]) + (x[2] + x[3]);
-            double up = mine;
+        Tokens y;
+        ask(r, found, V, y);
 #pragma unroll
-            for (int y = 1; y < 64; y <<= 1) {
-                const double z = __shfl_up(up, y, 64);
-                if (lane >= y) up += z;
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int t = found * kBlock + i * 256 + lane * 4;
+            double x[4];
+            values(y, found, i, x);
+            const double mine = (x[0] + x[1]) + (x[2] + x[3]);
+            const double up = wave_scan(mine);
             double run = at_found + (up - mine);
             int here = -1, some = -1;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                run += x[y];
-                if (x[y] > 0.0) {
-                    some = t + y;
-                    if (here < 0 && run > to) here = t + y;
+            for (int z = 0; z < 4; ++z) {
+                run += x[z];
+                if (x[z] > 0.0) {
+                    some = t + z;
+                    if (here < 0 && run > to) here = t + z;
                 }
             }
             const unsigned long long past = __ballot(here >= 0), any = __ballot(some >= 0);
-            if (past) token = __shfl(here, __ffsll((long long)past) - 1, 64);
+            if (past && token < 0) token = __shfl(here, __ffsll((long long)past) - 1, 64);
             if (any) positive = __shfl(some, 63 - __clzll((long long)any), 64);
-            at_found += __shfl(up, 63, 64);
+            at_found += lane_of(up, 63);
         }
         if (token < 0) token = positive;        // rounding, or u = 1
         if (lane == 0) a.next[s] = token;
@@ -293,7 +354,13 @@ hipError_t verify_prepare()
 hipError_t launch_verify(const VerifyArgs &a, hipStream_t s)
 {
     const size_t lds = (size_t)((a.V + kBlock - 1) / kBlock) * sizeof(double);
-    return launch_kernel(k_verify, dim3(a.S), dim3(kThreads), lds, s, a);
+    // Greedy: all rows at once and the walk after them, or the rows of a walk one after the other.
+    const bool known = !a.uniforms && (long long)a.M * a.V <= kAtOnce;
+    if (known) {
+        const hipError_t e = launch_kernel(k_largest, dim3(a.M), dim3(kThreads), 0, s, a);
+        if (e != hipSuccess) return e;
+    }
+    return launch_kernel(k_verify, dim3(a.S), dim3(kThreads), lds, s, a, known);
 }
 
 }  // namespace muxq
