@@ -301,6 +301,7 @@ static int rows_attention(const void *Q, int M, int n_heads, int ldq, const muxq
     a.window = window;
     a.sinks = window ? sinks : 0;
     a.max_new = max_new < M ? max_new : M;
+    if ((long long)a.max_new * (n_heads / a.c.n_kv_heads) >= (1ll << 31) - 256) return MUXQ_ERR_SHAPE;
     const size_t need = muxq::rows_workspace_need(S, n_heads, a.c.n_kv_heads, d, a.max_new, max_length, a.window, a.sinks, tree);
     if (need > 0) {
         if (!workspace) return MUXQ_ERR_NULL;

@@ -64,12 +64,18 @@ struct Plan {
     float2 *ml;         // [row tile of all][piece][rows of a tile]: m and the sum
 };
 
+// A number that all lanes need: through the scalar cache.
+__device__ __forceinline__ int one(const int32_t *p)
+{
+    return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p;
+}
+
 // What one workgroup's rows are and see.
 template <int kTT>
 struct Span {
     int s, kvh, first, n, len, ctx;           // rows first..first + n of the call, tokens before the first
-    long long row0;                           // of the sequence's rows (token, head)
-    int i_lo, i_hi, t1;                       // its tokens, and the first token that none of its rows sees
+    int row0, n_rows;                         // of the sequence's rows (token, head), fewer than 2^31
+    int i_lo, i_hi, local0, t1;               // its tokens, the first row's place in the first of them, and the first token that none of its rows sees
     int sink_tiles, window_from, count;       // tiles that they see: the first ones, then from window_from on
 
     __device__ __forceinline__ bool find(const RowsArgs &a, int x, int seq, int row_tiles, int rows)
@@ -77,15 +83,18 @@ struct Span {
         s = seq;
         const int tile = x / a.c.n_kv_heads;
         kvh = x - tile * a.c.n_kv_heads;
-        first = max(0, min(a.starts[s], a.M));
-        n = max(0, min(a.starts[s + 1], a.M)) - first;
+        const int from = one(a.starts + s), to = one(a.starts + s + 1), length = one(a.lengths + s);
+        first = max(0, min(from, a.M));
+        n = max(0, min(to, a.M)) - first;
         if (n < 1 || n > a.max_new) return false;
-        row0 = (long long)(row_tiles - 1 - tile) * rows;          // the last tokens see most: they come first
-        if (row0 >= (long long)n * a.group) return false;
-        len = max(0, min(a.lengths[s], a.max_length));
+        row0 = (row_tiles - 1 - tile) * rows;          // the last tokens see most: they come first
+        n_rows = min(rows, n * a.group - row0);
+        if (n_rows <= 0) return false;
+        len = max(0, min(length, a.max_length));
         ctx = len - n;
-        i_lo = (int)(row0 / a.group);
-        i_hi = min(n - 1, (int)((row0 + rows - 1) / a.group));
+        i_lo = (int)((uint32_t)row0 / (uint32_t)a.group);
+        local0 = row0 - i_lo * a.group;
+        i_hi = (int)((uint32_t)(row0 + n_rows - 1) / (uint32_t)a.group);
         t1 = a.parents ? len : max(0, min(len, ctx + i_hi + 1));
         sink_tiles = window_from = 0;
         count = (t1 + kTT - 1) / kTT;
@@ -107,8 +116,9 @@ struct Row {
 
     __device__ __forceinline__ void find(const RowsArgs &a, int kvh, int n, int ctx_, int i_lo, int local)
     {
-        i = min(n - 1, i_lo + local / a.group);
-        head = kvh * a.group + local % a.group;
+        const int more = (int)((uint32_t)local / (uint32_t)a.group);
+        i = min(n - 1, i_lo + more);
+        head = kvh * a.group + local - more * a.group;
         ctx = ctx_;
         p = ctx + i;
         window = a.window ? a.window : 0x80000000u;
@@ -152,12 +162,11 @@ __device__ __forceinline__ uint64_t nodes_above(const int32_t *parents, int i)
 // Infinite and NaN values that the rows of a workgroup see, with weights of 1, or of 0 where the row's score is -infinity: all that counts for
 // a sum in which there is one.  The tiles' values went into the products without them; here they decide what they stand for.
 template <bool kInt8, int kTT>
-__device__ void put_loose(const RowsArgs &a, const Span<kTT> &w, int rows, int j0, int j1, const int *tiles, int n_tiles,
+__device__ void put_loose(const RowsArgs &a, const Span<kTT> &w, int j0, int j1, const int *tiles, int n_tiles,
                                                     const int32_t *parents, _Float16 *o, float *part)
 {
     const int d = a.c.head_dim, quads = d / 4, shift = a.c.block_shift, mask = (1 << shift) - 1;
-    const int local0 = (int)(w.row0 - (long long)w.i_lo * a.group);
-    const int n_rows = (int)min((long long)rows, (long long)w.n * a.group - w.row0);
+    const int local0 = w.local0, n_rows = w.n_rows;
     for (int item = threadIdx.x; item < n_rows * quads; item += blockDim.x) {
         const int r = item / quads, e = (item - r * quads) * 4;
         Row row;
@@ -205,18 +214,23 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     constexpr int kThreads = 64 * kWaves, kWT = kWaves / kWR, kR = 32 * kWR, kNB = kTT / kWT / 32;          // waves along tokens; rows; blocks of 32 tokens of a wave
     constexpr int kKeyRow = 2 * kD + 16, kValueRow = 2 * kD + 32;                   // bytes of a row in LDS
     constexpr int kCH = kInt8 ? kD / 16 : kD / 8, kTPP = kThreads / kCH, kP = kTT / kTPP;      // loads of a row, rows of a pass, passes
+    constexpr bool kAllJoin = kWR == 1 && kD * 128 * kWaves <= kTT * (kKeyRow + kValueRow);       // all waves' parts fit the tile's LDS
     static_assert(kNB >= 1 && kP >= 1, "tile");
     __shared__ __align__(16) char sh_k[kTT * (kKeyRow + kValueRow)];
     char *const sh_v = sh_k + kTT * kKeyRow;
+    f32x4 *const sh_o = (f32x4 *)sh_k;
     __shared__ long long sh_at[kChunk * (kTT / 8)];           // where runs of rows stand, in bytes; 0 for those that are nowhere
     __shared__ int sh_page[kChunk * (kTT / 8)];               // their pages; -1: not in the cache, or behind all tokens
     __shared__ __align__(16) float sh_ks[kInt8 ? kTT : 4], sh_vs[kInt8 ? kTT : 4];
     __shared__ float sh_m[kWaves][32], sh_l[kWaves][32];
+    __shared__ long long sh_row[32];
     __shared__ int sh_bad, sh_found, sh_n_loose, sh_loose[kLoose], sh_parents[kMaxNodes];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave % kWR, wt = wave / kWR, col = lane & 31, half = lane >> 5;
     const int d = a.c.head_dim, shift = a.c.block_shift, mask = (1 << shift) - 1;
     const bool tree = a.parents != nullptr;
 
+    if (tid == 0) sh_found = sh_n_loose = sh_bad = 0;
+    __syncthreads();
     Span<kTT> w;
     if (!w.find(a, blockIdx.x, blockIdx.y, plan.row_tiles, kR)) return;
     const int piece = blockIdx.z;
@@ -224,14 +238,28 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     const int j0 = whole ? 0 : piece * plan.tiles, j1 = whole || piece == plan.pieces - 1 ? w.count : min(w.count, j0 + plan.tiles);
     if (piece > 0 && (whole || j0 >= j1)) return;
 
-    if (tree && tid < w.n) sh_parents[tid] = a.parents[w.first + tid];
-    if (tid == 0) sh_found = sh_n_loose = 0;
-    __syncthreads();
-    const int local0 = (int)(w.row0 - (long long)w.i_lo * a.group);
-    const int n_rows = (int)min((long long)kR, (long long)w.n * a.group - w.row0);
+    // the pages of tiles j0..j9, and whether one is missing (0 before)
+    const int run_shift = min(shift, __builtin_ctz(kTPP)), e_shift = __builtin_ctz(kTT) - run_shift;      // runs of a tile: 1 << e_shift
+    auto find_pages = [&](int j0, int j9) {
+        for (int x = tid; x < (j9 - j0) << e_shift; x += kThreads) {
+            const int t = w.tile_of(j0 + (x >> e_shift)) * kTT + ((x & ((1 << e_shift) - 1)) << run_shift);
+            int page = -1;
+            if (t < w.t1) {
+                page = a.table[(long long)w.s * a.ld_table + (t >> shift)];
+                if (page < 0 || page >= a.c.n_blocks) page = -1, sh_bad = 1;
+            }
+            sh_at[x] = page < 0 ? 0 : (page * a.c.ld_block + w.kvh * a.c.ld_head + (t & mask) * a.c.ld_token) * (kInt8 ? 1 : 2);
+            sh_page[x] = page;
+        }
+    };
+
+    int parent = 0;
+    if (tree && tid < w.n) parent = a.parents[w.first + tid];
+    find_pages(j0, min(j1, j0 + kChunk));
+    if (tree && tid < w.n) sh_parents[tid] = parent;
+    const int local0 = w.local0, n_rows = w.n_rows;
     Row row;
     row.find(a, w.kvh, w.n, w.ctx, w.i_lo, local0 + min(wr * 32 + col, n_rows - 1));
-    row.above = tree ? nodes_above(sh_parents, row.i) : 0;
     // what the wave's rows see, from the first to the last of them
     const int p_lo = __builtin_amdgcn_readfirstlane(row.p), p_hi = __builtin_amdgcn_readlane(row.p, 31);
     const _Float16 *const q_row = a.q + (long long)(w.first + row.i) * a.ldq + (long long)row.head * d;
@@ -248,7 +276,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     }
     const float c = a.scale == 0.0f ? 1.0f : fminf(fabsf(a.scale) * 1.44269504088896f, 3.0e38f);
 
-    float m;
+    float m, total;
     int cap;                         // of codes: weights and their sum are over 2^cap, which scales of values do not pass
     f32x4 l;                         // the weights' sum, in four parts
     f32x16 o[kD / 32];
@@ -258,7 +286,6 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     const int lane_row = tid / kCH, piece_of = tid % kCH;
     const bool live = piece_of * (kInt8 ? 16 : 8) < d;
     // (rows of a run stand in one page and belong to one pass)
-    const int run_shift = min(shift, __builtin_ctz(kTPP)), e_shift = __builtin_ctz(kTT) - run_shift;      // runs of a tile: 1 << e_shift
     const long long lane_at = ((long long)(lane_row & ((1 << run_shift) - 1)) * a.c.ld_token + (live ? piece_of : 0) * (kInt8 ? 16 : 8)) * (kInt8 ? 1 : 2);
     u32x4 k[kP], v[kP];
     float scale_k = 0.0f, scale_v = 0.0f;
@@ -506,24 +533,18 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
         for (int x = 0; x < kD / 32; ++x) o[x] = f32x16{};
         for (jc = j0; jc < j1; jc += kChunk) {
             const int j9 = min(j1, jc + kChunk);
-            __syncthreads();                              // readers of the pages before
-            if (tid == 0) sh_bad = 0;
-            __syncthreads();
-            for (int x = tid; x < (j9 - jc) << e_shift; x += kThreads) {
-                const int t = w.tile_of(jc + (x >> e_shift)) * kTT + ((x & ((1 << e_shift) - 1)) << run_shift);
-                int page = -1;
-                if (t < w.t1) {
-                    page = a.table[(long long)w.s * a.ld_table + (t >> shift)];
-                    if (page < 0 || page >= a.c.n_blocks) page = -1, sh_bad = 1;
-                }
-                sh_at[x] = page < 0 ? 0 : (page * a.c.ld_block + w.kvh * a.c.ld_head + (t & mask) * a.c.ld_token) * (kInt8 ? 1 : 2);
-                sh_page[x] = page;
+            if (jc > j0 || careful) {
+                __syncthreads();                              // readers of the pages before
+                if (tid == 0) sh_bad = 0;
+                __syncthreads();
+                find_pages(jc, j9);
             }
             __syncthreads();
             bad = __builtin_amdgcn_readfirstlane(sh_bad) != 0;
             load(jc);
+            if (jc == j0) row.above = tree ? nodes_above(sh_parents, row.i) : 0;
             for (int j = jc; j < j9; ++j) {
-                __syncthreads();                          // readers of the tile before
+                if (j > j0) __syncthreads();              // readers of the tile before
                 store();
                 __syncthreads();
                 if (careful && tid == 0 && sh_found) {
@@ -535,79 +556,100 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
                 compute(j);
             }
         }
-        if (careful) break;
+        // the sum of a row's weights, of the wave's tokens
+        total = (l[0] + l[1]) + (l[2] + l[3]);
+        total += __shfl_xor(total, 32, 64);
+        if constexpr (kInt8) {
+            const float up = __uint_as_float((uint32_t)(cap + 127) << 23);
+            total *= up;
+#pragma unroll
+            for (int x = 0; x < kD / 32; ++x) o[x] *= up;
+        }
+        if (total == 0.0f && row.p >= 0) {                    // no weights: are there tokens?
+            bool seen = false;
+            for (int j = j0; j < j1 && !seen; ++j) {
+                const int t0 = w.tile_of(j) * kTT + wt * (32 * kNB);
+                for (int t = t0; t < min(t0 + 32 * kNB, w.t1) && !seen; ++t)
+                    if (row.sees(tree, t)) {
+                        const int page = a.table[(long long)w.s * a.ld_table + (t >> shift)];
+                        seen = page >= 0 && page < a.c.n_blocks;
+                    }
+            }
+            if (seen) total = kNone;
+        }
         float sum = 0.0f;
 #pragma unroll
         for (int x = 0; x < kD / 32; ++x)
 #pragma unroll
             for (int y = 0; y < 16; ++y) sum += fabsf(o[x][y]);
-        careful = __builtin_amdgcn_readfirstlane(__syncthreads_or(!(sum <= 3.4e38f))) != 0;
-        if (!careful) break;
+        if constexpr (kWT > 1) {
+            // Waves with the same rows leave their parts in LDS, lane by lane, where all threads join them; or the first takes what the others
+            // leave there, where it does not hold all.
+            __syncthreads();                                  // readers of the last tile
+            static_assert(kD / 8 * 64 * 16 * (kWaves - kWR) <= sizeof(sh_k), "the parts fit the tile");
+            if (half == 0) sh_m[wave][col] = m, sh_l[wave][col] = total;
+            if (half == 0 && wave == 0) sh_row[col] = (long long)(w.first + row.i) * a.ldo + (long long)row.head * d;
+            if (kAllJoin || wt > 0)
+#pragma unroll
+                for (int x = 0; x < kD / 8; ++x)
+                    sh_o[((wave - (kAllJoin ? 0 : kWR)) * (kD / 8) + x) * 64 + lane] = f32x4{o[x >> 2][4 * (x & 3)], o[x >> 2][4 * (x & 3) + 1], o[x >> 2][4 * (x & 3) + 2], o[x >> 2][4 * (x & 3) + 3]};
+        }
+        if (careful && kWT == 1) break;
+        if (!careful && __any(!(sum <= 3.4e38f))) sh_found = 1;
+        __syncthreads();
+        if (careful || __builtin_amdgcn_readfirstlane(sh_found) == 0) break;
+        careful = true;
+        __syncthreads();
+        if (tid == 0) sh_found = 0;
     }
 
-    // The parts of the waves that have the same rows: m and the sum by row, then the values through LDS, lane by lane.
-    float total = (l[0] + l[1]) + (l[2] + l[3]);
-    total += __shfl_xor(total, 32, 64);
-    if constexpr (kInt8) {
-        const float up = __uint_as_float((uint32_t)(cap + 127) << 23);
-        total *= up;
-#pragma unroll
-        for (int x = 0; x < kD / 32; ++x) o[x] *= up;
-    }
-    if (total == 0.0f && row.p >= 0) {                    // no weights: are there tokens?
-        bool seen = false;
-        for (int j = j0; j < j1 && !seen; ++j) {
-            const int t0 = w.tile_of(j) * kTT + wt * (32 * kNB);
-            for (int t = t0; t < min(t0 + 32 * kNB, w.t1) && !seen; ++t)
-                if (row.sees(tree, t)) {
-                    const int page = a.table[(long long)w.s * a.ld_table + (t >> shift)];
-                    seen = page >= 0 && page < a.c.n_blocks;
-                }
-        }
-        if (seen) total = kNone;
-    }
-    float top = m;
-    if constexpr (kWT > 1) {
-        if (half == 0) sh_m[wave][col] = m, sh_l[wave][col] = total;
-        __syncthreads();
-#pragma unroll
-        for (int x = 0; x < kWT; ++x) top = fmaxf(top, sh_m[x * kWR + wr][col]);
-        const float f = weight_of(m, total, top);
-        total = 0.0f;
-#pragma unroll
-        for (int x = 0; x < kWT; ++x) {
-            const float y = sh_m[x * kWR + wr][col], z = sh_l[x * kWR + wr][col];
-            total += weight_of(y, z, top) * z;
-        }
-#pragma unroll
-        for (int x = 0; x < kD / 32; ++x) o[x] *= f;
-        // the upper half of the waves gives, the lower half takes
-        f32x4 *const sh = (f32x4 *)sh_k;
-        static_assert(kD / 32 * 16 * 64 * 4 * (kWaves / 2) <= sizeof(sh_k), "the join fits the tile");
-#pragma unroll
-        for (int give = kWT / 2; give >= 1; give /= 2) {
-            const int to = (wt - give) * kWR + wr, from = wt * kWR + wr;
-#pragma unroll
-            for (int x = 0; x < kD / 8; ++x) {
-                if (wt >= give && wt < 2 * give) {
-                    sh[(to * (kD / 8) + x) * 64 + lane] = f32x4{o[x >> 2][4 * (x & 3)], o[x >> 2][4 * (x & 3) + 1], o[x >> 2][4 * (x & 3) + 2], o[x >> 2][4 * (x & 3) + 3]};
-                }
-            }
-            __syncthreads();
-#pragma unroll
-            for (int x = 0; x < kD / 8; ++x) {
-                if (wt < give) {
-                    const f32x4 y = sh[(from * (kD / 8) + x) * 64 + lane];
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) o[x >> 2][4 * (x & 3) + z] += y[z];
-                }
-            }
-            if (give > 1) __syncthreads();
-        }
-    }
     const long long part = ((((long long)w.s * a.c.n_kv_heads + w.kvh) * plan.row_tiles + blockIdx.x / a.c.n_kv_heads) * plan.pieces + piece) * kR;
     float *const part_o = whole ? nullptr : plan.o + part * d;
-    if (wt == 0 && wr * 32 + col < n_rows) {
+    float top = m;
+    if constexpr (kAllJoin) {
+        // (not unrolled: a short call is bound by the fetching of instructions)
+#pragma unroll 1
+        for (int item = tid; item < kD / 8 * 64; item += kThreads) {
+            const int x = item >> 6, r = item & 31, e = 32 * (x >> 2) + 8 * (x & 3) + 4 * (item >> 5 & 1);
+            if (r >= n_rows || e >= d) continue;
+            float top = sh_m[0][r], total = 0.0f;
+#pragma unroll
+            for (int y = 1; y < kWaves; ++y) top = fmaxf(top, sh_m[y][r]);
+            f32x4 sum = {};
+#pragma unroll
+            for (int y = 0; y < kWaves; ++y) {
+                const float z = sh_l[y][r], f = weight_of(sh_m[y][r], z, top);
+                total += f * z;
+                sum += f * sh_o[y * (kD * 8) + item];
+            }
+            if (whole)
+                *(f16x4 *)(a.o + sh_row[r] + e) = __builtin_convertvector(sum * factor_of(top, total), f16x4);
+            else
+                *(f32x4 *)(part_o + (long long)r * d + e) = sum;
+            if (!whole && e == 0) plan.ml[part + r] = make_float2(top, top == kFloor && total > 0.0f ? kNone : total);
+        }
+    } else if constexpr (kWT > 1) {
+        if (wt == 0) {
+#pragma unroll
+            for (int x = 1; x < kWT; ++x) top = fmaxf(top, sh_m[x * kWR + wr][col]);
+            const float f = weight_of(m, total, top);
+            total *= f;
+#pragma unroll
+            for (int x = 0; x < kD / 32; ++x) o[x] *= f;
+#pragma unroll
+            for (int x = 1; x < kWT; ++x) {
+                const float z = sh_l[x * kWR + wr][col], f = weight_of(sh_m[x * kWR + wr][col], z, top);
+                total += f * z;
+#pragma unroll
+                for (int y = 0; y < kD / 8; ++y) {
+                    const f32x4 v = f * sh_o[(((x - 1) * kWR + wr) * (kD / 8) + y) * 64 + lane];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) o[y >> 2][4 * (y & 3) + z] += v[z];
+                }
+            }
+        }
+    }
+    if (!kAllJoin && wt == 0 && wr * 32 + col < n_rows) {
         const int r = wr * 32 + col;
         const float inv = factor_of(top, total);
         _Float16 *const o_row = a.o + (long long)(w.first + row.i) * a.ldo + (long long)row.head * d;
@@ -625,10 +667,11 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
             }
         if (!whole && half == 0) plan.ml[part + r] = make_float2(top, top == kFloor && total > 0.0f ? kNone : total);
     }
+    if (!careful) return;
     __syncthreads();
     if (sh_n_loose > 0) {
         __threadfence_block();
-        put_loose<kInt8, kTT>(a, w, kR, j0, j1, sh_loose, sh_n_loose, sh_parents, a.o, part_o);
+        put_loose<kInt8, kTT>(a, w, j0, j1, sh_loose, sh_n_loose, sh_parents, a.o, part_o);
     }
 }
 
@@ -642,8 +685,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_rows_join(RowsArgs a, Plan pla
     Span<kTT> w;
     if (!w.find(a, blockIdx.x, blockIdx.y, plan.row_tiles, rows) || w.count <= plan.tiles) return;
     const int d = a.c.head_dim, quads = d / 4, pieces = min(plan.pieces, (w.count + plan.tiles - 1) / plan.tiles);
-    const int local0 = (int)(w.row0 - (long long)w.i_lo * a.group);
-    const int n_rows = (int)min((long long)rows, (long long)w.n * a.group - w.row0);
+    const int local0 = w.local0, n_rows = w.n_rows;
     const long long part = (((long long)w.s * a.c.n_kv_heads + w.kvh) * plan.row_tiles + blockIdx.x / a.c.n_kv_heads) * plan.pieces * rows;
     for (int item = threadIdx.x + kJoinThreads * blockIdx.z; item < n_rows * quads; item += kJoinThreads * gridDim.z) {
         const int r = item / quads, e = (item - r * quads) * 4;
