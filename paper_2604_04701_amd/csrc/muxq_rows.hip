@@ -56,6 +56,15 @@ __device__ __forceinline__ float weight_of(float m, float l, float top) { return
 // What the sum of the values is multiplied by in the end.
 __device__ __forceinline__ float factor_of(float m, float l) { return m != kFloor ? 1.0f / l : l == 0.0f ? 0.0f : __builtin_nanf(""); }
 
+// 16 bytes of each lane to LDS, one lane behind the other from `to` on, which is the same for all of them.  (Written out, so that reads of
+// the other tile do not wait for it; wait_for_memory() does.)
+__device__ __forceinline__ void to_lds(const char *from, char *to)
+{
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(at), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void wait_for_memory() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // How the work is divided: a workgroup to a sequence, key-value head, tile of rows and piece of `tiles` tiles of tokens.  Rows that
 // see no more tiles than that are finished by their first piece; the others leave parts in the workspace.
 struct Plan {
@@ -212,11 +221,15 @@ template <int kD, bool kInt8, int kWaves, int kWR, int kTT>
 __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void k_rows(RowsArgs a, Plan plan)
 {
     constexpr int kThreads = 64 * kWaves, kWT = kWaves / kWR, kR = 32 * kWR, kNB = kTT / kWT / 32;          // waves along tokens; rows; blocks of 32 tokens of a wave
-    constexpr int kKeyRow = 2 * kD + 16, kValueRow = 2 * kD + 32;                   // bytes of a row in LDS
+    // fp16 of many rows: memory writes to LDS by itself, into one of two tiles; its rows are not longer then, but their 16-byte pieces
+    // change places by the row's number, for the same end.
+    constexpr bool kDirect = !kInt8 && kWR == 4;
+    constexpr int kKeyRow = kDirect ? 2 * kD : 2 * kD + 16, kValueRow = kDirect ? 2 * kD : 2 * kD + 32;                   // bytes of a row in LDS
+    constexpr int kTile = kTT * (kKeyRow + kValueRow);
     constexpr int kCH = kInt8 ? kD / 16 : kD / 8, kTPP = kThreads / kCH, kP = kTT / kTPP;      // loads of a row, rows of a pass, passes
     constexpr bool kAllJoin = kWR == 1 && kD * 128 * kWaves <= kTT * (kKeyRow + kValueRow);       // all waves' parts fit the tile's LDS
     static_assert(kNB >= 1 && kP >= 1, "tile");
-    __shared__ __align__(16) char sh_k[kTT * (kKeyRow + kValueRow)];
+    __shared__ __align__(1024) char sh_k[kTile * (kDirect ? 2 : 1)];
     char *const sh_v = sh_k + kTT * kKeyRow;
     f32x4 *const sh_o = (f32x4 *)sh_k;
     __shared__ long long sh_at[kChunk * (kTT / 8)];           // where runs of rows stand, in bytes; 0 for those that are nowhere
@@ -253,6 +266,8 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
         }
     };
 
+    if (kDirect && d != kD)              // dimensions that nothing is written to
+        for (int x = tid; x < (int)sizeof(sh_k) / 16; x += kThreads) ((u32x4 *)sh_k)[x] = u32x4{};
     int parent = 0;
     if (tree && tid < w.n) parent = a.parents[w.first + tid];
     find_pages(j0, min(j1, j0 + kChunk));
@@ -286,8 +301,13 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     const int lane_row = tid / kCH, piece_of = tid % kCH;
     const bool live = piece_of * (kInt8 ? 16 : 8) < d;
     // (rows of a run stand in one page and belong to one pass)
+    // (in LDS the lane's piece is of other dimensions, by the row, where pieces change places)
+    const int piece_k = kDirect ? piece_of ^ (lane_row & 7) : piece_of, piece_v = kDirect ? piece_of ^ ((lane_row & 3) << 1) : piece_of;
+    const bool live_k = piece_k * 8 < d, live_v = piece_v * 8 < d;
+    const long long lane_row_at = (long long)(lane_row & ((1 << run_shift) - 1)) * a.c.ld_token * 2;
+    const long long lane_at_k = lane_row_at + piece_k * 16, lane_at_v = lane_row_at + piece_v * 16;
     const long long lane_at = ((long long)(lane_row & ((1 << run_shift) - 1)) * a.c.ld_token + (live ? piece_of : 0) * (kInt8 ? 16 : 8)) * (kInt8 ? 1 : 2);
-    u32x4 k[kP], v[kP];
+    u32x4 k[kDirect ? 1 : kP], v[kDirect ? 1 : kP];
     float scale_k = 0.0f, scale_v = 0.0f;
     bool bad = false, edge = false;
     int jc = j0, t_next = 0, slot_next = 0;
@@ -298,9 +318,14 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
         edge = bad || t_next + kTT > w.t1;
 #pragma unroll
         for (int x = 0; x < kP; ++x) {
-            const long long at = sh_at[slot_next + ((x * kTPP + lane_row) >> run_shift)] + lane_at;
-            k[x] = *(const u32x4 *)(a.c.k + at);
-            v[x] = *(const u32x4 *)(a.c.v + at);
+            const long long at = sh_at[slot_next + ((x * kTPP + lane_row) >> run_shift)] + (kDirect ? 0 : lane_at);
+            if constexpr (kDirect) {
+                if (live_k) to_lds(a.c.k + (at + lane_at_k), sh_k + (j & 1) * kTile + (x * kWaves + wave) * 1024);
+                if (live_v) to_lds(a.c.v + (at + lane_at_v), sh_v + (j & 1) * kTile + (x * kWaves + wave) * 1024);
+            } else {
+                k[x] = *(const u32x4 *)(a.c.k + at);
+                v[x] = *(const u32x4 *)(a.c.v + at);
+            }
         }
         if (kInt8 && tid < kTT) {
             const int page = max(0, sh_page[slot_next + (tid >> run_shift)]);
@@ -308,6 +333,30 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
             scale_k = a.c.k_scale[at];
             scale_v = a.c.v_scale[at];
         }
+    };
+    // Of a tile that memory wrote to LDS: values of rows that are nowhere become 0, where care is taken infinite and NaN ones too.
+    auto mend = [&](int j) {
+        bool found = false;
+        const int t0 = w.tile_of(j) * kTT, slot = (j - jc) << e_shift;
+#pragma unroll
+        for (int x = 0; x < kP; ++x) {
+            const int in = x * kTPP + lane_row;
+            u32x4 *const at = (u32x4 *)(sh_v + (j & 1) * kTile) + x * kThreads + tid;
+            u32x4 y = *at;
+            if (t0 + in >= w.t1 || sh_page[slot + (in >> run_shift)] < 0) {
+                y = u32x4{};
+            } else if (careful) {
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    const uint32_t was = y[z];
+                    if ((was & 0x7c00u) == 0x7c00u) y[z] &= 0xffff0000u;
+                    if ((was & 0x7c000000u) == 0x7c000000u) y[z] &= 0xffffu;
+                    found |= y[z] != was;
+                }
+            }
+            *at = y;
+        }
+        if (careful && __any(found)) sh_found = 1;
     };
     // the tile that is on its way to LDS; where care is taken without its infinite and NaN values
     auto store = [&]() {
@@ -356,6 +405,14 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
         if (careful && __any(found)) sh_found = 1;
     };
 
+    int turn_k[4], turn_v[2];           // where a lane's pieces of a row begin
+    if constexpr (kDirect) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) turn_k[x] = ((2 * x + half) ^ (col & 7)) * 16;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) turn_v[x] = ((4 * x + ((lane & 16) >> 3) + ((lane & 3) >> 1)) ^ ((lane >> 2 & 3) << 1)) * 16 + (lane & 1) * 8;
+    }
+
     auto compute = [&](int j) {
         const int t0 = w.tile_of(j) * kTT + wt * (32 * kNB), slot = (j - jc) << e_shift;
         // nothing, or all of it, to be seen by the wave's rows
@@ -369,8 +426,9 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
             all = all && t9 <= p_lo && (!a.window || (long long)t0 > (long long)p_hi - a.window || t9 < a.sinks);
         }
         f32x16 acc[kNB] = {};
-        const char *const keys = sh_k + (wt * kNB * 32 + col) * kKeyRow + half * 16;
-        const char *const values = sh_v + (wt * kNB * 32 + 4 * half + ((lane & 15) >> 2)) * kValueRow + ((lane & 16) + 4 * (lane & 3)) * 2;
+        const int tile_at = kDirect ? (j & 1) * kTile : 0;
+        const char *const keys = sh_k + tile_at + (wt * kNB * 32 + col) * kKeyRow + (kDirect ? 0 : half * 16);
+        const char *const values = sh_v + tile_at + (wt * kNB * 32 + 4 * half + ((lane & 15) >> 2)) * kValueRow + (kDirect ? 0 : ((lane & 16) + 4 * (lane & 3)) * 2);
         // A block is 32 tokens: kQ products with its keys, kQ with its values, and 16 weights of a lane between them.  While a block is
         // weighed, the products with the keys of the next one and with the values of the last one go on; reads of LDS are kAhead products in
         // front of theirs.  (In the compiler's own order each product waits for its read, and the weights for all of them.)
@@ -380,10 +438,13 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
         s16x8 value[kAhead];
         uint32_t weights[2][8];
         f32x4 vs[4];
-        auto ask_key = [&](int b, int x) { key[x % kAhead] = *(const f16x8 *)(keys + b * 32 * kKeyRow + x * 32); };
+        auto ask_key = [&](int b, int x) {
+            key[x % kAhead] = *(const f16x8 *)(keys + b * 32 * kKeyRow + (kDirect ? turn_k[x & 3] + (x >> 2) * 128 : x * 32));
+        };
         auto ask_value = [&](int b, int x) {
             // rows 4 half + 0..3 of 16 tokens, and 8 rows on, 32 dimensions
-            const char *const at = values + (b * 32 + x / (kD / 32) * 16) * kValueRow + x % (kD / 32) * 64;
+            const int y = x % (kD / 32);
+            const char *const at = values + (b * 32 + x / (kD / 32) * 16) * kValueRow + (kDirect ? turn_v[y & 1] + (y >> 1) * 128 : y * 64);
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad)(at + 8 * kValueRow));
             value[x % kAhead] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
@@ -544,9 +605,18 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
             load(jc);
             if (jc == j0) row.above = tree ? nodes_above(sh_parents, row.i) : 0;
             for (int j = jc; j < j9; ++j) {
-                if (j > j0) __syncthreads();              // readers of the tile before
-                store();
-                __syncthreads();
+                if constexpr (kDirect) {
+                    wait_for_memory();
+                    __syncthreads();                          // the tile is there, and the readers of the one before are through
+                    if (edge || careful) {
+                        mend(j);
+                        __syncthreads();
+                    }
+                } else {
+                    if (j > j0) __syncthreads();              // readers of the tile before
+                    store();
+                    __syncthreads();
+                }
                 if (careful && tid == 0 && sh_found) {
                     if (sh_n_loose < kLoose) sh_loose[sh_n_loose] = j;
                     ++sh_n_loose;
