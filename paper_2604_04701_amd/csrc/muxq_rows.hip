@@ -759,16 +759,34 @@ __global__ __launch_bounds__(kJoinThreads) void k_rows_join(RowsArgs a, Plan pla
     const long long part = (((long long)w.s * a.c.n_kv_heads + w.kvh) * plan.row_tiles + blockIdx.x / a.c.n_kv_heads) * plan.pieces * rows;
     for (int item = threadIdx.x + kJoinThreads * blockIdx.z; item < n_rows * quads; item += kJoinThreads * gridDim.z) {
         const int r = item / quads, e = (item - r * quads) * 4;
+        // eight parts on their way at a time, the last one again where there are fewer (a maximum more does not change, a weight counts as 0)
         float top = kFloor, total = 0.0f;
-        for (int x = 0; x < pieces; ++x) top = fmaxf(top, plan.ml[part + (long long)x * rows + r].x);
         f32x4 sum = {};
-        for (int x = 0; x < pieces; ++x) {
-            const long long at = part + (long long)x * rows + r;
-            const float2 ml = plan.ml[at];
-            const float f = weight_of(ml.x, ml.y, top);
-            total += f * ml.y;
-            sum += f * *(const f32x4 *)(plan.o + at * d + e);
+        for (int x0 = 0; x0 < pieces; x0 += 8) {
+            float2 ml[8];
+            f32x4 v[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const long long at = part + (long long)min(x0 + x, pieces - 1) * rows + r;
+                ml[x] = plan.ml[at];
+                v[x] = *(const f32x4 *)(plan.o + at * d + e);
+            }
+            float to = top;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) to = fmaxf(to, ml[x].x);
+            const float keep = weight_of(top, total, to);
+            total *= keep;
+            sum *= keep;
+            top = to;
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+                if (x0 + x < pieces) {
+                    const float f = weight_of(ml[x].x, ml[x].y, top);
+                    total += f * ml[x].y;
+                    sum += f * v[x];
+                }
         }
+        if (top == kFloor && total > 0.0f) total = kNone;
         const int i = w.i_lo + (local0 + r) / a.group, head = w.kvh * a.group + (local0 + r) % a.group;
         *(f16x4 *)(a.o + (long long)(w.first + i) * a.ldo + (long long)head * d + e) = __builtin_convertvector(sum * factor_of(top, total), f16x4);
     }
@@ -783,7 +801,10 @@ struct Form {
     int pieces, tiles;
 };
 
-constexpr int kFill = 512, kLeast = 4;        // workgroups that fill the chip; tiles of a piece, at least
+// Workgroups that fill the chip, of 32 rows and heads of more than 64 dimensions twice as many; tiles of a piece, at least.  (22 trees of 20
+// nodes, 16 heads of 96, to 4571 tokens, codes: 78 us with 3 pieces each, 104 with 2; 5 of 15 nodes, 12 heads of 80, 4580 tokens, fp16: 38
+// us with 9 pieces, 45 with 17, which cost more to join than they gain.)
+constexpr int kFill = 512, kLeast = 4;
 
 // Tiles of `tile` tokens that a workgroup's rows see at most, `span` tokens being its own.
 long long tiles_seen(int max_length, int window, int sinks, long long span, int tile)
@@ -811,8 +832,9 @@ Form form_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int 
     const long long tiles = tiles_seen(max_length, window, sinks, std::min((long long)max_new, (long long)f.rows / group + 2), f.tile);
     f.pieces = 1;
     f.tiles = (int)tiles;
-    if (f.groups < kFill && tiles >= 2 * kLeast) {
-        const long long want = std::min((kFill + f.groups - 1) / f.groups, tiles / kLeast);
+    const long long twice = f.rows == 32 && head_dim > 64 ? std::min((2 * kFill + f.groups - 1) / f.groups, 8ll) : 1;
+    const long long want = std::min(std::max((kFill + f.groups - 1) / f.groups, twice), tiles / kLeast);
+    if (want > 1) {
         f.tiles = (int)((tiles + want - 1) / want);
         f.pieces = (int)((tiles + f.tiles - 1) / f.tiles);
     }
@@ -853,13 +875,13 @@ size_t rows_workspace_need(int S, int n_heads, int n_kv_heads, int head_dim, int
     return f.pieces > 1 ? bytes_of((size_t)f.groups * f.pieces * f.rows, head_dim) : 0;
 }
 
-// Enough for every smaller call: where a call is cut, all its workgroups are fewer than 2 kFill.
+// Enough for every smaller call: where a call is cut, all its workgroups are fewer than 4 kFill.
 size_t rows_workspace_bytes(int, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length, int window, int sinks, bool)
 {
     const long long most = (long long)max_new * (n_heads / n_kv_heads);
     const int rows = head_dim > 128 || most > 64 ? 128 : most > 32 ? 64 : 32;
     if (tiles_seen(max_length, window, sinks, std::min(max_new, 130), head_dim > 128 ? 32 : 64) < 2 * kLeast) return 0;
-    return bytes_of((size_t)2 * kFill * rows, head_dim);
+    return bytes_of((size_t)4 * kFill * rows, head_dim);
 }
 
 hipError_t rows_prepare()
