@@ -42,10 +42,20 @@ class Block:
         for x in (ks, vs):
             if x is not None:
                 x.fill_(0.025)
+        self.alloc_room(S, max_tokens)
+
+    def alloc_room(self, S, max_tokens):
+        """Workspaces for S rows."""
+        K, heads = self.K, self.heads
+        self.S = S
         self.ws_attn, self.lay = B.alloc_workspace(S, K, 3 * K, 64), B.workspace_layout(S, K, 3 * K, 64)
         self.ws_proj = B.alloc_workspace(S, K, K, 64)
         self.ws_mlp = torch.empty(B.lib().muxq_mlp_workspace_bytes(S, K, 4 * K, K, 64), dtype=torch.uint8, device=DEV)
         self.ws_kv = B.alloc_attention_workspace(S, heads, heads, self.d, max_tokens)
+
+    def attend(self, q, batch):
+        k, v, ks, vs = self.cache
+        return B.muxq_paged_attention(q, k, v, batch.table, batch.lengths, batch.max_tokens, k_scale=ks, v_scale=vs, workspace=self.ws_kv)
 
     def step(self, x, stream, batch):
         """x: what the block before adds to the residual stream (or, with stream None, the stream itself).  Returns the
@@ -60,7 +70,7 @@ class Block:
         tuned = B.muxq_lora(h, self.A, self.B, self.scales, batch.starts, batch.adapters, qkv)
         q, kk, vv = tuned.view(S, 3 * self.heads, self.d).split(self.heads, 1)
         q = B.muxq_kv_append(kk, vv, batch.slots, k, v, k_scale=ks, v_scale=vs, q=q, positions=batch.positions, cos_sin=batch.cos_sin)
-        o = B.muxq_paged_attention(q, k, v, batch.table, batch.lengths, batch.max_tokens, k_scale=ks, v_scale=vs, workspace=self.ws_kv)
+        o = self.attend(q, batch)
         w, s, b = self.c_proj
         a = B.muxq_linear(o.view(S, K), w, s, K, "channel", bias=b, workspace=self.ws_proj)
         h2, stream2 = B.muxq_norm(a, *self.ln[1], residual=stream)

@@ -37,3 +37,10 @@ def test_no_token_beyond_the_bound(monkeypatch, most):
 def test_no_sequence_beyond_the_bound(monkeypatch):
     with pytest.raises(ValueError, match="32"):
         make(monkeypatch, [3, 32], 32)
+
+
+def test_trees_of_a_draft():
+    from paper_2604_04701_amd.draft_step import tree
+    assert tree(1, 3) == ([-1], [0])
+    assert tree(6, 2) == ([-1, 0, 0, 1, 1, 2], [0, 1, 1, 2, 2, 2])
+    assert tree(4, 1) == ([-1, 0, 1, 2], [0, 1, 2, 3])
