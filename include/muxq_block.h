@@ -69,8 +69,8 @@ int muxq_kv_append(const void *K_fp16, const void *V_fp16, int M, int ldk, int l
                    const int32_t *positions, const float *cos_sin, int n_positions, int rot_dim,
                    int interleaved, const muxq_kv_cache *cache, void *stream);
 
-/* The other way: rows of the cache as fp16 (codes times scale in binary32, rounded once), e.g. the
- * cached prefix of a prompt for a caller's own attention over it (there is none for prompts here).  K_out, V_out: M rows of
+/* The other way: rows of the cache as fp16 (codes times scale in binary32, rounded once), e.g. a
+ * cached prefix for a caller's own use of it.  K_out, V_out: M rows of
  * n_kv_heads * head_dim, row strides ldk, ldv.  Rows of slots outside the cache are zeros. */
 int muxq_kv_gather(const int32_t *slots, int M, const muxq_kv_cache *cache, void *K_out_fp16, int ldk,
                    void *V_out_fp16, int ldv, void *stream);
@@ -197,7 +197,7 @@ int muxq_tree_attention(const void *Q_fp16, int M, int n_heads, int ldq, const m
  * A drafted token outside [0, V) is not accepted and leaves r as it is.  Probabilities need not sum to 1; infinite, NaN or
  * negative ones give unspecified tokens within [-1, V).
  * path: int32 [M], the accepted nodes of sequence s, as numbers within it, at starts[s] + j (0 first), -1 behind them; counts: int32 [S], how
- * many; next_token: int32 [S].  A sequence without rows gives a count of 0 and a token of -1.  1 <= V <= 2^22, strides
+ * many; next_token: int32 [S]; the three share no memory with each other or with what is read.  A sequence without rows gives a count of 0 and a token of -1.  1 <= V <= 2^22, strides
  * below 2^31. */
 int muxq_verify_tree(const float *target, int ldt, const float *draft, int ldd, int M, int V, const int32_t *tokens,
                      const int32_t *parents, const float *uniforms, const int32_t *starts, int S, int max_nodes,

@@ -838,6 +838,16 @@ def muxq_norm(x, weight, bias=None, residual=None, residual_scale=1.0, post_weig
 
 # ---- several new tokens of a sequence ----------------------------------------------------------
 
+def _together(what, *tensors):
+    """All on one device, the current one, whose stream the call goes to."""
+    at = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            _refuse(f"{what}: tensors of several devices")
+    if at >= 0 and at != torch._C._cuda_getDevice():
+        _refuse(f"{what}: the tensors are on device {at}, the current one is {torch._C._cuda_getDevice()}")
+
+
 def alloc_window_attention_workspace(S, n_heads, n_kv_heads, head_dim, max_new, max_length, window=0, sinks=0, device="cuda"):
     """Workspace of muxq_window_attention, also good for fewer sequences and tokens and smaller windows (empty where none is needed)."""
     n = lib().muxq_window_attention_workspace_bytes(S, n_heads, n_kv_heads, head_dim, max_new, max_length, window, sinks)
@@ -866,6 +876,7 @@ def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_leng
         _rows(q, "q"), _rows(out, "out"), _flat(lengths, S, _I32, "lengths"), _flat(starts, S + 1, _I32, "starts")
         _refuse(f"{what}: q, out and the cache differ in head size, starts has not one entry more than lengths, or block_table is no "
                 "int32 GPU tensor [S, pages] with contiguous rows of max_length tokens")
+    _together(what, q, out, k_cache, v_cache, k_scale, v_scale, block_table, starts, lengths)
     return c, out, os[0], S, (q.data_ptr(), M, n_heads, qs[0], C.byref(c), block_table.data_ptr(),
                               ts[0] if S > 1 else block_table.shape[1], starts.data_ptr(), lengths.data_ptr())
 
@@ -892,6 +903,7 @@ def muxq_tree_attention(q, k_cache, v_cache, block_table, starts, lengths, paren
     sequence, -1 for a root.  max_nodes: a bound on the nodes of a tree, at most 64."""
     c, out, ldo, S, args = _rows_args("muxq_tree_attention", q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale,
                                       v_scale, out)
+    _together("muxq_tree_attention", q, parents)
     args += (_flat(parents, q.shape[0], _I32, "parents"), S, max_nodes, max_length, c.head_dim ** -0.5 if scale is None else scale,
              out.data_ptr(), ldo)
     _call(lib().muxq_tree_attention, args, workspace, _stream(),
@@ -913,6 +925,7 @@ def muxq_verify_tree(target, tokens, starts, parents, max_nodes, draft=None, uni
     for name, t in (("target", target), ("draft", draft)):
         if t is not None and (t.dtype is not _F32 or not t.is_cuda or t.dim() != 2 or t.shape != (M, V) or (t.stride(1) != 1 and V > 1)):
             _refuse(f"{name}: a GPU tensor of float [{M}, {V}] with contiguous rows is expected")
+    _together("muxq_verify_tree", target, tokens, starts, parents, draft, uniforms, path, counts, next_token)
     # (a dimension of one element may carry any stride)
     ldt = target.stride(0) if M > 1 else V
     ldd = 0 if draft is None else draft.stride(0) if M > 1 else V
@@ -934,6 +947,7 @@ def muxq_kv_copy(src, dst, k_cache, v_cache, k_scale=None, v_scale=None):
     n = src.numel()
     if dst.numel() != n:
         _refuse("muxq_kv_copy: src and dst differ in length")
+    _together("muxq_kv_copy", k_cache, v_cache, k_scale, v_scale, src, dst)
     status = lib().muxq_kv_copy(_flat(src, n, _I32, "src"), _flat(dst, n, _I32, "dst"), n, C.byref(c), _stream())
     if status != 0:
         _check(status, "muxq_kv_copy")
@@ -946,6 +960,7 @@ def muxq_kv_compact(path, counts, starts, lengths, block_table, k_cache, v_cache
     S, M = counts.numel(), path.numel()
     if block_table.dtype is not _I32 or not block_table.is_cuda or block_table.dim() != 2 or block_table.shape[0] != S or block_table.stride(1) != 1:
         _refuse("muxq_kv_compact: block_table is no int32 GPU tensor [S, pages] with contiguous rows")
+    _together("muxq_kv_compact", k_cache, v_cache, k_scale, v_scale, path, counts, starts, lengths, block_table)
     status = lib().muxq_kv_compact(_flat(path, M, _I32, "path"), _flat(counts, S, _I32, "counts"), _flat(starts, S + 1, _I32, "starts"),
                                    _flat(lengths, S, _I32, "lengths"), block_table.data_ptr(),
                                    block_table.stride(0) if S > 1 else block_table.shape[1], M, S, max_nodes, C.byref(c), _stream())

@@ -364,6 +364,12 @@ int muxq_verify_tree(const float *target, int ldt, const float *draft, int ldd, 
     for (const void *p : {(const void *)target, (const void *)draft, (const void *)tokens, (const void *)parents, (const void *)uniforms,
                           (const void *)starts, (const void *)path, (const void *)counts, (const void *)next_token})
         if (!aligned(p, 4)) return MUXQ_ERR_ALIGN;
+    // (path is written while tokens are still read, by other workgroups too)
+    const struct { const void *p; long long n; } own[] = {{path, M}, {counts, S}, {next_token, S}, {tokens, M}, {parents, M}, {starts, S + 1}, {uniforms, M}};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 7; ++j)
+            if (own[j].p && (uintptr_t)own[i].p < (uintptr_t)own[j].p + 4 * own[j].n && (uintptr_t)own[j].p < (uintptr_t)own[i].p + 4 * own[i].n)
+                return MUXQ_ERR_PARAM;
     muxq::VerifyArgs a{};
     a.target = target;
     a.draft = uniforms ? draft : nullptr;

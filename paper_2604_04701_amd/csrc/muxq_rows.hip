@@ -204,6 +204,7 @@ __device__ void put_loose(const RowsArgs &a, const Span<kTT> &w, int j0, int j1,
                 if (kInt8) score *= a.c.k_scale[at_s];
                 for (int y = 0; y < 4; ++y)
                     if (zero[y] != 0.0f) sum[y] += score == kFloor ? 0.0f * v[y] : v[y];
+                if (sum[0] != sum[0] && sum[1] != sum[1] && sum[2] != sum[2] && sum[3] != sum[3]) x = n, t = w.t1;      // NaN stays
             }
         }
         for (int y = 0; y < 4; ++y)

@@ -59,6 +59,22 @@ def test_head_sizes(d, layout, bits):
     check_window(Case(d, [40, 1, 130], [100, 300, 130], 6, 2, d, 16, bits, layout, columns=True), 90, 3, what=f"d={d}")
 
 
+# batches that fill the chip with tiles of 64 and of 128 rows
+FULL = {"rows128": ([150] * 9 + [131, 140, 150], [150 + 31 * i for i in range(12)], 32, 16, 128), "rows128_d80": ([150] * 12, [400] * 11 + [150], 32, 16, 80),
+        "rows128_d64": ([100] * 12, [100 + 50 * i for i in range(12)], 48, 24, 64), "rows64": ([60, 33] * 20, [60, 333] * 20, 16, 16, 64),
+        "rows64_d128": ([60, 64] * 20, [160, 64] * 20, 16, 16, 128), "heads256": ([100] * 4, [100, 130, 333, 1000], 12, 6, 256)}
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("win,sinks", [(0, 0), (70, 5)])
+@pytest.mark.parametrize("layout", ["heads", "tokens"])
+@pytest.mark.parametrize("name", FULL)
+def test_full_batches(name, layout, win, sinks, bits):
+    new, lengths, H, heads, d = FULL[name]
+    say(f"[case] full {name} {layout} window={win} sinks={sinks} bits={bits}")
+    check_window(Case(13, new, lengths, H, heads, d, 32, bits, layout), win, sinks, what=name)
+
+
 @pytest.mark.parametrize("H,heads", [(1, 1), (5, 1), (32, 1), (40, 1), (12, 4), (130, 2)])
 def test_groups(H, heads):
     say(f"[case] window {H} of {heads}")

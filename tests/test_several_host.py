@@ -24,7 +24,7 @@ def rows(c=None, tree=False, **kw):
 
 def verify(**kw):
     a = dict(target=FAKE, ldt=100, draft=FAKE, ldd=100, M=10, V=100, tokens=FAKE, parents=FAKE, uniforms=FAKE, starts=FAKE, S=4, nodes=8,
-             path=AWAY, counts=AWAY, next=AWAY)
+             path=AWAY, counts=AWAY + 64, next=AWAY + 128)
     assert not set(kw) - set(a)
     a.update(kw)
     return B.lib().muxq_verify_tree(*a.values(), None)
@@ -70,7 +70,8 @@ def test_caches_that_are_refused(kw, status):
     (dict(target=None), 1), (dict(tokens=None), 1), (dict(parents=None), 1), (dict(starts=None), 1), (dict(path=None), 1), (dict(counts=None), 1),
     (dict(next=None), 1), (dict(M=0), 2), (dict(M=(1 << 24) + 1), 2), (dict(S=0), 2), (dict(S=65536), 2), (dict(V=0, ldt=0), 2), (dict(ldt=99), 2),
     (dict(V=(1 << 22) + 1, ldt=1 << 23, ldd=1 << 23), 2), (dict(ldd=99), 2), (dict(nodes=0), 2), (dict(nodes=65), 2), (dict(target=FAKE + 2), 3),
-    (dict(draft=FAKE + 1), 3), (dict(uniforms=FAKE + 2), 3), (dict(tokens=FAKE + 3), 3), (dict(path=AWAY + 2), 3)])
+    (dict(draft=FAKE + 1), 3), (dict(uniforms=FAKE + 2), 3), (dict(tokens=FAKE + 3), 3), (dict(path=AWAY + 2), 3),
+    (dict(path=FAKE + 36), 4), (dict(counts=AWAY + 36), 4), (dict(next=AWAY + 76), 4), (dict(next=AWAY - 12), 4), (dict(starts=AWAY + 76), 4)])
 def test_verification_refuses(kw, status):
     assert verify(**kw) == status
 
@@ -197,3 +198,29 @@ def test_tensors_that_the_pages_refuse(calls):          # noqa: F811
     assert calls == []
     B.muxq_kv_compact(**good)
     assert calls[0][0] == "muxq_kv_compact"
+
+
+def test_tensors_of_other_devices_are_refused(calls, monkeypatch):          # noqa: F811
+    class There(type(gpu(1))):
+        at = 0
+
+        def get_device(self):
+            return self.at
+
+    def there(t, at=0):
+        t = t.as_subclass(There)
+        t.at = at
+        return t
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    a = attention_args()
+    with pytest.raises(B.MuxqError, match="several devices"):
+        B.muxq_window_attention(**{**a, "lengths": there(a["lengths"])}, max_new=2)
+    for q, rest in ((0, 0), (1, 1)):
+        b = {n: there(x, q) if torch.is_tensor(x) else x for n, x in a.items()}
+        if q == 0:
+            with pytest.raises(B.MuxqError, match="current"):
+                B.muxq_window_attention(**b, max_new=2)
+            assert calls == []
+        else:
+            B.muxq_window_attention(**b, max_new=2)
+            assert len(calls) == 1
