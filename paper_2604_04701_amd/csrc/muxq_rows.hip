@@ -269,10 +269,6 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
 
     if (kDirect && d != kD)              // dimensions that nothing is written to
         for (int x = tid; x < (int)sizeof(sh_k) / 16; x += kThreads) ((u32x4 *)sh_k)[x] = u32x4{};
-    int parent = 0;
-    if (tree && tid < w.n) parent = a.parents[w.first + tid];
-    find_pages(j0, min(j1, j0 + kChunk));
-    if (tree && tid < w.n) sh_parents[tid] = parent;
     const int local0 = w.local0, n_rows = w.n_rows;
     Row row;
     row.find(a, w.kvh, w.n, w.ctx, w.i_lo, local0 + min(wr * 32 + col, n_rows - 1));
@@ -287,9 +283,15 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
         const int e = 16 * x + 8 * half;
         q[x] = f16x8{};
         if (e < d) q[x] = *(const f16x8 *)(q_row + e);
-        if (a.scale < 0.0f) q[x] = -q[x];
-        if (a.scale == 0.0f) q[x] = q[x] * (_Float16)0.0f;
     }
+    // (all of the first loads on their way together)
+    int parent = 0;
+    if (tree && tid < w.n) parent = a.parents[w.first + tid];
+    find_pages(j0, min(j1, j0 + kChunk));
+    if (tree && tid < w.n) sh_parents[tid] = parent;
+    if (a.scale <= 0.0f)
+#pragma unroll
+        for (int x = 0; x < kD / 16; ++x) q[x] = a.scale < 0.0f ? -q[x] : q[x] * (_Float16)0.0f;
     const float c = a.scale == 0.0f ? 1.0f : fminf(fabsf(a.scale) * 1.44269504088896f, 3.0e38f);
 
     float m, total;
