@@ -838,14 +838,16 @@ def muxq_norm(x, weight, bias=None, residual=None, residual_scale=1.0, post_weig
 
 # ---- several new tokens of a sequence ----------------------------------------------------------
 
+# (get_device() is -1 for host memory: one comparison says that a tensor is on a GPU, and on the current one, whose stream the call
+# goes to.)
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+
+
 def _together(what, *tensors):
-    """All on one device, the current one, whose stream the call goes to."""
-    at = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and t.get_device() != at:
-            _refuse(f"{what}: tensors of several devices")
-    if at >= 0 and at != torch._C._cuda_getDevice():
-        _refuse(f"{what}: the tensors are on device {at}, the current one is {torch._C._cuda_getDevice()}")
+    """Says of tensors on GPUs why they are not all on the current one."""
+    at = {t.get_device() for t in tensors if t is not None}
+    if at != {_device()}:
+        _refuse(f"{what}: the tensors are on devices {sorted(at)}, the current one is {_device()}")
 
 
 def alloc_window_attention_workspace(S, n_heads, n_kv_heads, head_dim, max_new, max_length, window=0, sinks=0, device="cuda"):
@@ -860,7 +862,7 @@ def alloc_tree_attention_workspace(S, n_heads, n_kv_heads, head_dim, max_nodes, 
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale, v_scale, out):
+def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale, v_scale, out, parents=None):
     """The checks that both attentions of several new tokens share: (descriptor of the cache, out, arguments up to lengths)."""
     M, n_heads, d = q.shape
     c = _kv(k_cache, v_cache, k_scale, v_scale)
@@ -868,15 +870,19 @@ def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_leng
     if out is None:
         out = torch.empty((M, n_heads, d), dtype=torch.float16, device=q.device)
     qs, os, ts = q.stride(), out.stride(), block_table.stride()
-    if not (q.dtype is out.dtype is _F16 and block_table.dtype is lengths.dtype is starts.dtype is _I32 and q.is_cuda and out.is_cuda and
-            block_table.is_cuda and lengths.is_cuda and starts.is_cuda and d == c.head_dim and out.shape == q.shape and
+    if not (q.dtype is out.dtype is _F16 and block_table.dtype is lengths.dtype is starts.dtype is _I32 and
+            _device() == q.get_device() == out.get_device() == k_cache.get_device() == v_cache.get_device() == block_table.get_device() ==
+            lengths.get_device() == starts.get_device() and (k_scale is None or k_scale.get_device() == v_scale.get_device() == q.get_device()) and
+            (parents is None or (parents.dtype is _I32 and parents.get_device() == q.get_device() and parents.is_contiguous() and
+                                 parents.numel() == M)) and d == c.head_dim and out.shape == q.shape and
             qs[2] == os[2] == 1 and (n_heads == 1 or qs[1] == os[1] == d) and block_table.dim() == 2 and block_table.shape[0] == S and
             ts[1] == 1 and lengths.is_contiguous() and starts.is_contiguous() and starts.numel() == S + 1 and
             max_length <= block_table.shape[1] * c.block_size):
-        _rows(q, "q"), _rows(out, "out"), _flat(lengths, S, _I32, "lengths"), _flat(starts, S + 1, _I32, "starts")
+        _rows(q, "q"), _rows(out, "out"), _flat(lengths, S, _I32, "lengths"), _flat(starts, S + 1, _I32, "starts"), _flat(parents, M, _I32, "parents")
+        if block_table.is_cuda:
+            _together(what, q, out, k_cache, v_cache, k_scale, v_scale, block_table, starts, lengths, parents)
         _refuse(f"{what}: q, out and the cache differ in head size, starts has not one entry more than lengths, or block_table is no "
                 "int32 GPU tensor [S, pages] with contiguous rows of max_length tokens")
-    _together(what, q, out, k_cache, v_cache, k_scale, v_scale, block_table, starts, lengths)
     return c, out, os[0], S, (q.data_ptr(), M, n_heads, qs[0], C.byref(c), block_table.data_ptr(),
                               ts[0] if S > 1 else block_table.shape[1], starts.data_ptr(), lengths.data_ptr())
 
@@ -902,9 +908,8 @@ def muxq_tree_attention(q, k_cache, v_cache, block_table, starts, lengths, paren
     new tokens only itself and the nodes above it; parents (int32 [M]): the number of each node's parent within its
     sequence, -1 for a root.  max_nodes: a bound on the nodes of a tree, at most 64."""
     c, out, ldo, S, args = _rows_args("muxq_tree_attention", q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale,
-                                      v_scale, out)
-    _together("muxq_tree_attention", q, parents)
-    args += (_flat(parents, q.shape[0], _I32, "parents"), S, max_nodes, max_length, c.head_dim ** -0.5 if scale is None else scale,
+                                      v_scale, out, parents)
+    args += (parents.data_ptr(), S, max_nodes, max_length, c.head_dim ** -0.5 if scale is None else scale,
              out.data_ptr(), ldo)
     _call(lib().muxq_tree_attention, args, workspace, _stream(),
           lambda: alloc_tree_attention_workspace(S, q.shape[1], c.n_kv_heads, c.head_dim, max_nodes, max_length, q.device),
@@ -922,20 +927,25 @@ def muxq_verify_tree(target, tokens, starts, parents, max_nodes, draft=None, uni
     path = torch.empty(M, dtype=torch.int32, device=device) if path is None else path
     counts = torch.empty(S, dtype=torch.int32, device=device) if counts is None else counts
     next_token = torch.empty(S, dtype=torch.int32, device=device) if next_token is None else next_token
-    for name, t in (("target", target), ("draft", draft)):
-        if t is not None and (t.dtype is not _F32 or not t.is_cuda or t.dim() != 2 or t.shape != (M, V) or (t.stride(1) != 1 and V > 1)):
-            _refuse(f"{name}: a GPU tensor of float [{M}, {V}] with contiguous rows is expected")
-    _together("muxq_verify_tree", target, tokens, starts, parents, draft, uniforms, path, counts, next_token)
+    if not (target.dtype is _F32 and tokens.dtype is parents.dtype is starts.dtype is path.dtype is counts.dtype is next_token.dtype is _I32 and
+            _device() == target.get_device() == tokens.get_device() == parents.get_device() == starts.get_device() == path.get_device() ==
+            counts.get_device() == next_token.get_device() and
+            (target.stride(1) == 1 or V == 1) and tokens.is_contiguous() and parents.is_contiguous() and starts.is_contiguous() and
+            path.is_contiguous() and counts.is_contiguous() and next_token.is_contiguous() and tokens.numel() == parents.numel() == path.numel() == M and
+            counts.numel() == next_token.numel() == S and
+            (draft is None or (draft.dtype is _F32 and draft.get_device() == target.get_device() and draft.shape == (M, V) and (draft.stride(1) == 1 or V == 1))) and
+            (uniforms is None or (uniforms.dtype is _F32 and uniforms.get_device() == target.get_device() and uniforms.is_contiguous() and uniforms.numel() == M))):
+        _flat(tokens, M, _I32, "tokens"), _flat(parents, M, _I32, "parents"), _flat(starts, S + 1, _I32, "starts"), _flat(uniforms, M, _F32, "uniforms")
+        _flat(path, M, _I32, "path"), _flat(counts, S, _I32, "counts"), _flat(next_token, S, _I32, "next_token")
+        if target.is_cuda and (draft is None or draft.is_cuda):
+            _together("muxq_verify_tree", target, tokens, starts, parents, draft, uniforms, path, counts, next_token)
+        _refuse(f"muxq_verify_tree: target and draft are GPU tensors of float [{M}, {V}] with contiguous rows; tokens, parents and path have a number "
+                "for each row, counts and next_token for each sequence")
     # (a dimension of one element may carry any stride)
     ldt = target.stride(0) if M > 1 else V
     ldd = 0 if draft is None else draft.stride(0) if M > 1 else V
-    for name, t, n in (("path", path, M), ("counts", counts, S), ("next_token", next_token, S)):
-        if t.numel() != n:
-            _refuse(f"{name}: {n} entries are expected")
-    status = lib().muxq_verify_tree(target.data_ptr(), ldt, _p(draft), ldd, M, V, _flat(tokens, M, _I32, "tokens"),
-                                    _flat(parents, M, _I32, "parents"), _flat(uniforms, M, _F32, "uniforms"),
-                                    _flat(starts, S + 1, _I32, "starts"), S, max_nodes, _flat(path, M, _I32, "path"),
-                                    _flat(counts, S, _I32, "counts"), _flat(next_token, S, _I32, "next_token"), _stream())
+    status = lib().muxq_verify_tree(target.data_ptr(), ldt, _p(draft), ldd, M, V, tokens.data_ptr(), parents.data_ptr(), _p(uniforms),
+                                    starts.data_ptr(), S, max_nodes, path.data_ptr(), counts.data_ptr(), next_token.data_ptr(), _stream())
     if status != 0:
         _check(status, "muxq_verify_tree")
     return path, counts, next_token
@@ -945,10 +955,14 @@ def muxq_kv_copy(src, dst, k_cache, v_cache, k_scale=None, v_scale=None):
     """Pages dst[i] of the cache become copies of pages src[i] (int32 [n]; pairs with a page outside it are left out)."""
     c = _kv(k_cache, v_cache, k_scale, v_scale)
     n = src.numel()
-    if dst.numel() != n:
+    if not (src.dtype is dst.dtype is _I32 and _device() == src.get_device() == dst.get_device() == k_cache.get_device() == v_cache.get_device() and
+            (k_scale is None or k_scale.get_device() == v_scale.get_device() == src.get_device()) and
+            src.is_contiguous() and dst.is_contiguous() and dst.numel() == n):
+        _flat(src, n, _I32, "src"), _flat(dst, n, _I32, "dst")
+        if dst.numel() == n:
+            _together("muxq_kv_copy", k_cache, v_cache, k_scale, v_scale, src, dst)
         _refuse("muxq_kv_copy: src and dst differ in length")
-    _together("muxq_kv_copy", k_cache, v_cache, k_scale, v_scale, src, dst)
-    status = lib().muxq_kv_copy(_flat(src, n, _I32, "src"), _flat(dst, n, _I32, "dst"), n, C.byref(c), _stream())
+    status = lib().muxq_kv_copy(src.data_ptr(), dst.data_ptr(), n, C.byref(c), _stream())
     if status != 0:
         _check(status, "muxq_kv_copy")
 
@@ -958,11 +972,18 @@ def muxq_kv_compact(path, counts, starts, lengths, block_table, k_cache, v_cache
     cache; starts, lengths (the nodes among them) and block_table as muxq_tree_attention takes them."""
     c = _kv(k_cache, v_cache, k_scale, v_scale)
     S, M = counts.numel(), path.numel()
-    if block_table.dtype is not _I32 or not block_table.is_cuda or block_table.dim() != 2 or block_table.shape[0] != S or block_table.stride(1) != 1:
-        _refuse("muxq_kv_compact: block_table is no int32 GPU tensor [S, pages] with contiguous rows")
-    _together("muxq_kv_compact", k_cache, v_cache, k_scale, v_scale, path, counts, starts, lengths, block_table)
-    status = lib().muxq_kv_compact(_flat(path, M, _I32, "path"), _flat(counts, S, _I32, "counts"), _flat(starts, S + 1, _I32, "starts"),
-                                   _flat(lengths, S, _I32, "lengths"), block_table.data_ptr(),
+    if not (path.dtype is counts.dtype is starts.dtype is lengths.dtype is block_table.dtype is _I32 and
+            _device() == path.get_device() == counts.get_device() == starts.get_device() == lengths.get_device() == block_table.get_device() ==
+            k_cache.get_device() == v_cache.get_device() and (k_scale is None or k_scale.get_device() == v_scale.get_device() == path.get_device()) and
+            path.is_contiguous() and counts.is_contiguous() and
+            starts.is_contiguous() and lengths.is_contiguous() and starts.numel() == S + 1 and lengths.numel() == S and block_table.dim() == 2 and
+            block_table.shape[0] == S and block_table.stride(1) == 1):
+        _flat(path, M, _I32, "path"), _flat(counts, S, _I32, "counts"), _flat(starts, S + 1, _I32, "starts"), _flat(lengths, S, _I32, "lengths")
+        if block_table.is_cuda:
+            _together("muxq_kv_compact", k_cache, v_cache, k_scale, v_scale, path, counts, starts, lengths, block_table)
+        _refuse("muxq_kv_compact: starts has one entry more than counts, lengths as many, and block_table is an int32 GPU tensor [S, pages] with "
+                "contiguous rows")
+    status = lib().muxq_kv_compact(path.data_ptr(), counts.data_ptr(), starts.data_ptr(), lengths.data_ptr(), block_table.data_ptr(),
                                    block_table.stride(0) if S > 1 else block_table.shape[1], M, S, max_nodes, C.byref(c), _stream())
     if status != 0:
         _check(status, "muxq_kv_compact")

@@ -6,10 +6,32 @@ import pytest
 import torch
 
 from paper_2604_04701_amd import binding as B
-from test_block_binding_host import calls, gpu          # noqa: F401
+from test_block_binding_host import Library
 from test_block_host import AWAY, FAKE, cache
 
 I32 = torch.int32
+
+
+class OnGpu(torch.Tensor):
+    """A tensor that passes for one on a GPU, the first one if it does not say otherwise."""
+    is_cuda = True
+    at = 0
+
+    def get_device(self):
+        return self.at
+
+
+def gpu(*shape, dtype=torch.float16):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    library = Library()
+    monkeypatch.setattr(B, "lib", lambda: library)
+    monkeypatch.setattr(B, "_stream", lambda: None)
+    monkeypatch.setattr(B, "_device", lambda: 0)
+    return library.calls
 
 
 def rows(c=None, tree=False, **kw):
@@ -201,26 +223,25 @@ def test_tensors_that_the_pages_refuse(calls):          # noqa: F811
 
 
 def test_tensors_of_other_devices_are_refused(calls, monkeypatch):          # noqa: F811
-    class There(type(gpu(1))):
-        at = 0
-
-        def get_device(self):
-            return self.at
-
-    def there(t, at=0):
-        t = t.as_subclass(There)
-        t.at = at
-        return t
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
-    a = attention_args()
-    with pytest.raises(B.MuxqError, match="several devices"):
-        B.muxq_window_attention(**{**a, "lengths": there(a["lengths"])}, max_new=2)
-    for q, rest in ((0, 0), (1, 1)):
-        b = {n: there(x, q) if torch.is_tensor(x) else x for n, x in a.items()}
-        if q == 0:
-            with pytest.raises(B.MuxqError, match="current"):
-                B.muxq_window_attention(**b, max_new=2)
-            assert calls == []
-        else:
-            B.muxq_window_attention(**b, max_new=2)
-            assert len(calls) == 1
+    kv = dict(k_cache=gpu(4, 2, 16, 64), v_cache=gpu(4, 2, 16, 64))
+    copies = dict(src=gpu(3, dtype=I32), dst=gpu(3, dtype=I32), **kv)
+    moved = dict(path=gpu(5, dtype=I32), counts=gpu(2, dtype=I32), starts=gpu(3, dtype=I32), lengths=gpu(2, dtype=I32), block_table=gpu(2, 3, dtype=I32),
+                 max_nodes=4, **kv)
+    for call, args in ((B.muxq_window_attention, dict(attention_args(), max_new=2)),
+                       (B.muxq_tree_attention, dict(attention_args(), max_nodes=2, parents=gpu(5, dtype=I32))),
+                       (B.muxq_verify_tree, verify_args()), (B.muxq_kv_copy, copies), (B.muxq_kv_compact, moved)):
+        tensors = [n for n, x in args.items() if torch.is_tensor(x)]
+        for name in tensors:
+            args[name].at = 1
+            with pytest.raises(B.MuxqError, match="devices"):
+                call(**args)
+            args[name].at = 0
+        assert calls == []
+        call(**args)
+        assert len(calls) == 1
+        monkeypatch.setattr(B, "_device", lambda: 1)
+        with pytest.raises(B.MuxqError, match="current"):
+            call(**args)
+        monkeypatch.setattr(B, "_device", lambda: 0)
+        assert len(calls) == 1
+        calls.clear()
