@@ -13,7 +13,7 @@ namespace muxq {
 namespace {
 
 constexpr long long kAtOnce = 8 << 20;          // numbers of a target whose rows are looked at all at once
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kBlock = 1024, kMaxBlocks = (1 << 22) / kBlock;
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kBlock = 1024;
 
 typedef float Four __attribute__((ext_vector_type(4), aligned(4)));        // rows of an odd vocabulary begin anywhere
 
@@ -55,18 +55,27 @@ struct Rest {
     const int *gone;            // without q: their tokens
 };
 
+// r of one token, from p and q there.
 __device__ __forceinline__ double less(const Rest &r, double x, double q, int t)
 {
-    if (r.rejected == 0) return x;
     if (r.q) {
-        x = fmax(x - q, 0.0);
+        if (r.rejected) x = fmax(x - q, 0.0);
         for (int j = 1; j < r.rejected; ++j) x = fmax(x * r.inv[j] - q, 0.0);
     } else {
+        // (what the earlier sums divide it by does not change its share: one number for all tokens)
         for (int j = 0; j < r.rejected; ++j)
             if (r.gone[j] == t) x = 0.0;
-        // what the earlier sums divide it by does not change its share: one number for all tokens
     }
     return x;
+}
+
+// Four numbers of a row from t on, or its last four where t is near its end or beyond: of those the ones before t are another lane's.
+// (Rows of an odd vocabulary begin between 16-byte pieces; blocks that begin at such a piece instead were no faster.)
+__device__ __forceinline__ int first_of(int t, int V) { return V >= 4 ? min(t, V - 4) : 0; }
+__device__ __forceinline__ Four four(const float *p, int t, int V)
+{
+    if (V >= 4) return *(const Four *)(p + first_of(t, V));
+    return Four{p[0], p[min(1, V - 1)], p[min(2, V - 1)], p[V - 1]};
 }
 
 // A lane's tokens of a block: four runs of four, 256 tokens apart.
@@ -77,23 +86,37 @@ struct Tokens {
 __device__ __forceinline__ void ask(const Rest &r, int block, int V, Tokens &x)
 {
     const int t0 = block * kBlock + (threadIdx.x & 63) * 4;
-    const bool two = r.q && r.rejected;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = t0 + i * 256;
-        x.p[i] = x.q[i] = Four{};
-        if (t + 4 <= V) {
-            x.p[i] = *(const Four *)(r.p + t);
-            if (two) x.q[i] = *(const Four *)(r.q + t);
-        } else {
+    for (int i = 0; i < 4; ++i) x.p[i] = four(r.p, t0 + i * 256, V);
+    if (r.q && r.rejected)
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
-                if (t + y < V) {
-                    x.p[i][y] = r.p[t + y];
-                    if (two) x.q[i][y] = r.q[t + y];
-                }
+        for (int i = 0; i < 4; ++i) x.q[i] = four(r.q, t0 + i * 256, V);
+}
+
+// r of the i-th of these runs, 0 for what is another lane's or none's.
+__device__ __forceinline__ void values(const Rest &r, int block, int i, int V, const Tokens &y, double x[4])
+{
+    const int t = block * kBlock + i * 256 + (threadIdx.x & 63) * 4, from = first_of(t, V);
+#pragma unroll
+    for (int z = 0; z < 4; ++z) x[z] = y.p[i][z];
+    if (r.q && r.rejected) {
+#pragma unroll
+        for (int z = 0; z < 4; ++z) x[z] = fmax(x[z] - (double)y.q[i][z], 0.0);
+        for (int j = 1; j < r.rejected; ++j) {
+            const double inv = r.inv[j];
+#pragma unroll
+            for (int z = 0; z < 4; ++z) x[z] = fmax(x[z] * inv - (double)y.q[i][z], 0.0);
+        }
+    } else {
+        for (int j = 0; j < r.rejected; ++j) {
+            const int gone = r.gone[j];
+#pragma unroll
+            for (int z = 0; z < 4; ++z) x[z] = from + z == gone ? 0.0 : x[z];
         }
     }
+    if ((block + 1) * kBlock > V)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) x[z] = from + z < t || from + z >= V ? 0.0 : x[z];
 }
 
 // The largest of a row, the lowest index of equal ones, for all threads of a workgroup.
@@ -106,24 +129,19 @@ __device__ int largest(const float *p, int V, float *sh_most, int *sh_best)
     auto look = [&](float x, int t) {
         if (x > most) most = x, best = t;
     };
-    for (int t0 = tid * 4; t0 < V; t0 += 4 * kThreads * kEach) {
+    // (numbers looked at twice change nothing)
+    for (int t0 = 0; t0 < V; t0 += 4 * kThreads * kEach) {
         Four x[kEach];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int t = t0 + i * 4 * kThreads;
-            x[i] = Four{};
-            if (t + 4 <= V) x[i] = *(const Four *)(p + t);
-        }
+        for (int i = 0; i < kEach; ++i)
+            if (t0 + i * 4 * kThreads < V) x[i] = four(p, t0 + (i * kThreads + tid) * 4, V);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int t = t0 + i * 4 * kThreads;
-            if (t + 4 <= V) {
+        for (int i = 0; i < kEach; ++i)
+            if (t0 + i * 4 * kThreads < V) {
+                const int at = first_of(t0 + (i * kThreads + tid) * 4, V);
 #pragma unroll
-                for (int y = 0; y < 4; ++y) look(x[i][y], t + y);
-            } else {
-                for (int y = t; y < V; ++y) look(p[y], y);
+                for (int y = 0; y < 4; ++y) look(x[i][y], at + y);
             }
-        }
     }
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) {
@@ -220,11 +238,6 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a, bool known)
         Z = 1.0;
     };
     // the sum of r, and of its blocks
-    auto values = [&](const Tokens &y, int b, int i, double x[4]) {
-        const int t = b * kBlock + i * 256 + lane * 4;
-#pragma unroll
-        for (int z = 0; z < 4; ++z) x[z] = less(r, y.p[i][z], y.q[i][z], t + z);
-    };
     auto pass = [&]() {
         Tokens y[2];
         int b = wave;
@@ -235,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a, bool known)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 double x[4];
-                values(y[0], b, i, x);
+                values(r, b, i, V, y[0], x);
                 sum += (x[0] + x[1]) + (x[2] + x[3]);
             }
             sum = wave_sum(sum);
@@ -316,9 +329,9 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a, bool known)
         ask(r, found, V, y);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = found * kBlock + i * 256 + lane * 4;
+            const int t = first_of(found * kBlock + i * 256 + lane * 4, V);
             double x[4];
-            values(y, found, i, x);
+            values(r, found, i, V, y, x);
             const double mine = (x[0] + x[1]) + (x[2] + x[3]);
             const double up = wave_scan(mine);
             double run = at_found + (up - mine);
