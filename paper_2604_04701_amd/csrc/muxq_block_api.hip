@@ -365,9 +365,10 @@ int muxq_verify_tree(const float *target, int ldt, const float *draft, int ldd, 
                           (const void *)starts, (const void *)path, (const void *)counts, (const void *)next_token})
         if (!aligned(p, 4)) return MUXQ_ERR_ALIGN;
     // (path is written while tokens are still read, by other workgroups too)
-    const struct { const void *p; long long n; } own[] = {{path, M}, {counts, S}, {next_token, S}, {tokens, M}, {parents, M}, {starts, S + 1}, {uniforms, M}};
+    const struct { const void *p; long long n; } own[] = {{path, M}, {counts, S}, {next_token, S}, {tokens, M}, {parents, M}, {starts, S + 1}, {uniforms, M},
+                                                      {target, (M - 1ll) * ldt + V}, {uniforms ? draft : nullptr, (M - 1ll) * ldd + V}};
     for (int i = 0; i < 3; ++i)
-        for (int j = i + 1; j < 7; ++j)
+        for (int j = i + 1; j < 9; ++j)
             if (own[j].p && (uintptr_t)own[i].p < (uintptr_t)own[j].p + 4 * own[j].n && (uintptr_t)own[j].p < (uintptr_t)own[i].p + 4 * own[i].n)
                 return MUXQ_ERR_PARAM;
     muxq::VerifyArgs a{};

@@ -98,6 +98,13 @@ def test_verification_refuses(kw, status):
     assert verify(**kw) == status
 
 
+def test_verification_refuses_outputs_among_the_probabilities():
+    last = 4 * (9 * 100 + 99)                   # the last number of target and draft
+    assert verify(path=FAKE + last) == verify(next=FAKE + last) == 4
+    assert verify(target=FAKE + (1 << 20), counts=FAKE + last) == verify(draft=FAKE + (1 << 20), counts=FAKE + last) == 4
+    assert verify(draft=FAKE + (1 << 20), next=FAKE + (1 << 20) + last) == 4
+
+
 @pytest.mark.parametrize("kw,status", [(dict(src=None), 1), (dict(dst=None), 1), (dict(n=0), 2), (dict(n=(1 << 24) + 1), 2), (dict(src=FAKE + 2), 3),
                                        (dict(dst=FAKE + 1), 3)])
 def test_copy_refuses(kw, status):
