@@ -543,6 +543,13 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
                     for (int z = 0; z < 4; ++z) most = fmaxf(most, fabsf(vs[x][z]));
                 }
                 if (__any(most > __uint_as_float((uint32_t)(cap + 127) << 23))) {          // rare: scales of values beyond 2^cap
+                    if (!all) {                       // (one that the row does not see is nothing to it)
+                        uint32_t word = row.sees32(tree, t0 + 32 * b, w.t1) >> 4 * half;
+                        asm volatile("" : "+v"(word));
+                        most = 0.0f;
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) most = fmaxf(most, word >> (8 * (x >> 2) + (x & 3)) & 1 ? fabsf(vs[x >> 2][x & 3]) : 0.0f);
+                    }
                     most = fmaxf(most, __shfl_xor(most, 32, 64));
                     const int to = max(cap, (int)(min(__float_as_uint(most) >> 23, 252u) + 1) - 127);
                     scale_all(b, exp2_((float)(cap - to)));

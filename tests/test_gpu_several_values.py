@@ -68,6 +68,37 @@ def test_infinite_values(name, bits):
     assert torch.isfinite(got).all() and (got - plain).abs().max() <= 2.0 ** -10 * plain.abs().max()
 
 
+@pytest.mark.parametrize("kind", ["causal", "window", "tree"])
+@pytest.mark.parametrize("name", SHAPES)
+def test_large_scales_in_places_that_a_row_does_not_see(name, kind):
+    """Weights are cut by the largest scale of a value; one that other rows of the batch see, or none, changes no bit of a row."""
+    say(f"[case] large scales {name} {kind}")
+    new, lengths, H, heads, d = SHAPES[name]
+    if kind == "tree":
+        new = [min(n, 64) for n in new]
+    s, n, length, group = len(new) - 1, new[-1], lengths[-1], H // heads
+    win = 9 if kind == "window" else 0
+    parents = sum((random_tree(n, i) for i, n in enumerate(new)), [])
+    seen = below(parents[-n:], length) if kind == "tree" else causal(n, length, win, 0)
+    places = [max(0, length - max(1, n // 2))] if kind != "window" else [length - 1, max(0, length - n - 20), max(0, length - n // 2 - 12)]
+    found = []
+    for large in (False, True):
+        c = Case(6, new, lengths, H, heads, d, 16, 8)
+        starts, at = c.device()
+        for t in places if large else []:
+            page, i = place(c, s, t)
+            c.vs[page, :, i] = 1e30
+        if kind == "tree":
+            found.append(B.muxq_tree_attention(c.q, c.k, c.v, c.table, starts, at, ints(parents), max(new), max(lengths), **c.scales()))
+        else:
+            found.append(window(c, win))
+    clear = ~seen[:, places].any(1)
+    assert clear.any() or n == 1 or kind == "window"
+    plain, got = (x[c.starts[s]:][clear] for x in found)
+    assert torch.equal(plain, got), (plain.float() - got.float()).abs().max()
+    assert torch.equal(found[0][:c.starts[s]], found[1][:c.starts[s]])
+
+
 def test_more_infinite_tiles_than_are_remembered():
     say("[case] infinite values in 60 tiles")
     c = Case(9, [40], [64 * 70], 2, 2, 128, 16)
