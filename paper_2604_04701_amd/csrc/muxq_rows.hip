@@ -10,11 +10,26 @@
 // 32 x 32 x 16 steps with the tokens, or the dimensions, as rows of the left operand and 32 rows of the problem as the columns of the right one: scores
 // come out with a row per lane column, which is where the weights of the second product have to stand, so that they never leave their
 // lanes.  The second product's left operand is the transposed values, which LDS turns while it reads (16 lanes, 4 tokens of 16 dimensions).
-// Rows in LDS are 16 bytes longer for keys and 32 for values, so that neither kind of read meets the same banks twice.
+// Rows in LDS are 16 bytes longer for keys and 32 for values, so that neither kind of read meets the same banks twice.  In the form for many rows of
+// fp16 memory writes to LDS itself, two tiles in turn, and pieces of rows change places instead: no registers hold a tile (1.07 against
+// 1.11 ms for the 16384 tokens below).
 //
 // Weights are 2^(s - m + 8), rounded to fp16, and m follows the maximum only when a score is 7 above it, which is rare: up to
-// 2^15, so that small ones keep their bits.  The scale of a key goes to its score, the scale of a value to its weight; weights and
-// their sum are over a running power of two that the scales do not pass.
+// 2^15, so that small ones keep their bits.  The rounding is the one that a matrix instruction asks for; sums take the weights as they were rounded, so
+// that it falls out of a sum of equal values.  The scale of a key goes to its score, the scale of a value to its weight; weights and
+// their sum are over a running power of two that the scales which a row sees do not pass.
+//
+// What bounds it and what it reaches:
+//   16384 tokens within a window of 4096, 32 heads of 128 over 8 of keys, fp16: 1.08 ms, 894 TFLOP/s of the 1190 that a large product reaches.
+//     The matrix pipes are busy 37 % of the cycles of a chip that power holds below its clock; without the reads of LDS it would be 7 %
+//     faster, without the loads 12 %.
+//   13 prompts, 8192 tokens together, behind up to 1500, a window of 1024, in codes: 0.22 ms, 530 TFLOP/s: conversion and scales are as many vector
+//     instructions as the softmax is.
+//   64 trees of 32 nodes over up to 8192 tokens: 0.26 ms, 4.4 TB/s: loads on their way, 32 KB a workgroup and two workgroups a CU.
+//   1024 tokens, 12 heads of 64: 16.6 us with the join; 24 single tokens with a window of 256 in codes, 20 heads: 15.5 us; 8 nodes behind 37
+//     tokens, 12 heads: 9.3 us: chains of loads (lengths, pages, keys), one tile after the other, and what a launch costs.
+// Taken back: eight waves of 32 rows (1.10 ms against 1.12 then, but 254 against 230 us in codes), loads between the products (their
+// registers spilled), streaming loads (the trees 2 % faster, prompts 10 % slower).
 #include "muxq_block_kernels.h"
 
 #include <algorithm>
@@ -811,7 +826,7 @@ struct Form {
     int pieces, tiles;
 };
 
-// Workgroups that fill the chip, of 32 rows and heads of more than 64 dimensions twice as many; tiles of a piece, at least.  (22 trees of 20
+// Workgroups that fill the chip, of 32 rows and heads of more than 64 dimensions, whose two waves hold half as much, twice as many; tiles of a piece, at least.  (22 trees of 20
 // nodes, 16 heads of 96, to 4571 tokens, codes: 78 us with 3 pieces each, 104 with 2; 5 of 15 nodes, 12 heads of 80, 4580 tokens, fp16: 38
 // us with 9 pieces, 45 with 17, which cost more to join than they gain.)
 constexpr int kFill = 512, kLeast = 4;
@@ -828,13 +843,26 @@ Form form_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int 
     Form f;
     const int group = n_heads / n_kv_heads;
     const long long most = (long long)max_new * group, all = (long long)S * n_kv_heads;
-    // the widest tile of rows that the rows fill, and that fills the chip; of a tree's keys and values each is read once
+    // Rows of a workgroup.  Wider tiles read keys and values less often and keep the matrix pipes busier, narrower ones are more workgroups, and waste
+    // less at the edges of a window.  us with 32 / 64 / 128 rows, workgroups of 64 (of 128) rows in brackets:
+    //   heads of 128, 12 of 512 tokens 19.2 / 16.7 / 19.4 [96 (48)]; 32 of 8, 1000 tokens 49.8 / 41.3 / 38.8 [504 (256)];
+    //     a window of 256: 2 sequences of 1024, 16 heads 23 / 19.1 / 23.2 [512 (256)]; 32 of 8, 4096 codes 90 / 69 / 51 [2048 (1024)];
+    //     trees of 32 nodes, 32 of 8, 4000 tokens: 4 of them 36.8 / 29.5 / 32.5 [64 (32)], 8 55 / 44 / 41, 64 375 / 257 / 198;
+    //   heads of 64, 16 of 2048 tokens 31.2 / 32.9 / 36.8 [512 (256)], codes 37.6 / 44.7 / 50.9; of 4096 tokens 85.7 / 67.9 / 80.4 [1024 (512)];
+    //     32 of 8, 8192 tokens - / 449 / 366 [4096 (2048)]; a window of 256: 12 of 512 tokens 11.1 / 13.6 / 15.9 [96 (48)],
+    //     16 of 2048 21.0 / 13.6 / 18.7 [512 (256)], 16 of 8192 - / 35.8 / 34.0 [2048 (1024)], codes - / 43.1 / 48.7;
+    //     trees of 64 nodes, 12 heads, 1000 tokens: 4 of them 15.4 / 14.1, 64 71 / 40; of 32 nodes, 32 of 8: 4 of them - / 14.0 / 15.5 [64 (32)], 64
+    //     - / 47.9 / 38.5 [1024 (512)].
+    auto groups = [&](int rows) { return all * ((most + rows - 1) / rows); };
+    const bool narrow = window && window < max_length;
     f.rows = 32;
-    for (int r : {128, 64})
-        if (most > r / 2 && (tree || all * ((most + r - 1) / r) >= kFill)) {
-            f.rows = r;
-            break;
-        }
+    if (head_dim > 64) {
+        if (most > 32) f.rows = 64;
+        if (most > 64 && groups(128) >= (tree ? 64 : narrow ? 512 : 128)) f.rows = 128;
+    } else {
+        if (most > 32 && (tree || groups(64) >= (narrow ? 192 : 768))) f.rows = 64;
+        if (most > 64 && groups(128) >= (tree ? 256 : 1024)) f.rows = 128;
+    }
     if (head_dim > 128) f.rows = 128;
     f.tile = head_dim > 128 ? 32 : f.rows == 32 && head_dim <= 64 ? 128 : 64;
     f.row_tiles = (most + f.rows - 1) / f.rows;

@@ -7,12 +7,19 @@
 // forms it anew from p, q and the sums of the earlier rejections, in binary64 (the difference of two binary32 numbers is
 // exact there but for 2^-53, and a sum's order moves a token only where u is within 2^-45 of a border).
 // Sums stand for blocks of 1024 tokens in LDS, so that the search for the next token goes through the blocks' sums and one block.
+//
+// 64 sampled trees of 32 nodes, 50257 tokens: 45 us, two to six passes a tree of 7 to 9 us, each 400 KB through one CU and 100000 conversions to
+// binary64; 64 of the 256 CUs work.  More CUs a tree would have to wait for each other within a launch, or take a launch for each
+// rejection.  A chain of four, greedy: 13 us, 6.5 of them the rows' largest, five workgroups, and 2.4 the walk.
+// Taken back: half of the threads, more blocks on their way (50 us, greedy ones 28 against 23); sixteen numbers of a lane at once (they spilled: 111 us).
 #include "muxq_block_kernels.h"
 
 namespace muxq {
 namespace {
 
-constexpr long long kAtOnce = 8 << 20;          // numbers of a target whose rows are looked at all at once
+// Numbers of a target whose rows are looked at all at once where greedy: 8 chains of 16 nodes, 50257 tokens each, 12.8 us, 45.4 row after row along the
+// path; 5 trees of 32 14.5 and 20.0; 8 of them 19.0 and 19.9; 32 of 8 nodes (12 million numbers) 16.9 and 13.4.
+constexpr long long kAtOnce = 8 << 20;
 constexpr int kThreads = 1024, kWaves = kThreads / 64, kBlock = 1024;
 
 typedef float Four __attribute__((ext_vector_type(4), aligned(4)));        // rows of an odd vocabulary begin anywhere
