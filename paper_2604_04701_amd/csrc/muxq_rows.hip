@@ -871,7 +871,11 @@ Form form_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int 
     f.pieces = 1;
     f.tiles = (int)tiles;
     const long long twice = f.rows == 32 && head_dim > 64 ? std::min((2 * kFill + f.groups - 1) / f.groups, 8ll) : 1;
-    const long long want = std::min(std::max((kFill + f.groups - 1) / f.groups, twice), tiles / kLeast);
+    // Heads to 64 dimensions: no more of them than the chip holds at a time, three a CU.  (24 single tokens over 1000, 20 heads, fp16: 27.7 us with 480
+    // workgroups, 34.3 with 960; over 100 to 1000 21.8 and 27.0.  Wider heads, two a CU, gain as much where sequences are equally long, 40 trees over 4000
+    // tokens 152 us and 184, but lose more where they are not, 130 and 95 over 400 to 4000.)
+    const long long at_once = head_dim <= 64 ? std::max(3 * 256 / f.groups, 1ll) : kFill;
+    const long long want = std::min({std::max((kFill + f.groups - 1) / f.groups, twice), at_once, tiles / kLeast});
     if (want > 1) {
         f.tiles = (int)((tiles + want - 1) / want);
         f.pieces = (int)((tiles + f.tiles - 1) / f.tiles);
