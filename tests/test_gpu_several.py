@@ -62,7 +62,9 @@ def test_head_sizes(d, layout, bits):
 # batches that fill the chip with tiles of 64 and of 128 rows
 FULL = {"rows128": ([150] * 9 + [131, 140, 150], [150 + 31 * i for i in range(12)], 32, 16, 128), "rows128_d80": ([150] * 12, [400] * 11 + [150], 32, 16, 80),
         "rows128_d64": ([100] * 12, [100 + 50 * i for i in range(12)], 48, 24, 64), "rows64": ([60, 33] * 20, [60, 333] * 20, 16, 16, 64),
-        "rows64_d128": ([60, 64] * 20, [160, 64] * 20, 16, 16, 128), "heads256": ([100] * 4, [100, 130, 333, 1000], 12, 6, 256)}
+        "rows64_d128": ([60, 64] * 20, [160, 64] * 20, 16, 16, 128), "heads256": ([100] * 4, [100, 130, 333, 1000], 12, 6, 256),
+        "rows128_of_64": ([200] * 9 + [131], [200 + 31 * i for i in range(10)], 104, 52, 64), "rows64_of_64": ([60, 33] * 26, [60, 133] * 26, 16, 16, 64),
+        "rows128_in_pieces": ([260, 1, 200], [900, 2000, 260], 32, 8, 128), "rows64_in_pieces": ([64, 3], [1500, 64], 16, 4, 80)}
 
 
 @pytest.mark.parametrize("bits", [16, 8])
@@ -91,7 +93,9 @@ def test_scales(scale):
 @pytest.mark.parametrize("kind", ["tree", "chain", "star", "forest"])
 @pytest.mark.parametrize("new,lengths,H,heads,d", [
     ([1], [1], 4, 4, 64), ([8], [45], 12, 12, 64), ([64, 64], [64, 1000], 8, 2, 128), ([31, 1, 0, 64, 17], [31, 200, 30, 77, 900], 4, 1, 64),
-    ([33, 20], [300, 25], 6, 6, 256), ([5], [2000], 32, 8, 128)])
+    ([33, 20], [300, 25], 6, 6, 256), ([5], [2000], 32, 8, 128),
+    ([64, 50, 64] * 3, [64, 700, 300] * 3, 16, 8, 128), ([40, 37] * 4, [100, 340] * 4, 64, 32, 64), ([30, 40], [800, 40], 12, 12, 80),
+    ([9, 5, 64], [4, 0, 63], 4, 2, 64)])
 def test_trees(new, lengths, H, heads, d, kind, bits):
     say(f"[case] tree {new} {lengths} {H} of {heads} d={d} {kind} bits={bits}")
     c = Case(5, new, lengths, H, heads, d, 16, bits)
