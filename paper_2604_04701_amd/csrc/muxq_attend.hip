@@ -14,13 +14,16 @@
 // score is 7 above it, which is rare: up to 2^15, so that small ones keep their bits.  8-bit codes are exact in
 // fp16; the scale of a key goes to its score, the scale of a value to its weight, over a running power of two.
 //
+// The rows of a packed batch that has at most one for each sequence, within a window, take the same kernel (kRows; muxq_rows.hip has the other
+// batches): 24 of them with a window of 256, 20 heads of 64, codes, 9.9 us.
+//
 // How it is divided (Plan below): short or many sequences have a workgroup of 8 waves each and key-value head, and no second
 // launch; otherwise as many workgroups as the chip holds have equal shares, and a second launch joins what they cut through.
 // Measured: 64 sequences of 131 to 8192 tokens, 8 key-value heads of 128, fp16, 1.09 GB: 183 us, 6.0 TB/s; one of 131071 tokens
 // 95 us, 5.7 TB/s; 64 of 4096 to 8192, 8 heads of 128, 8-bit codes, 0.83 GB: 152 us, 5.5 TB/s; 24 sequences to 1024, 20 heads of 64, codes,
 // 34 MB: 15.3 us, where a wave has 32 tokens on its way at a time, of 128 bytes in codes, and four such steps one after the other; one of
-// 37 tokens 5.2 us (kernel trace).  Heads of 144 to 256 in fp16 without shares keep arrays in scratch memory: 64 sequences to 1000, 4
-// heads of 256, 157 us, in codes 25.
+// 37 tokens 5.2 us (kernel trace).  Lambdas of loads are inlined by force: left as calls they kept their arrays in scratch memory (64 sequences to
+// 1000, 4 heads of 256, fp16, 157 us, now 47, in codes 25).
 #include "muxq_block_kernels.h"
 
 #include <algorithm>
@@ -95,11 +98,12 @@ constexpr int kHeads = kD == 256 ? 8 : 16;
 // The values of tokens t0 to t1 that are infinite or NaN, four dimensions from e on, with weights of 1, or of 0 where the query's score is
 // -infinity: all that counts for a sum in which there is one.  The matrix product makes NaN of it, since the low part of a weight, or all of
 // it, may be 0 in 16 bits; a thread that finds NaN or an infinity goes through the tokens by itself.
+// (row_of: the query's row)
 template <bool kInt8>
-__device__ __forceinline__ f32x4 loose_values(const AttendArgs &a, int s, int kvh, int head, int e, int t0, int t1)
+__device__ __forceinline__ f32x4 loose_values(const AttendArgs &a, int s, int row_of, int kvh, int head, int e, int t0, int t1)
 {
     const int d = a.c.head_dim, shift = a.c.block_shift, mask = (1 << shift) - 1;
-    const _Float16 *const q = a.q + (long long)s * a.ldq + (long long)head * d;
+    const _Float16 *const q = a.q + (long long)row_of * a.ldq + (long long)head * d;
     f32x4 sum = {};
     for (int t = t0; t < t1; ++t) {
         const int page = a.table[(long long)s * a.ld_table + (t >> shift)];
@@ -129,7 +133,9 @@ __device__ __forceinline__ f32x4 loose_values(const AttendArgs &a, int s, int kv
     return sum;
 }
 
-template <int kD, bool kInt8, bool kFull, int kWaves, bool kShares>
+// kRows: the query of a sequence is where starts[] says, if anywhere, and sees a window and the first tokens: [0, sinks) and [from, len), or all.
+// Both stand one behind the other then, the first ones in whole steps of a wave, and t0 to t1 counts them so.
+template <int kD, bool kInt8, bool kFull, int kWaves, bool kShares, bool kRows>
 __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 8 ? 2 : 1) void k_attend(AttendArgs a, Plan plan)
 {
     constexpr int NS = kD / 32, VE = kD / 16, kThreads = 64 * kWaves;
@@ -204,8 +210,22 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
         const int kvh = pair / subs, sub = pair - kvh * subs;
         const int head0 = kvh * a.group + sub * kHeads<kD>, n_here = min(kHeads<kD>, a.group - sub * kHeads<kD>);
         const int len = length_of(s);
-        int t0 = 0, t1 = len;
+        int t0 = 0, t1 = len, row_of = s;
+        int sinks = 0, sinks_up = 0, from = 0, begin = 0;
         bool whole = true;
+        if constexpr (kRows) {
+            const int a0 = max(0, min(a.starts[s], a.M)), a1 = max(0, min(a.starts[s + 1], a.M));
+            if (a1 - a0 != 1) return;
+            row_of = a0;
+            if (a.window && len - a.window > a.sinks) {
+                sinks = a.sinks, sinks_up = (sinks + kTile - 1) / kTile * kTile;
+                from = len - a.window, begin = from & ~3;
+                t1 = sinks_up + len - begin;
+            }
+        }
+        // the token that stands at place x of these, and where the next ones begin to be others
+        auto token_of = [&](int x) { return kRows && x >= sinks_up ? x - sinks_up + begin : x; };
+        auto end_of = [&](int x) { return kRows && x < sinks_up ? sinks : len; };
         if constexpr (kShares) {
             const int steps = (int)min((long long)(n - j), end - at);
             t0 = min(len, max(0, j - kBegin) * kStep);
@@ -213,13 +233,13 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
             whole = steps == n;
             at += steps;
         } else if (len == 0) {                       // an idle place
-            for (int i = tid; i < n_here * d; i += kThreads) a.o[(long long)s * a.ldo + (long long)head0 * d + i] = (_Float16)0.0f;
+            for (int i = tid; i < n_here * d; i += kThreads) a.o[(long long)row_of * a.ldo + (long long)head0 * d + i] = (_Float16)0.0f;
             return;
         }
 
         // queries: column `col` of the right operand, the dimensions in the left one's order
         f16x8 q[NS];
-        const _Float16 *qrow = a.q + (long long)s * a.ldq + (long long)(head0 + min(col, n_here - 1)) * d;
+        const _Float16 *qrow = a.q + (long long)row_of * a.ldq + (long long)(head0 + min(col, n_here - 1)) * d;
 #pragma unroll
         for (int st = 0; st < NS; ++st) {
             const int e = kInt8 ? 64 * (st >> 1) + 16 * g + 8 * (st & 1) : 32 * st + 8 * g;
@@ -239,14 +259,17 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
         long long *const sh_off = (long long *)rest;
         int first = 0, c1 = 0;
         bool any_bad = false;
-        auto is_masked = [&](int tok) { return any_bad || tok + kTile > c1; };
-        auto load_k = [&](auto masked_c, int tok) {
+        auto is_masked = [&](int tok) { return any_bad || tok + kTile > c1 || (kRows && from > 0 && tok <= sinks_up); };
+        int first_other = 0;                              // of the tokens behind the first ones
+        auto page_of = [&](int tok, int t) { return sh_off[(t >> shift) - (kRows && tok >= sinks_up ? first_other : first)]; };
+        auto here = [&](int tok, int t) { return kRows ? t < end_of(tok) && (tok < sinks_up || t >= from) : t < c1; };
+        auto load_k = [&](auto masked_c, int tok) __attribute__((always_inline)) {
             constexpr bool kMasked = decltype(masked_c)::value;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const int kt = tok + 16 * t + col;
-                long long at = sh_off[(kt >> shift) - first];
-                const bool there = !kMasked || (at >= 0 && kt < c1);
+                const int kt = token_of(tok) + 16 * t + col;
+                long long at = page_of(tok, kt);
+                const bool there = !kMasked || (at >= 0 && here(tok, kt));
                 if (kInt8) at = at * a.c.ld_block + kvh * a.c.ld_head;
                 const long long row = there ? at + (kt & mask) * a.c.ld_token : 0;
 #pragma unroll
@@ -257,13 +280,13 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                 }
             }
         };
-        auto load_v = [&](auto masked_c, int tok) {
+        auto load_v = [&](auto masked_c, int tok) __attribute__((always_inline)) {
             constexpr bool kMasked = decltype(masked_c)::value;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 // the lane's tokens are 16 t + 4 g + 0..3, in one page
-                const int vt = tok + 16 * t + 4 * g;
-                const long long page = sh_off[(vt >> shift) - first];
+                const int vt = token_of(tok) + 16 * t + 4 * g;
+                const long long page = page_of(tok, vt);
                 const long long at = kInt8 ? page * a.c.ld_block + kvh * a.c.ld_head : page;
                 if constexpr (kInt8) {
                     const long long at_s = (kMasked && page < 0) ? 0 : ((page * a.c.n_kv_heads + kvh) << shift) + (vt & mask);
@@ -272,7 +295,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool there = !kMasked || (page >= 0 && vt + i < c1);
+                    const bool there = !kMasked || (page >= 0 && here(tok, vt + i));
                     const char *p = a.c.v + (there ? at + ((vt & mask) + i) * a.c.ld_token + VE * col : 0) * (kInt8 ? 1 : 2);
                     uint32_t *w = v[4 * t + i];
 #pragma unroll
@@ -298,24 +321,27 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                 }
             }
         };
-        auto ask_k = [&](int tok) {
+        auto ask_k = [&](int tok) __attribute__((always_inline)) {
             if (is_masked(tok)) load_k(std::true_type{}, tok); else load_k(std::false_type{}, tok);
         };
-        auto ask_v = [&](int tok) {
+        auto ask_v = [&](int tok) __attribute__((always_inline)) {
             if (is_masked(tok)) load_v(std::true_type{}, tok); else load_v(std::false_type{}, tok);
         };
 
         for (int c0 = t0; c0 < t1; c0 = c1) {
-            c1 = min(t1, c0 + kPages);
+            c1 = kRows ? t1 : min(t1, c0 + kPages);
             first = c0 >> shift;
-            const int pages = ((c1 - 1) >> shift) - first + 1;
+            // (of the first tokens' last step also pages that they do not reach)
+            const int pages_first = kRows ? (sinks_up + (1 << shift) - 1) >> shift : 0, pages_sinks = (sinks + (1 << shift) - 1) >> shift;
+            const int pages = kRows ? pages_first + ((len - 1) >> shift) - (begin >> shift) + 1 : ((c1 - 1) >> shift) - first + 1;
+            first_other = (begin >> shift) - pages_first;
             __syncthreads();                              // the last piece's readers
             if (tid == 0) sh_bad = 0;
             __syncthreads();
             for (int i = tid; i < pages + 4; i += kThreads) {
                 long long where = -1;
-                if (i < pages) {
-                    const int page = a.table[(long long)s * a.ld_table + first + i];
+                if (i < pages && (!kRows || i < pages_sinks || i >= pages_first)) {
+                    const int page = a.table[(long long)s * a.ld_table + (kRows && i >= pages_first ? first_other : first) + i];
                     if (page >= 0 && page < a.c.n_blocks)
                         where = kInt8 ? page : page * a.c.ld_block + kvh * a.c.ld_head;
                     else
@@ -367,8 +393,15 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                 if (is_masked(tok)) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const int kt = tok + 16 * (j >> 2) + 4 * g + (j & 3);
-                        if (kt >= c1 || sh_off[(kt >> shift) - first] < 0) p[j] = kFloor, w[j] = 0.0f;
+                        const int kt = token_of(tok) + 16 * (j >> 2) + 4 * g + (j & 3);
+                        if constexpr (kRows) {
+                            // (without branches: of `a || b` the compiler loses p[0] = kFloor where only b holds)
+                            const bool out = !here(tok, kt) | (page_of(tok, kt) < 0);
+                            p[j] = out ? kFloor : p[j];
+                            if constexpr (kInt8) w[j] = out ? 0.0f : w[j];
+                        } else {
+                            if (kt >= c1 || sh_off[(kt >> shift) - first] < 0) p[j] = kFloor, w[j] = 0.0f;
+                        }
                     }
                 }
                 float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
@@ -443,8 +476,8 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
         if (__any(l == 0.0f)) {                           // no weights: are there tokens?
             bool seen = false;
             for (int tok = t0 + wave * kTile; tok < t1; tok += kWaves * kTile) {
-                const int kt = tok + (lane & (kTile - 1));
-                if (kt >= t1) break;
+                const int kt = token_of(tok) + (lane & (kTile - 1));
+                if (kRows ? !here(tok, kt) : kt >= t1) continue;
                 const int page = a.table[(long long)s * a.ld_table + (kt >> shift)];
                 seen |= page >= 0 && page < a.c.n_blocks;
             }
@@ -493,7 +526,8 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
             for (int w = 0; w < 4; ++w) sum += *(const f32x4 *)(sh_o + (w * n_here + h) * kD + e);
             const f32x4 zero = sum - sum;
             if (!(zero[0] + zero[1] + (zero[2] + zero[3]) == 0.0f) && all == all) {
-                const f32x4 loose = loose_values<kInt8>(a, s, kvh, head0 + h, e, t0, t1);
+                f32x4 loose = loose_values<kInt8>(a, s, row_of, kvh, head0 + h, e, kRows ? from : t0, kRows ? len : t1);
+                if constexpr (kRows) loose += loose_values<kInt8>(a, s, row_of, kvh, head0 + h, e, 0, sinks);
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
                     if (loose[x] - loose[x] != 0.0f) sum[x] = loose[x];
@@ -504,7 +538,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
                 f16x4 r;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) r[x] = (_Float16)(sum[x] * inv);
-                *(f16x4 *)(a.o + (long long)s * a.ldo + (long long)(head0 + h) * d + e) = r;
+                *(f16x4 *)(a.o + (long long)row_of * a.ldo + (long long)(head0 + h) * d + e) = r;
             } else {
                 const int part = (blockIdx.x * 2 + (piece ? 1 : 0)) * min(a.group, kHeads<kD>) + h;
                 *(f32x4 *)(plan.o + (long long)part * d + e) = sum;
@@ -613,28 +647,30 @@ size_t parts_of(int n_heads, int n_kv_heads, int head_dim)
     return (size_t)resident(head_dim) * 2 * std::min(n_heads / n_kv_heads, heads_of(head_dim));
 }
 
-template <int kD, int kWaves, bool kShares>
+template <int kD, int kWaves, bool kShares, bool kRows>
 hipError_t launch_w(const AttendArgs &a, const Plan &plan, bool int8, hipStream_t s)
 {
     const int pairs = a.c.n_kv_heads * ((a.group + kHeads<kD> - 1) / kHeads<kD>);
     const dim3 grid = kShares ? dim3(plan.groups) : dim3(pairs, a.S), block(64 * kWaves);
-    const size_t offs = ((size_t)(std::min(a.max_length, kPages) >> a.c.block_shift) + 6) * 8;
+    // (rows with a window: pages of two runs of tokens, each with a page more)
+    const long long tokens = kRows ? std::min((long long)a.max_length, (long long)a.window + a.sinks) + 2 * kTile : std::min(a.max_length, kPages);
+    const size_t offs = ((size_t)((kRows && !a.window ? a.max_length : tokens) >> a.c.block_shift) + (kRows ? 10 : 6)) * 8;
     const size_t join = (size_t)4 * std::min(a.group, kHeads<kD>) * kD * 4;
     const size_t lds = std::max(offs, join) + (kShares ? (size_t)((a.S + 4) / 4) * 16 : 0);
     const bool full = a.c.head_dim == kD;
     if (int8)
-        return full ? launch_kernel(k_attend<kD, true, true, kWaves, kShares>, grid, block, lds, s, a, plan)
-                    : launch_kernel(k_attend<kD, true, false, kWaves, kShares>, grid, block, lds, s, a, plan);
-    return full ? launch_kernel(k_attend<kD, false, true, kWaves, kShares>, grid, block, lds, s, a, plan)
-                : launch_kernel(k_attend<kD, false, false, kWaves, kShares>, grid, block, lds, s, a, plan);
+        return full ? launch_kernel(k_attend<kD, true, true, kWaves, kShares, kRows>, grid, block, lds, s, a, plan)
+                    : launch_kernel(k_attend<kD, true, false, kWaves, kShares, kRows>, grid, block, lds, s, a, plan);
+    return full ? launch_kernel(k_attend<kD, false, true, kWaves, kShares, kRows>, grid, block, lds, s, a, plan)
+                : launch_kernel(k_attend<kD, false, false, kWaves, kShares, kRows>, grid, block, lds, s, a, plan);
 }
 
 template <int kD>
 hipError_t launch_d(const AttendArgs &a, const Plan &plan, bool int8, hipStream_t s)
 {
-    if (plan.groups) return launch_w<kD, 4, true>(a, plan, int8, s);
+    if (plan.groups) return launch_w<kD, 4, true, false>(a, plan, int8, s);
     // 8 waves where each has tokens (4 sequences of 12 heads to 1024 tokens: 10.8 us, 13.0 with 4)
-    return a.max_length > 128 ? launch_w<kD, 8, false>(a, plan, int8, s) : launch_w<kD, 4, false>(a, plan, int8, s);
+    return a.max_length > 128 ? launch_w<kD, 8, false, false>(a, plan, int8, s) : launch_w<kD, 4, false, false>(a, plan, int8, s);
 }
 
 }  // namespace
@@ -658,7 +694,30 @@ size_t attend_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, 
 hipError_t attend_prepare()
 {
     hipFuncAttributes at;
-    return hipFuncGetAttributes(&at, (const void *)k_attend<64, false, true, 4, false>);
+    return hipFuncGetAttributes(&at, (const void *)k_attend<64, false, true, 4, false, false>);
+}
+
+// Tokens that a row sees at most.
+static long long seen_of(int max_length, int window, int sinks) { return window ? std::min<long long>(max_length, (long long)window + sinks) : max_length; }
+
+// Where this is faster than tiles of rows, which waste 31 of their 32 rows but are split over the tokens.  us, tiles and this: 24 sequences of 20
+// heads of 64 over 1000 tokens, codes, 24.3 / 20.7, over 2500 45.3 / 38.7, window of 256 15.5 / 9.9; 1 of 12 heads over 1000 13.9 / 10.9, over
+// 3000 14.2 / 21.7; heads of 128, 8 of 32 over 8, 1500 tokens 24.0 / 22.7, 4000 31.3 / 43.7; 70 of 8, 8000 tokens 450 / 433, 800 to 8000 256 / 240.
+// (All pages that a row sees stand in LDS at once: 8192 tokens at most.)
+bool attend_rows_fits(int S, int n_heads, int n_kv_heads, int head_dim, int max_length, int window, int sinks)
+{
+    if (head_dim > 128) return false;
+    const int group = n_heads / n_kv_heads, subs = (group + heads_of(head_dim) - 1) / heads_of(head_dim);
+    const bool idle = (long long)S * n_kv_heads * subs * 2 < resident8(head_dim);
+    return seen_of(max_length, window, sinks) <= (!idle ? 8192 : head_dim <= 64 ? 1250 : 1000);
+}
+
+hipError_t launch_attend_rows(const AttendArgs &a, bool int8, hipStream_t s)
+{
+    const bool eight = seen_of(a.max_length, a.window, a.sinks) > 128;
+    const Plan plan{};
+    if (a.c.head_dim <= 64) return eight ? launch_w<64, 8, false, true>(a, plan, int8, s) : launch_w<64, 4, false, true>(a, plan, int8, s);
+    return eight ? launch_w<128, 8, false, true>(a, plan, int8, s) : launch_w<128, 4, false, true>(a, plan, int8, s);
 }
 
 hipError_t launch_attend(const AttendArgs &a, bool int8, hipStream_t s)

@@ -34,7 +34,12 @@ struct AttendArgs {
     float scale;
     void *workspace;
     KvView c;
+    // one row of a sequence at most, with a window (launch_attend_rows only)
+    const int32_t *starts;
+    int M, window, sinks;
 };
+bool attend_rows_fits(int S, int n_heads, int n_kv_heads, int head_dim, int max_length, int window, int sinks);
+hipError_t launch_attend_rows(const AttendArgs &a, bool int8, hipStream_t s);
 size_t attend_workspace_need(int S, int n_heads, int n_kv_heads, int head_dim, int max_length);
 size_t attend_workspace_bytes(int S, int n_heads, int n_kv_heads, int head_dim, int max_length);
 hipError_t launch_attend(const AttendArgs &a, bool int8, hipStream_t s);

@@ -6,6 +6,8 @@
 // heads that share a key-value head, in this order: many rows make it a matrix product (4 d operations for a row and token, bound by the matrix
 // pipes), few rows a stream through the cache (bound by memory).
 //
+// (Batches of at most one row for each sequence go to muxq_attend.hip, where that is faster: single() below.)
+//
 // Keys and values of a tile of tokens go through LDS as fp16, 8-bit codes converted on the way (exactly).  Both products are
 // 32 x 32 x 16 steps with the tokens, or the dimensions, as rows of the left operand and 32 rows of the problem as the columns of the right one: scores
 // come out with a row per lane column, which is where the weights of the second product have to stand, so that they never leave their
@@ -26,7 +28,7 @@
 //   13 prompts, 8192 tokens together, behind up to 1500, a window of 1024, in codes: 0.22 ms, 530 TFLOP/s: conversion and scales are as many vector
 //     instructions as the softmax is.
 //   64 trees of 32 nodes over up to 8192 tokens: 0.26 ms, 4.4 TB/s: loads on their way, 32 KB a workgroup and two workgroups a CU.
-//   1024 tokens, 12 heads of 64: 16.6 us with the join; 24 single tokens with a window of 256 in codes, 20 heads: 15.5 us; 8 nodes behind 37
+//   1024 tokens, 12 heads of 64: 16.6 us with the join; 8 nodes behind 37
 //     tokens, 12 heads: 9.3 us: chains of loads (lengths, pages, keys), one tile after the other, and what a launch costs.
 // Taken back: eight waves of 32 rows (1.10 ms against 1.12 then, but 254 against 230 us in codes), loads between the products (their
 // registers spilled), streaming loads (the trees 2 % faster, prompts 10 % slower).
@@ -883,6 +885,12 @@ Form form_of(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int 
     return f;
 }
 
+// Whether a call goes to the attention of one new token.
+bool single(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length, int window, int sinks, bool tree)
+{
+    return !tree && max_new == 1 && attend_rows_fits(S, n_heads, n_kv_heads, head_dim, max_length, window, sinks);
+}
+
 size_t bytes_of(size_t parts, int head_dim) { return up256(parts * head_dim * 4) + up256(parts * 8); }
 
 template <int kD, bool kInt8>
@@ -913,6 +921,7 @@ hipError_t launch_d(const RowsArgs &a, const Plan &plan, const Form &f, hipStrea
 
 size_t rows_workspace_need(int S, int n_heads, int n_kv_heads, int head_dim, int max_new, int max_length, int window, int sinks, bool tree)
 {
+    if (single(S, n_heads, n_kv_heads, head_dim, max_new, max_length, window, sinks, tree)) return 0;
     const Form f = form_of(S, n_heads, n_kv_heads, head_dim, max_new, max_length, window, sinks, tree);
     return f.pieces > 1 ? bytes_of((size_t)f.groups * f.pieces * f.rows, head_dim) : 0;
 }
@@ -935,6 +944,15 @@ hipError_t rows_prepare()
 hipError_t launch_rows(const RowsArgs &a, bool int8, hipStream_t s)
 {
     const int d = a.c.head_dim;
+    if (single(a.S, a.n_heads, a.c.n_kv_heads, d, a.max_new, a.max_length, a.window, a.sinks, a.parents != nullptr)) {
+        AttendArgs b{};
+        b.q = a.q, b.o = a.o, b.table = a.table, b.lengths = a.lengths, b.starts = a.starts;
+        b.S = a.S, b.M = a.M, b.n_heads = a.n_heads, b.group = a.group, b.ldq = a.ldq, b.ldo = a.ldo, b.ld_table = a.ld_table;
+        b.max_length = a.max_length, b.window = a.window, b.sinks = a.sinks;
+        b.scale = std::min(std::max(a.scale, -2.0e38f), 2.0e38f);            // (times log2(e) it stays a number)
+        b.c = a.c;
+        return launch_attend_rows(b, int8, s);
+    }
     const Form f = form_of(a.S, a.n_heads, a.c.n_kv_heads, d, a.max_new, a.max_length, a.window, a.sinks, a.parents != nullptr);
     if (f.row_tiles * a.c.n_kv_heads > 1 << 23) return hipErrorInvalidValue;
     Plan plan{(int)f.row_tiles, f.pieces, f.tiles, nullptr, nullptr};

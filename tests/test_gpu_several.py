@@ -52,6 +52,15 @@ def test_windows(name, win, sinks, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("win,sinks", [(0, 0), (700, 45), (1, 33), (33, 1), (128, 0), (100, 1000), (2000, 64), (5000, 3)])
+@pytest.mark.parametrize("H,heads,d,page", [(8, 4, 64, 8), (5, 1, 128, 16), (40, 2, 80, 64), (6, 6, 32, 256)])
+def test_single_rows(H, heads, d, page, win, sinks, bits):
+    """At most a row of each sequence: rows and sequences do not go by the same numbers."""
+    say(f"[case] single rows {H} of {heads} d={d} page={page} window={win} sinks={sinks} bits={bits}")
+    check_window(Case(17, [1, 0, 1, 1, 1, 0, 1, 1], [2300, 5, 1000, 9, 1, 0, 0, 131], H, heads, d, page, bits), win, sinks, what="single rows")
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("layout", ["heads", "tokens"])
 @pytest.mark.parametrize("d", [16, 48, 80, 96, 144, 256])
 def test_head_sizes(d, layout, bits):

@@ -24,7 +24,8 @@ def place(c, s, t):
 
 SHAPES = {"few": ([5, 1], [70, 300], 4, 4, 64), "wide": ([1, 7], [200, 77], 8, 4, 128), "rows64": ([60, 60, 61], [60, 200, 61], 4, 4, 64),
           "rows128": ([130, 128], [130, 300], 4, 2, 128), "full128": ([130] * 12, [130] * 11 + [200], 32, 16, 128), "full80": ([130] * 12, [130] * 11 + [200], 32, 16, 80), "many": ([300] * 12, [300] * 12, 24, 12, 64), "heads256": ([40, 3], [40, 90], 2, 1, 256),
-          "full64": ([130] * 12, [130] * 11 + [200], 60, 30, 64), "split128": ([130] * 3, [130, 150, 900], 32, 16, 128)}
+          "full64": ([130] * 12, [130] * 11 + [200], 60, 30, 64), "split128": ([130] * 3, [130, 150, 900], 32, 16, 128),
+          "single": ([1, 1, 1], [70, 5, 300], 8, 2, 64), "single80": ([1, 0, 1], [40, 3, 900], 4, 4, 80)}
 
 
 @pytest.mark.parametrize("bits", [16, 8])
