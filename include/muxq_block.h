@@ -164,7 +164,7 @@ int muxq_norm(const void *X_fp16, int M, int K, int ldx, const void *R_fp16, int
  * does not see, NaN and infinity included, has no influence on it; infinite and NaN values in places that it sees
  * come out as the formula has them, with weights that are never quite 0, and scores that are all -infinity give NaN (0 / 0).
  * Arithmetic: products of fp16 with binary32 sums; scales of codes multiply scores and weights; statistics of the softmax are
- * binary32; the weights enter the second product rounded to fp16 (11 bits, and whole multiples of 2^-32 of a row's largest, with
+ * binary32; the weights enter the second product rounded to fp16 (11 bits or more, and whole multiples of 2^-32 of a row's largest, with
  * codes 2^-31 of the largest weight times the largest scale that the row sees).
  * max_length: the host's bound on lengths[], 1 <= max_length <= ld_table * block_size, at most 2^26; max_new and max_nodes: the
  * host's bound on the rows of a sequence.  The work is divided by them.
