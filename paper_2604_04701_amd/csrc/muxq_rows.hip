@@ -186,15 +186,19 @@ __device__ __forceinline__ uint64_t nodes_above(const int32_t *parents, int i)
 }
 
 // Infinite and NaN values that the rows of a workgroup see, with weights of 1, or of 0 where the row's score is -infinity: all that counts for
-// a sum in which there is one.  The tiles' values went into the products without them; here they decide what they stand for.
-template <bool kInt8, int kTT>
+// a sum in which there is one.  The tiles' values went into the products without them; here they decide what they stand for.  A row whose
+// sum of weights is NaN, in any of the kWT waves that have it, stays NaN.
+template <bool kInt8, int kTT, int kWR, int kWT>
 __device__ void put_loose(const RowsArgs &a, const Span<kTT> &w, int j0, int j1, const int *tiles, int n_tiles,
-                                                    const int32_t *parents, _Float16 *o, float *part)
+                                                    const int32_t *parents, const float (*totals)[32], _Float16 *o, float *part)
 {
     const int d = a.c.head_dim, quads = d / 4, shift = a.c.block_shift, mask = (1 << shift) - 1;
     const int local0 = w.local0, n_rows = w.n_rows;
     for (int item = threadIdx.x; item < n_rows * quads; item += blockDim.x) {
         const int r = item / quads, e = (item - r * quads) * 4;
+        float all = 0.0f;
+        for (int x = 0; x < kWT; ++x) all += totals[x * kWR + (r >> 5)][r & 31];
+        if (all != all) continue;
         Row row;
         row.find(a, w.kvh, w.n, w.ctx, w.i_lo, local0 + r);
         row.above = a.parents ? nodes_above(parents, row.i) : 0;
@@ -691,7 +695,10 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
                 for (int x = 0; x < kD / 8; ++x)
                     sh_o[((wave - (kAllJoin ? 0 : kWR)) * (kD / 8) + x) * 64 + lane] = f32x4{o[x >> 2][4 * (x & 3)], o[x >> 2][4 * (x & 3) + 1], o[x >> 2][4 * (x & 3) + 2], o[x >> 2][4 * (x & 3) + 3]};
         }
-        if (careful && kWT == 1) break;
+        if (careful && kWT == 1) {
+            if (half == 0) sh_l[wave][col] = total;
+            break;
+        }
         if (!careful && __any(!(sum <= 3.4e38f))) sh_found = 1;
         __syncthreads();
         if (careful || __builtin_amdgcn_readfirstlane(sh_found) == 0) break;
@@ -768,7 +775,7 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 3 : kD == 128 ? 2 : 1) void
     __syncthreads();
     if (sh_n_loose > 0) {
         __threadfence_block();
-        put_loose<kInt8, kTT>(a, w, j0, j1, sh_loose, sh_n_loose, sh_parents, a.o, part_o);
+        put_loose<kInt8, kTT, kWR, kWT>(a, w, j0, j1, sh_loose, sh_n_loose, sh_parents, sh_l, a.o, part_o);
     }
 }
 
