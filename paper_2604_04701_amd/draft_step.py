@@ -94,9 +94,13 @@ class Model:
 
     def prompt(self, tokens, starts, window=0, sinks=0):
         """Packed prompts, tokens [M] and starts (a list of S + 1): the stream behind the blocks."""
-        M, most = starts[-1], max(b - a for a, b in zip(starts, starts[1:]))
-        rows = Rows(self, torch.tensor(starts, dtype=torch.int32, device=DEV), None, most, window, sinks)
         new = [b - a for a, b in zip(starts, starts[1:])]
+        if len(new) != self.S or starts[0] != 0 or min(new) < 0 or not tokens.numel() == starts[-1] > 0:
+            raise ValueError(f"starts {starts} do not divide {tokens.numel()} tokens into {self.S} prompts")
+        M, most = starts[-1], max(new)
+        if most > self.max_tokens:
+            raise ValueError(f"a prompt of {most} tokens, where the tables and angles hold {self.max_tokens}")
+        rows = Rows(self, torch.tensor(starts, dtype=torch.int32, device=DEV), None, most, window, sinks)
         sequence = torch.repeat_interleave(torch.arange(self.S, device=DEV), torch.tensor(new, device=DEV))
         rows.positions = torch.cat([torch.arange(n, device=DEV) for n in new]).int()
         rows.slots = self._slots(sequence, rows.positions.long())
