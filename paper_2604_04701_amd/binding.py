@@ -862,7 +862,7 @@ def alloc_tree_attention_workspace(S, n_heads, n_kv_heads, head_dim, max_nodes, 
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale, v_scale, out, parents=None):
+def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale, v_scale, out, workspace, parents=None):
     """The checks that both attentions of several new tokens share: (descriptor of the cache, out, arguments up to lengths)."""
     M, n_heads, d = q.shape
     c = _kv(k_cache, v_cache, k_scale, v_scale)
@@ -883,6 +883,8 @@ def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_leng
             _together(what, q, out, k_cache, v_cache, k_scale, v_scale, block_table, starts, lengths, parents)
         _refuse(f"{what}: q, out and the cache differ in head size, starts has not one entry more than lengths, or block_table is no "
                 "int32 GPU tensor [S, pages] with contiguous rows of max_length tokens")
+    if workspace is not None and workspace.get_device() != _device():
+        _refuse(f"{what}: the workspace is no tensor of the current device")
     return c, out, os[0], S, (q.data_ptr(), M, n_heads, qs[0], C.byref(c), block_table.data_ptr(),
                               ts[0] if S > 1 else block_table.shape[1], starts.data_ptr(), lengths.data_ptr())
 
@@ -894,7 +896,7 @@ def muxq_window_attention(q, k_cache, v_cache, block_table, starts, lengths, max
     last of them (0: all), with the first `sinks` of the sequence beside them.  max_new, max_length: bounds on the rows and tokens of a
     sequence known on the host.  scale: 1 / sqrt(d) when not given."""
     c, out, ldo, S, args = _rows_args("muxq_window_attention", q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale,
-                                      v_scale, out)
+                                      v_scale, out, workspace)
     args += (S, max_new, max_length, window, sinks, c.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), ldo)
     _call(lib().muxq_window_attention, args, workspace, _stream(),
           lambda: alloc_window_attention_workspace(S, q.shape[1], c.n_kv_heads, c.head_dim, max_new, max_length, window, sinks, q.device),
@@ -908,7 +910,7 @@ def muxq_tree_attention(q, k_cache, v_cache, block_table, starts, lengths, paren
     new tokens only itself and the nodes above it; parents (int32 [M]): the number of each node's parent within its
     sequence, -1 for a root.  max_nodes: a bound on the nodes of a tree, at most 64."""
     c, out, ldo, S, args = _rows_args("muxq_tree_attention", q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale,
-                                      v_scale, out, parents)
+                                      v_scale, out, workspace, parents)
     args += (parents.data_ptr(), S, max_nodes, max_length, c.head_dim ** -0.5 if scale is None else scale,
              out.data_ptr(), ldo)
     _call(lib().muxq_tree_attention, args, workspace, _stream(),
