@@ -843,6 +843,10 @@ def muxq_norm(x, weight, bias=None, residual=None, residual_scale=1.0, post_weig
 _device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
+# (ctypes cuts a number to the 32 bits of a C int without a word.)
+_INT = (1 << 31) - 1
+
+
 def _together(what, *tensors):
     """Says of tensors on GPUs why they are not all on the current one."""
     at = {t.get_device() for t in tensors if t is not None}
@@ -862,7 +866,7 @@ def alloc_tree_attention_workspace(S, n_heads, n_kv_heads, head_dim, max_nodes, 
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale, v_scale, out, workspace, parents=None):
+def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_new, max_length, k_scale, v_scale, out, workspace, parents=None):
     """The checks that both attentions of several new tokens share: (descriptor of the cache, out, arguments up to lengths)."""
     M, n_heads, d = q.shape
     c = _kv(k_cache, v_cache, k_scale, v_scale)
@@ -877,12 +881,13 @@ def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_leng
                                  parents.numel() == M)) and d == c.head_dim and out.shape == q.shape and
             qs[2] == os[2] == 1 and (n_heads == 1 or qs[1] == os[1] == d) and block_table.dim() == 2 and block_table.shape[0] == S and
             ts[1] == 1 and lengths.is_contiguous() and starts.is_contiguous() and starts.numel() == S + 1 and
-            max_length <= block_table.shape[1] * c.block_size):
+            max_length <= block_table.shape[1] * c.block_size and qs[0] <= _INT and os[0] <= _INT and ts[0] <= _INT and
+            0 <= max_new <= _INT and 0 <= max_length <= _INT):
         _rows(q, "q"), _rows(out, "out"), _flat(lengths, S, _I32, "lengths"), _flat(starts, S + 1, _I32, "starts"), _flat(parents, M, _I32, "parents")
         if block_table.is_cuda:
             _together(what, q, out, k_cache, v_cache, k_scale, v_scale, block_table, starts, lengths, parents)
         _refuse(f"{what}: q, out and the cache differ in head size, starts has not one entry more than lengths, or block_table is no "
-                "int32 GPU tensor [S, pages] with contiguous rows of max_length tokens")
+                "int32 GPU tensor [S, pages] with contiguous rows of max_length tokens, or a row stride or a bound takes more than 31 bits")
     if workspace is not None and workspace.get_device() != _device():
         _refuse(f"{what}: the workspace is no tensor of the current device")
     return c, out, os[0], S, (q.data_ptr(), M, n_heads, qs[0], C.byref(c), block_table.data_ptr(),
@@ -895,7 +900,9 @@ def muxq_window_attention(q, k_cache, v_cache, block_table, starts, lengths, max
     starts[s]..starts[s + 1] (int32 [S + 1]) are the last of lengths[s] tokens (int32 [S]).  window: how many tokens a row sees, its own the
     last of them (0: all), with the first `sinks` of the sequence beside them.  max_new, max_length: bounds on the rows and tokens of a
     sequence known on the host.  scale: 1 / sqrt(d) when not given."""
-    c, out, ldo, S, args = _rows_args("muxq_window_attention", q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale,
+    if not (0 <= window <= _INT and 0 <= sinks <= _INT):
+        _refuse("muxq_window_attention: window and sinks are numbers of tokens, 31 bits at most")
+    c, out, ldo, S, args = _rows_args("muxq_window_attention", q, k_cache, v_cache, block_table, starts, lengths, max_new, max_length, k_scale,
                                       v_scale, out, workspace)
     args += (S, max_new, max_length, window, sinks, c.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), ldo)
     _call(lib().muxq_window_attention, args, workspace, _stream(),
@@ -909,7 +916,7 @@ def muxq_tree_attention(q, k_cache, v_cache, block_table, starts, lengths, paren
     """Attention of the nodes of a drafted tree of each sequence, as muxq_window_attention without a window, but a node sees of the
     new tokens only itself and the nodes above it; parents (int32 [M]): the number of each node's parent within its
     sequence, -1 for a root.  max_nodes: a bound on the nodes of a tree, at most 64."""
-    c, out, ldo, S, args = _rows_args("muxq_tree_attention", q, k_cache, v_cache, block_table, starts, lengths, max_length, k_scale,
+    c, out, ldo, S, args = _rows_args("muxq_tree_attention", q, k_cache, v_cache, block_table, starts, lengths, max_nodes, max_length, k_scale,
                                       v_scale, out, workspace, parents)
     args += (parents.data_ptr(), S, max_nodes, max_length, c.head_dim ** -0.5 if scale is None else scale,
              out.data_ptr(), ldo)
@@ -932,17 +939,18 @@ def muxq_verify_tree(target, tokens, starts, parents, max_nodes, draft=None, uni
     if not (target.dtype is _F32 and tokens.dtype is parents.dtype is starts.dtype is path.dtype is counts.dtype is next_token.dtype is _I32 and
             _device() == target.get_device() == tokens.get_device() == parents.get_device() == starts.get_device() == path.get_device() ==
             counts.get_device() == next_token.get_device() and
-            (target.stride(1) == 1 or V == 1) and tokens.is_contiguous() and parents.is_contiguous() and starts.is_contiguous() and
+            (target.stride(1) == 1 or V == 1) and target.stride(0) <= _INT and 0 <= max_nodes <= _INT and tokens.is_contiguous() and parents.is_contiguous() and starts.is_contiguous() and
             path.is_contiguous() and counts.is_contiguous() and next_token.is_contiguous() and tokens.numel() == parents.numel() == path.numel() == M and
             counts.numel() == next_token.numel() == S and
-            (draft is None or (draft.dtype is _F32 and draft.get_device() == target.get_device() and draft.shape == (M, V) and (draft.stride(1) == 1 or V == 1))) and
+            (draft is None or (draft.dtype is _F32 and draft.get_device() == target.get_device() and draft.shape == (M, V) and (draft.stride(1) == 1 or V == 1) and
+                               draft.stride(0) <= _INT)) and
             (uniforms is None or (uniforms.dtype is _F32 and uniforms.get_device() == target.get_device() and uniforms.is_contiguous() and uniforms.numel() == M))):
         _flat(tokens, M, _I32, "tokens"), _flat(parents, M, _I32, "parents"), _flat(starts, S + 1, _I32, "starts"), _flat(uniforms, M, _F32, "uniforms")
         _flat(path, M, _I32, "path"), _flat(counts, S, _I32, "counts"), _flat(next_token, S, _I32, "next_token")
         if target.is_cuda and (draft is None or draft.is_cuda):
             _together("muxq_verify_tree", target, tokens, starts, parents, draft, uniforms, path, counts, next_token)
         _refuse(f"muxq_verify_tree: target and draft are GPU tensors of float [{M}, {V}] with contiguous rows; tokens, parents and path have a number "
-                "for each row, counts and next_token for each sequence")
+                "for each row, counts and next_token for each sequence; row strides and max_nodes take 31 bits at most")
     # (a dimension of one element may carry any stride)
     ldt = target.stride(0) if M > 1 else V
     ldd = 0 if draft is None else draft.stride(0) if M > 1 else V
@@ -979,12 +987,12 @@ def muxq_kv_compact(path, counts, starts, lengths, block_table, k_cache, v_cache
             k_cache.get_device() == v_cache.get_device() and (k_scale is None or k_scale.get_device() == v_scale.get_device() == path.get_device()) and
             path.is_contiguous() and counts.is_contiguous() and
             starts.is_contiguous() and lengths.is_contiguous() and starts.numel() == S + 1 and lengths.numel() == S and block_table.dim() == 2 and
-            block_table.shape[0] == S and block_table.stride(1) == 1):
+            block_table.shape[0] == S and block_table.stride(1) == 1 and block_table.stride(0) <= _INT and 0 <= max_nodes <= _INT):
         _flat(path, M, _I32, "path"), _flat(counts, S, _I32, "counts"), _flat(starts, S + 1, _I32, "starts"), _flat(lengths, S, _I32, "lengths")
         if block_table.is_cuda:
             _together("muxq_kv_compact", k_cache, v_cache, k_scale, v_scale, path, counts, starts, lengths, block_table)
         _refuse("muxq_kv_compact: starts has one entry more than counts, lengths as many, and block_table is an int32 GPU tensor [S, pages] with "
-                "contiguous rows")
+                "contiguous rows; its row stride and max_nodes take 31 bits at most")
     status = lib().muxq_kv_compact(path.data_ptr(), counts.data_ptr(), starts.data_ptr(), lengths.data_ptr(), block_table.data_ptr(),
                                    block_table.stride(0) if S > 1 else block_table.shape[1], M, S, max_nodes, C.byref(c), _stream())
     if status != 0:

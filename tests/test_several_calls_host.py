@@ -1,10 +1,9 @@
 """What the bindings for several new tokens make of workspaces, strides and numbers, without a GPU."""
 import pytest
+import torch
 
 from paper_2604_04701_amd import binding as B
-from test_several_host import ATTENTIONS, attention_args, calls, gpu          # noqa: F401
-
-import torch
+from test_several_host import ATTENTIONS, OnGpu, attention_args, calls, gpu, verify_args          # noqa: F401
 
 
 @pytest.mark.parametrize("call,more", ATTENTIONS, ids=["window", "tree"])
@@ -16,3 +15,46 @@ def test_a_workspace_of_another_device_is_refused(calls, call, more):          #
     with pytest.raises(B.MuxqError, match="workspace"):
         call(**attention_args(), **more, workspace=ws)
     assert len(calls) == 1
+
+
+I32, F32 = torch.int32, torch.float32
+FAR = 1 << 32
+
+
+def far(shape, stride, dtype=torch.float16):
+    """A tensor with strides that no memory here holds."""
+    return torch.empty_strided(shape, stride, dtype=dtype, device="meta").as_subclass(OnGpu)
+
+
+def moves(**kw):
+    return dict(path=gpu(5, dtype=I32), counts=gpu(3, dtype=I32), starts=gpu(4, dtype=I32), lengths=gpu(3, dtype=I32), block_table=gpu(3, 2, dtype=I32),
+                max_nodes=4, k_cache=gpu(4, 2, 16, 64), v_cache=gpu(4, 2, 16, 64)) | kw
+
+
+@pytest.mark.parametrize("call,more", ATTENTIONS, ids=["window", "tree"])
+def test_row_strides_beyond_31_bits_are_refused(calls, call, more):          # noqa: F811
+    for kw in (dict(q=far((5, 4, 64), (FAR + 512, 64, 1))), dict(out=far((5, 4, 64), (FAR + 512, 64, 1))), dict(block_table=far((3, 2), (FAR + 2, 1), I32))):
+        with pytest.raises(B.MuxqError):
+            call(**attention_args() | more | kw)
+    with pytest.raises(B.MuxqError):
+        B.muxq_verify_tree(**verify_args() | dict(target=far((5, 100), (FAR + 100, 1), F32)))
+    with pytest.raises(B.MuxqError):
+        B.muxq_verify_tree(**verify_args() | dict(draft=far((5, 100), (FAR + 100, 1), F32)))
+    with pytest.raises(B.MuxqError):
+        B.muxq_kv_compact(**moves(block_table=far((3, 2), (FAR + 2, 1), I32)))
+    assert calls == []
+
+
+def test_numbers_beyond_31_bits_are_refused(calls):          # noqa: F811
+    window, tree = (dict(attention_args(), **more) for _, more in ATTENTIONS)
+    for call, args, names in ((B.muxq_window_attention, dict(window, window=0, sinks=0), ("max_new", "window", "sinks")),
+                              (B.muxq_tree_attention, tree, ("max_nodes",)), (B.muxq_verify_tree, verify_args(), ("max_nodes",)),
+                              (B.muxq_kv_compact, moves(), ("max_nodes",))):
+        for name in names:
+            for n in (FAR + 2, FAR, -FAR + 2, -1):
+                with pytest.raises(B.MuxqError):
+                    call(**args | {name: n})
+            assert calls == []
+        call(**args)
+        assert len(calls) == 1
+        calls.clear()
