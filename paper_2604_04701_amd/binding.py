@@ -880,7 +880,7 @@ def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_new,
             (parents is None or (parents.dtype is _I32 and parents.get_device() == q.get_device() and parents.is_contiguous() and
                                  parents.numel() == M)) and d == c.head_dim and out.shape == q.shape and
             qs[2] == os[2] == 1 and (n_heads == 1 or qs[1] == os[1] == d) and block_table.dim() == 2 and block_table.shape[0] == S and
-            ts[1] == 1 and lengths.is_contiguous() and starts.is_contiguous() and starts.numel() == S + 1 and
+            (ts[1] == 1 or block_table.shape[1] == 1) and lengths.is_contiguous() and starts.is_contiguous() and starts.numel() == S + 1 and
             max_length <= block_table.shape[1] * c.block_size and qs[0] <= _INT and os[0] <= _INT and ts[0] <= _INT and
             0 <= max_new <= _INT and 0 <= max_length <= _INT):
         _rows(q, "q"), _rows(out, "out"), _flat(lengths, S, _I32, "lengths"), _flat(starts, S + 1, _I32, "starts"), _flat(parents, M, _I32, "parents")
@@ -890,8 +890,10 @@ def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_new,
                 "int32 GPU tensor [S, pages] with contiguous rows of max_length tokens, or a row stride or a bound takes more than 31 bits")
     if workspace is not None and workspace.get_device() != _device():
         _refuse(f"{what}: the workspace is no tensor of the current device")
-    return c, out, os[0], S, (q.data_ptr(), M, n_heads, qs[0], C.byref(c), block_table.data_ptr(),
-                              ts[0] if S > 1 else block_table.shape[1], starts.data_ptr(), lengths.data_ptr())
+    # (a dimension of one element may carry any stride)
+    ldq, ldo = (qs[0], os[0]) if M > 1 else (n_heads * d, n_heads * d)
+    return c, out, ldo, S, (q.data_ptr(), M, n_heads, ldq, C.byref(c), block_table.data_ptr(), ts[0] if S > 1 else block_table.shape[1],
+                            starts.data_ptr(), lengths.data_ptr())
 
 
 def muxq_window_attention(q, k_cache, v_cache, block_table, starts, lengths, max_new, max_length, window=0, sinks=0, scale=None,
@@ -987,7 +989,7 @@ def muxq_kv_compact(path, counts, starts, lengths, block_table, k_cache, v_cache
             k_cache.get_device() == v_cache.get_device() and (k_scale is None or k_scale.get_device() == v_scale.get_device() == path.get_device()) and
             path.is_contiguous() and counts.is_contiguous() and
             starts.is_contiguous() and lengths.is_contiguous() and starts.numel() == S + 1 and lengths.numel() == S and block_table.dim() == 2 and
-            block_table.shape[0] == S and block_table.stride(1) == 1 and block_table.stride(0) <= _INT and 0 <= max_nodes <= _INT):
+            block_table.shape[0] == S and (block_table.stride(1) == 1 or block_table.shape[1] == 1) and block_table.stride(0) <= _INT and 0 <= max_nodes <= _INT):
         _flat(path, M, _I32, "path"), _flat(counts, S, _I32, "counts"), _flat(starts, S + 1, _I32, "starts"), _flat(lengths, S, _I32, "lengths")
         if block_table.is_cuda:
             _together("muxq_kv_compact", k_cache, v_cache, k_scale, v_scale, path, counts, starts, lengths, block_table)

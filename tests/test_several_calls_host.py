@@ -58,3 +58,21 @@ def test_numbers_beyond_31_bits_are_refused(calls):          # noqa: F811
         call(**args)
         assert len(calls) == 1
         calls.clear()
+
+
+def test_a_single_row_may_carry_any_stride(calls):          # noqa: F811
+    """As a view of another order gives it; there is no second row that it leads to."""
+    one = dict(q=gpu(4, 1, 64).transpose(0, 1), out=gpu(4, 1, 64).transpose(0, 1), k_cache=gpu(4, 2, 16, 64), v_cache=gpu(4, 2, 16, 64),
+               block_table=gpu(1, 2, dtype=I32), starts=gpu(2, dtype=I32), lengths=gpu(1, dtype=I32), max_length=32)
+    assert one["q"].stride() == one["out"].stride() == (64, 64, 1)
+    B.muxq_window_attention(**one, max_new=1)
+    B.muxq_tree_attention(**one, max_nodes=1, parents=gpu(1, dtype=I32))
+    for name, args in calls:
+        assert args[1:4] == (1, 4, 256) and args[16 if "window" in name else 15] == 256, name
+    calls.clear()
+    # tables of one page each
+    table = gpu(1, 3, dtype=I32).t()
+    assert table.stride() == (1, 3)
+    B.muxq_window_attention(**attention_args() | dict(block_table=table, max_length=16), max_new=1)
+    B.muxq_kv_compact(**moves(block_table=table))
+    assert [args[6 if "window" in name else 5] for name, args in calls] == [1, 1]
