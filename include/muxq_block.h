@@ -160,6 +160,7 @@ int muxq_norm(const void *X_fp16, int M, int K, int ldx, const void *R_fp16, int
  * muxq_tree_attention: the rows are the nodes of a tree (or forest), parents (int32 [M]) the parent of each as its number within the
  *   sequence, smaller than its own; anything else (-1) marks a root.  Node i sees all tokens before the
  *   tree (t < lengths[s] - n), itself and the nodes above it.  max_nodes <= 64.
+ *   (There is no window: for a model with a sliding one this is its attention only while lengths[s] <= window.)
  * A row that sees nothing (a length below 1, pages outside the cache) is zeros.  What stands in places that a row
  * does not see, NaN and infinity included, has no influence on it; infinite and NaN values in places that it sees
  * come out as the formula has them, with weights that are never quite 0, and scores that are all -infinity give NaN (0 / 0).

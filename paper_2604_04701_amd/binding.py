@@ -917,7 +917,7 @@ def muxq_tree_attention(q, k_cache, v_cache, block_table, starts, lengths, paren
                         v_scale=None, out=None, workspace=None):
     """Attention of the nodes of a drafted tree of each sequence, as muxq_window_attention without a window, but a node sees of the
     new tokens only itself and the nodes above it; parents (int32 [M]): the number of each node's parent within its
-    sequence, -1 for a root.  max_nodes: a bound on the nodes of a tree, at most 64."""
+    sequence, -1 for a root.  max_nodes: a bound on the nodes of a tree, at most 64.  There is no window for trees."""
     c, out, ldo, S, args = _rows_args("muxq_tree_attention", q, k_cache, v_cache, block_table, starts, lengths, max_nodes, max_length, k_scale,
                                       v_scale, out, workspace, parents)
     args += (parents.data_ptr(), S, max_nodes, max_length, c.head_dim ** -0.5 if scale is None else scale,

@@ -2,15 +2,17 @@
 
     python -m paper_2604_04701_amd.draft_step --width 768 --heads 12 --blocks 4 --batch 8 --prompt 300 --nodes 16
 
-A prompt of every sequence goes through the blocks of decode_block.py in one packed batch, attending causally, within a window if
-asked.  Then rounds follow: a draft proposes a tree of tokens behind each sequence's last one, the blocks see all nodes at once (each node
-the tokens before the tree and the nodes above it), the head gives the target's probabilities after every node, the verification
-says which nodes stand and what comes after them, and their keys and values move to the front in every block's cache.  Weights
-are random; the draft is a bigram model of the embedding, as undecided as the target is, so that many of its tokens stand.
+A prompt of every sequence goes through the blocks of decode_block.py in one packed batch, attending causally.  Then rounds
+follow: a draft proposes a tree of tokens behind each sequence's last one, the blocks see all nodes at once (each node the tokens
+before the tree and the nodes above it), the head gives the target's probabilities after every node, the verification says which
+nodes stand and what comes after them, and their keys and values move to the front in every block's cache.  The nodes of a tree
+have no window; a prompt may have one (Model.prompt), but as soon as sequences are longer than that the two are different models.
+Weights are random; the draft is a bigram model of the embedding, as undecided as the target is, so that many of its tokens stand.
 """
 import argparse
 import copy
 import time
+import warnings
 
 import torch
 
@@ -58,6 +60,11 @@ def tree(nodes, branch):
     return parents, depth
 
 
+def reach(longest, nodes, branch, rounds):
+    """The tokens that a sequence may come to: its prompt, the deepest path of every round, and one more tree."""
+    return longest + rounds * (max(tree(nodes, branch)[1]) + 1) + nodes
+
+
 class Model:
     def __init__(self, width, heads, blocks, prompts, nodes, branch, rounds, vocab, page, kv_dtype, adapters, rank, rotated, seed):
         g = torch.Generator(device=DEV)
@@ -66,7 +73,8 @@ class Model:
         self.tree, self.depth = tree(nodes, branch)
         self.deepest = max(self.depth) + 1
         self.longest = max(prompts)                       # of the lengths, known on the host
-        self.max_tokens = self.longest + rounds * self.deepest + nodes
+        self.window = 0                                   # of the prompts
+        self.max_tokens = reach(self.longest, nodes, branch, rounds)
         per = -(-self.max_tokens // page)
         self.table = torch.randperm(self.S * per, generator=g, device=DEV).int().view(self.S, per)
         self.lengths = torch.zeros(self.S, dtype=torch.int32, device=DEV)          # tokens that stand in the cache
@@ -108,7 +116,7 @@ class Model:
         stack = [b.rows(M, self.max_tokens, self.S, most, window, sinks) for b in self.blocks]
         out, seen = run_step(stack, rows, self.embedding[tokens.long()])
         self.lengths.copy_(rows.lengths)
-        self.longest = max(new)
+        self.longest, self.window = most, window
         return out, seen, rows
 
     def draft(self, last, generator=None):
@@ -127,6 +135,8 @@ class Model:
         """Where the next trees stand."""
         if self.longest + self.nodes > self.max_tokens:
             raise ValueError(f"trees up to token {self.longest + self.nodes}, where the tables and angles hold {self.max_tokens}")
+        if 0 < self.window < self.longest + self.nodes:
+            warnings.warn(f"the prompts had a window of {self.window} tokens, the nodes of a tree see all tokens: another model")
         r, n = self.at_round, torch.arange(self.nodes, device=DEV)
         at = self.lengths[:, None] + n
         positions = (self.lengths[:, None] + self.depths).view(-1).int()
@@ -176,13 +186,16 @@ def main():
     ap.add_argument("--blocks", type=int, default=4)
     ap.add_argument("--batch", type=int, default=8)
     ap.add_argument("--prompt", type=int, default=300)
-    ap.add_argument("--window", type=int, default=0)
+    ap.add_argument("--window", type=int, default=0, help="of the prompts, at least what a sequence comes to: trees have none")
     ap.add_argument("--nodes", type=int, default=16)
     ap.add_argument("--branch", type=int, default=2)
     ap.add_argument("--rounds", type=int, default=8)
     ap.add_argument("--vocab", type=int, default=50257)
     ap.add_argument("--fp16-cache", action="store_true")
     args = ap.parse_args()
+    most = reach(max(1, args.prompt), args.nodes, args.branch, args.rounds + 1)
+    if 0 < args.window < most:
+        ap.error(f"a window of {args.window} tokens: the nodes of a tree see all of up to {most}, which is another model")
     B.muxq_init()
     prompts = [max(1, args.prompt - 11 * i) for i in range(args.batch)]
     model = make(args.width, args.heads, args.blocks, prompts, args.nodes, args.branch, args.rounds + 1, args.vocab,
