@@ -394,9 +394,10 @@ __global__ __launch_bounds__(64 * kWaves, kD == 64 ? 4 : kD == 128 || kWaves == 
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const int kt = token_of(tok) + 16 * (j >> 2) + 4 * g + (j & 3);
-                        if constexpr (kRows) {
-                            // (without branches: of `a || b` the compiler loses p[0] = kFloor where only b holds)
-                            const bool out = !here(tok, kt) | (page_of(tok, kt) < 0);
+                        if constexpr (kRows || !kInt8) {
+                            // (without branches: of `if (a || b) p[j] = kFloor, w[j] = 0`, with w read by none, the compiler has lost p[0] = kFloor
+                            // where only b holds; codes, which read w, keep the branch: 24 sequences of 20 heads to 1024 tokens 14.3 us, 14.7 without)
+                            const int out = (int)!here(tok, kt) | (int)(page_of(tok, kt) < 0);
                             p[j] = out ? kFloor : p[j];
                             if constexpr (kInt8) w[j] = out ? 0.0f : w[j];
                         } else {
