@@ -1,0 +1,93 @@
+"""Attention of several new tokens where a workgroup goes through more tiles of tokens than it has pages at hand for, or remembers infinite values
+of; and batches of very unequal numbers of new tokens."""
+import math
+
+import pytest
+import torch
+
+from block_common import check, say
+from paper_2604_04701_amd import binding as B
+from several_common import *          # noqa: F401,F403
+from several_common import Case, below, causal, random_tree, rows64
+
+pytestmark = pytest.mark.gpu
+
+LONG = 4480          # tokens of the last sequence: 35 tiles of 128, the widest there are
+
+# new tokens and lengths of each sequence, heads: so many workgroups that none of them is cut along the tokens
+FORMS = {"rows32_of_64": ([2] * 65, [5] * 64 + [LONG], 8, 8, 64), "rows64_of_64": ([40] * 49, [40] * 48 + [LONG], 16, 16, 64),
+         "rows128_of_64": ([70] * 64, [70] * 63 + [LONG], 16, 16, 64), "rows32_of_128": ([2] * 64, [9] * 63 + [LONG], 16, 16, 128),
+         "rows64_of_128": ([40] * 33, [40] * 32 + [LONG], 16, 16, 128), "rows128_of_128": ([130] * 40, [130] * 39 + [LONG], 32, 16, 128),
+         "rows128_of_80": ([130] * 40, [130] * 39 + [LONG], 32, 16, 80), "rows128_of_256": ([40] * 64, [40] * 63 + [LONG], 8, 8, 256),
+         "trees64_of_64": ([40] * 33, [40] * 32 + [LONG], 16, 16, 64), "trees128_of_128": ([64] * 33, [64] * 32 + [LONG], 32, 16, 128)}
+
+
+def call(c, tree):
+    starts, lengths = c.device()
+    if tree:
+        parents = ints(sum((random_tree(n, n) for n in c.new), []))
+        return B.muxq_tree_attention(c.q, c.k, c.v, c.table, starts, lengths, parents, max(c.new), max(c.lengths), **c.scales())
+    return B.muxq_window_attention(c.q, c.k, c.v, c.table, starts, lengths, max(c.new), max(c.lengths), **c.scales())
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("kind", ["plain", "missing", "infinite"])
+@pytest.mark.parametrize("name", FORMS)
+def test_many_tiles_of_one_workgroup(monkeypatch, name, kind, bits):
+    new, lengths, H, heads, d = FORMS[name]
+    tree = name.startswith("trees")
+    say(f"[case] many tiles {name} {kind} bits={bits}")
+    c = Case(21, new, lengths, H, heads, d, 16, bits)
+    s, n, group = len(new) - 1, new[-1], H // heads
+    if kind == "missing":                # in every 32 tiles of 32, 64 or 128 tokens
+        for t in (500, 1030, 2100, 3000, 4100, 4200):
+            c.table[s, t // c.page] = [-1, c.n_pages][t % 2]
+    if kind == "infinite":
+        tokens = list(range(10, LONG - n, 64))
+        pages, at = c.table[s, torch.tensor(tokens, device=DEV) // c.page].long(), torch.tensor(tokens, device=DEV) % c.page
+        # (values are finite for the formula; the kernel sees them infinite)
+        if bits == 16:
+            c.v[pages, 1, at, 7] = 0
+            c.v[pages, 1, at, 9] = 0
+        else:
+            c.v[pages, 1, at] = 0
+    # (a workspace that is asked for would say that the work is cut into pieces)
+    for form in ("window", "tree"):
+        monkeypatch.setattr(B, f"alloc_{form}_attention_workspace", lambda *_: pytest.fail("in pieces: fewer than 33 tiles a workgroup"))
+    want, tol = rows64(c.q, c.k, c.v, c.ks, c.vs, c.table, c.starts, lengths,
+                       lambda i, m, length: below(random_tree(m, m), length) if tree else causal(m, length, 0, 0), d ** -0.5)
+    if kind != "infinite":
+        check(call(c, tree), want, tol, name)
+        return
+    if bits == 16:
+        c.v[pages, 1, at, 7] = math.inf
+        c.v[pages, 1, at, 9] = math.inf
+        c.v[pages[-1], 1, at[-1], 9] = -math.inf
+    else:
+        c.v[pages, 1, at] = 3
+        c.vs[pages, 1, at] = math.inf
+    got = call(c, tree).double()
+    a = c.starts[s]
+    mine = got[a:, group:2 * group]
+    for e in (7, 9) if bits == 16 else range(d):
+        assert (torch.isnan(mine[..., e]) if e == 9 and bits == 16 else mine[..., e] == math.inf).all(), e
+        mine[..., e] = want[a:, group:2 * group, e]
+    check(got, want, tol, name)
+
+
+# a chunk of a prompt beside single tokens, as a server's step has them
+MIXED = {"12x64": (12, 12, 64), "32of8x128": (32, 8, 128), "4of1x256": (4, 1, 256)}
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("win,sinks", [(0, 0), (300, 4)])
+@pytest.mark.parametrize("name", MIXED)
+def test_a_chunk_beside_single_tokens(name, win, sinks, bits):
+    H, heads, d = MIXED[name]
+    say(f"[case] mixed batch {name} window={win} sinks={sinks} bits={bits}")
+    singles = [1 + 37 * i * i % 4001 for i in range(40)]
+    c = Case(22, [1] * 11 + [512] + [1] * 29 + [3], singles[:11] + [1300] + singles[11:] + [700], H, heads, d, 16, bits)
+    starts, lengths = c.device()
+    got = B.muxq_window_attention(c.q, c.k, c.v, c.table, starts, lengths, 512, max(c.lengths), window=win, sinks=sinks, **c.scales())
+    want, tol = c.exact(lambda i, m, length: causal(m, length, win, sinks))
+    check(got, want, tol, name)
