@@ -91,3 +91,33 @@ def test_a_chunk_beside_single_tokens(name, win, sinks, bits):
     got = B.muxq_window_attention(c.q, c.k, c.v, c.table, starts, lengths, 512, max(c.lengths), window=win, sinks=sinks, **c.scales())
     want, tol = c.exact(lambda i, m, length: causal(m, length, win, sinks))
     check(got, want, tol, name)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_a_dimension_that_is_infinite_everywhere(bits):
+    """As a model has it that passes fp16 in a channel: right, and in milliseconds (each row's look at each token from memory took 600)."""
+    say(f"[case] a dimension of infinite values, bits={bits}")
+    n = 4096
+    c = Case(23, [n], [n], 32, 8, 128, 16, bits)
+    if bits == 16:
+        c.v[..., 3] = 0
+        want = call(c, False)
+        c.v[..., 3] = math.inf
+        c.v[c.table[0, 100].long(), 2, 5, 3] = -math.inf          # token 1605: NaN from there on, in its heads
+        want[..., 3] = math.inf
+        want[1605:, 8:12, 3] = math.nan
+    else:
+        want = torch.full_like(c.q, math.inf)
+        want[..., ::2] = -math.inf
+        c.v[..., ::2], c.v[..., 1::2] = -1, 1
+        c.vs[:] = math.inf
+    best = math.inf
+    for _ in range(3):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        got = call(c, False)
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b))
+    assert torch.equal(got.nan_to_num(7.0, 8.0, 9.0), want.nan_to_num(7.0, 8.0, 9.0))
+    assert best < 150.0, f"{best:.0f} ms"

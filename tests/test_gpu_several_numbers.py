@@ -81,3 +81,52 @@ def test_scores_that_are_no_numbers_beside_infinite_values(name, early, kind, bi
     assert (mine[infinite] == sign * math.inf).all(), f"{name}: rows that see an infinite value"
     got[a:, :group][broken | infinite] = want[a:, :group][broken | infinite]
     check(got, want, tol, name)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("what", ["key", "query"])
+@pytest.mark.parametrize("name", SHAPES)
+def test_infinite_values_with_weights_of_0(name, what, bits):
+    """A score of -infinity is a weight of 0, and 0 times an infinite value is NaN; a row that has no other scores is 0 / 0."""
+    new, lengths, H, heads, d = SHAPES[name]
+    say(f"[case] weights of 0 {name} {what} bits={bits}")
+    c = Case(14, new, lengths, H, heads, d, 16, bits)
+    s, n, length, group = len(new) - 1, new[-1], lengths[-1], H // heads
+    a, t = c.starts[s], length - max(1, n // 2)
+    p, i = int(c.table[s, t // c.page]), t % c.page
+    c.q[:, :, 2] = 1.0
+    spoilt = torch.arange(d, device=DEV) % 3 == 0
+
+    def seen_of(x, m, most):
+        seen = causal(m, most, 0, 0)
+        if x == s:
+            seen[:, t] = False
+        return seen
+    want, tol = c.exact(lambda x, m, most: causal(m, most, 0, 0))
+    without = c.exact(seen_of)
+    want[:, :group], tol[:, :group] = without[0][:, :group], without[1][:, :group]         # (only these heads' scores are infinite)
+    sees = causal(n, length, 0, 0)[:, t]
+    assert sees.any() and length > 1
+    c.k[p, 0, i] = 0
+    if bits == 16:
+        c.k[p, 0, i, 2] = -math.inf
+        c.v[p, 0, i] = torch.where(spoilt, math.inf, 1.0).half()
+    else:
+        c.k[p, 0, i, 2] = -1
+        c.ks[p, 0, i] = c.vs[p, 0, i] = math.inf
+        spoilt[:] = True
+    if what == "query":           # the same of all tokens, for one row
+        m = a + int(sees.nonzero()[0])
+        used = c.table[s, :-(-length // c.page)].long()
+        c.k[used, 0, :, 3] = -1
+        c.q[m, :group, 3] = math.inf
+    starts, at = c.device()
+    got = B.muxq_window_attention(c.q, c.k, c.v, c.table, starts, at, max(new), max(lengths), **c.scales()).double()
+    if what == "query":
+        assert torch.isnan(got[m, :group]).all()
+        return
+    mine = got[a:, :group]
+    assert torch.isnan(mine[sees][..., spoilt]).all()
+    hit = sees.to(DEV)[:, None, None] & spoilt
+    got[a:, :group] = torch.where(hit, want[a:, :group], mine)
+    check(got, want, tol, name)
