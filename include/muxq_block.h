@@ -148,8 +148,8 @@ int muxq_norm(const void *X_fp16, int M, int K, int ldx, const void *R_fp16, int
  * The rows of sequence s are starts[s] <= m < starts[s + 1] (int32 [S + 1], ascending, clamped to [0, M]); n of them are its
  * n new tokens, which stand in the cache already, as the last n of its lengths[s] tokens: row starts[s] + i is token
  * lengths[s] - n + i.  A length above max_length counts as max_length.  A sequence with more rows than max_new (max_nodes)
- * counts as one without rows.  Rows in no sequence are not written.  S <= 65535, M <= 2^24, and of a call's longest sequence
- * rows times n_heads / n_kv_heads below 2^31 - 256.
+ * counts as one without rows.  Rows in no sequence are not written.  S <= 65535, M <= 2^24, and the
+ * smaller of M and max_new times n_heads at most 2^30 for the attention.
  *
  * Attention of these tokens over the cache:
  *   O[m][h] = sum_t softmax_t(scale * Q[m][h] . K[t][h / g]) V[t][h / g]   over the tokens t that m sees,

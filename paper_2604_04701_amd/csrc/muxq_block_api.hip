@@ -301,7 +301,8 @@ static int rows_attention(const void *Q, int M, int n_heads, int ldq, const muxq
     a.window = window;
     a.sinks = window ? sinks : 0;
     a.max_new = max_new < M ? max_new : M;
-    if ((long long)a.max_new * (n_heads / a.c.n_kv_heads) >= (1ll << 31) - 256) return MUXQ_ERR_SHAPE;
+    // (workgroups of 128 rows then: 2^23 of them, and one more for each key-value head)
+    if ((long long)a.max_new * n_heads > 1ll << 30) return MUXQ_ERR_SHAPE;
     const size_t need = muxq::rows_workspace_need(S, n_heads, a.c.n_kv_heads, d, a.max_new, max_length, a.window, a.sinks, tree);
     if (need > 0) {
         if (!workspace) return MUXQ_ERR_NULL;

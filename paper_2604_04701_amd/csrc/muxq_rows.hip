@@ -996,7 +996,7 @@ hipError_t launch_rows(const RowsArgs &a, bool int8, hipStream_t s)
         return launch_attend_rows(b, int8, s);
     }
     const Form f = form_of(a.S, a.n_heads, a.c.n_kv_heads, d, a.max_new, a.max_length, a.window, a.sinks, a.parents != nullptr);
-    if (f.row_tiles * a.c.n_kv_heads > 1 << 23) return hipErrorInvalidValue;
+    if (f.row_tiles * a.c.n_kv_heads > (1 << 23) + a.c.n_kv_heads) return hipErrorInvalidValue;
     Plan plan{(int)f.row_tiles, f.pieces, f.tiles, nullptr, nullptr};
     if (f.pieces > 1) {
         const size_t parts = (size_t)f.groups * f.pieces * f.rows;

@@ -3,7 +3,8 @@ import pytest
 import torch
 
 from paper_2604_04701_amd import binding as B
-from test_several_host import ATTENTIONS, OnGpu, attention_args, calls, gpu, verify_args          # noqa: F401
+from test_block_host import cache
+from test_several_host import ATTENTIONS, OnGpu, attention_args, calls, gpu, rows, verify_args          # noqa: F401
 
 
 @pytest.mark.parametrize("call,more", ATTENTIONS, ids=["window", "tree"])
@@ -76,3 +77,11 @@ def test_a_single_row_may_carry_any_stride(calls):          # noqa: F811
     B.muxq_window_attention(**attention_args() | dict(block_table=table, max_length=16), max_new=1)
     B.muxq_kv_compact(**moves(block_table=table))
     assert [args[6 if "window" in name else 5] for name, args in calls] == [1, 1]
+
+
+@pytest.mark.parametrize("heads,n_heads,M,status", [(128, 128, 1 << 24, 2), (64, 256, (1 << 22) + 1, 2), (1, 1024, (1 << 20) + 1, 2)])
+def test_calls_of_more_workgroups_than_a_grid_has_are_refused(heads, n_heads, M, status):
+    """Rows times heads beyond 2^30, for shapes and not by the launch."""
+    c = cache(n_kv_heads=heads, ld_block=heads * 16 * 64)
+    wide = dict(M=M, new=M, n_heads=n_heads, ldq=n_heads * 64, ldo=n_heads * 64, o=1 << 46, window=0, sinks=0)
+    assert rows(c, **wide) == status
