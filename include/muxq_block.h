@@ -165,10 +165,12 @@ int muxq_norm(const void *X_fp16, int M, int K, int ldx, const void *R_fp16, int
  * does not see, NaN and infinity included, has no influence on it; infinite and NaN values in places that it sees
  * come out as the formula has them, with weights that are never quite 0, and scores that are all -infinity give NaN (0 / 0).
  * Arithmetic: products of fp16 with binary32 sums; scales of codes multiply scores and weights; statistics of the softmax are
- * binary32; the weights enter the second product rounded to fp16 (11 bits or more, and whole multiples of 2^-32 of a row's largest, with
- * codes 2^-31 of the largest weight times the largest scale that the row sees).
+ * binary32; the weights enter the second product rounded to fp16: each is off by at most 2^-11 of itself, or 2^-31 of the row's
+ * largest where that is more (with codes 2^-30 of the largest weight times the largest scale that the row sees).  Calls with max_new = 1 may take the
+ * kernel of muxq_paged_attention, by their sizes, whose weights have 22 bits.
  * max_length: the host's bound on lengths[], 1 <= max_length <= ld_table * block_size, at most 2^26; max_new and max_nodes: the
- * host's bound on the rows of a sequence.  The work is divided by them.
+ * host's bound on the rows of a sequence.  The work is divided by them, as if each sequence had that many rows: a long chunk of a prompt and
+ * many single tokens are faster as two calls (2048 tokens beside 256 single ones of 500 to 8000: 1.9 ms, in two calls 0.83).
  * workspace: ..._workspace_bytes(...) bytes, 256-byte aligned, content undefined on entry; enough for every call with S, max_new
  * (max_nodes), max_length, window and sinks no larger (a window of 0 is the largest); NULL where that is 0.  Calls that share one must
  * not overlap in time. */
@@ -187,7 +189,8 @@ int muxq_tree_attention(const void *Q_fp16, int M, int n_heads, int ldq, const m
 /* Drafted tokens against the target's probabilities.  Each sequence has a tree of n <= max_nodes <= 64 nodes (starts, parents as
  * above; a chain is a tree), whose node 0 is its last token and stands already; tokens[m] (int32 [M]) is the token of node m.  target: float
  * [M][V] (row stride ldt), row m what the target says after node m; draft: float [M][V] (ldd), row m what the children of
- * node m were drawn from, NULL: they were chosen without drawing (a probability of 1).  uniforms: float [M] in [0, 1).
+ * node m were drawn from, each by itself and with replacement (for others, drawn without replacement for instance, what comes out is not distributed
+ * as the target), NULL: they were chosen without drawing (a probability of 1).  uniforms: float [M] in [0, 1).
  * From v = 0, r = target[v], Z = 1 the children c of v, ascending, are tried:
  *   accepted if uniforms[c] * draft[v][x_c] * Z < r[x_c]: then v = c, and on with its children;
  *   otherwise r = max(r / Z - draft[v], 0), Z = sum r, and on with the next one.  If Z is 0, no other child is accepted and r = target[v].
