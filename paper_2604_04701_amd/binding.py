@@ -881,8 +881,7 @@ def _rows_args(what, q, k_cache, v_cache, block_table, starts, lengths, max_new,
                                  parents.numel() == M)) and d == c.head_dim and out.shape == q.shape and
             qs[2] == os[2] == 1 and (n_heads == 1 or qs[1] == os[1] == d) and block_table.dim() == 2 and block_table.shape[0] == S and
             (ts[1] == 1 or block_table.shape[1] == 1) and lengths.is_contiguous() and starts.is_contiguous() and starts.numel() == S + 1 and
-            max_length <= block_table.shape[1] * c.block_size and qs[0] <= _INT and os[0] <= _INT and ts[0] <= _INT and
-            0 <= max_new <= _INT and 0 <= max_length <= _INT):
+            max_length <= block_table.shape[1] * c.block_size and 0 <= qs[0] | os[0] | ts[0] | max_new | max_length <= _INT):
         _rows(q, "q"), _rows(out, "out"), _flat(lengths, S, _I32, "lengths"), _flat(starts, S + 1, _I32, "starts"), _flat(parents, M, _I32, "parents")
         if block_table.is_cuda:
             _together(what, q, out, k_cache, v_cache, k_scale, v_scale, block_table, starts, lengths, parents)
@@ -902,7 +901,7 @@ def muxq_window_attention(q, k_cache, v_cache, block_table, starts, lengths, max
     starts[s]..starts[s + 1] (int32 [S + 1]) are the last of lengths[s] tokens (int32 [S]).  window: how many tokens a row sees, its own the
     last of them (0: all), with the first `sinks` of the sequence beside them.  max_new, max_length: bounds on the rows and tokens of a
     sequence known on the host.  scale: 1 / sqrt(d) when not given."""
-    if not (0 <= window <= _INT and 0 <= sinks <= _INT):
+    if not 0 <= window | sinks <= _INT:
         _refuse("muxq_window_attention: window and sinks are numbers of tokens, 31 bits at most")
     c, out, ldo, S, args = _rows_args("muxq_window_attention", q, k_cache, v_cache, block_table, starts, lengths, max_new, max_length, k_scale,
                                       v_scale, out, workspace)
@@ -941,7 +940,7 @@ def muxq_verify_tree(target, tokens, starts, parents, max_nodes, draft=None, uni
     if not (target.dtype is _F32 and tokens.dtype is parents.dtype is starts.dtype is path.dtype is counts.dtype is next_token.dtype is _I32 and
             _device() == target.get_device() == tokens.get_device() == parents.get_device() == starts.get_device() == path.get_device() ==
             counts.get_device() == next_token.get_device() and
-            (target.stride(1) == 1 or V == 1) and target.stride(0) <= _INT and 0 <= max_nodes <= _INT and tokens.is_contiguous() and parents.is_contiguous() and starts.is_contiguous() and
+            (target.stride(1) == 1 or V == 1) and 0 <= target.stride(0) | max_nodes <= _INT and tokens.is_contiguous() and parents.is_contiguous() and starts.is_contiguous() and
             path.is_contiguous() and counts.is_contiguous() and next_token.is_contiguous() and tokens.numel() == parents.numel() == path.numel() == M and
             counts.numel() == next_token.numel() == S and
             (draft is None or (draft.dtype is _F32 and draft.get_device() == target.get_device() and draft.shape == (M, V) and (draft.stride(1) == 1 or V == 1) and
@@ -989,7 +988,7 @@ def muxq_kv_compact(path, counts, starts, lengths, block_table, k_cache, v_cache
             k_cache.get_device() == v_cache.get_device() and (k_scale is None or k_scale.get_device() == v_scale.get_device() == path.get_device()) and
             path.is_contiguous() and counts.is_contiguous() and
             starts.is_contiguous() and lengths.is_contiguous() and starts.numel() == S + 1 and lengths.numel() == S and block_table.dim() == 2 and
-            block_table.shape[0] == S and (block_table.stride(1) == 1 or block_table.shape[1] == 1) and block_table.stride(0) <= _INT and 0 <= max_nodes <= _INT):
+            block_table.shape[0] == S and (block_table.stride(1) == 1 or block_table.shape[1] == 1) and 0 <= block_table.stride(0) | max_nodes <= _INT):
         _flat(path, M, _I32, "path"), _flat(counts, S, _I32, "counts"), _flat(starts, S + 1, _I32, "starts"), _flat(lengths, S, _I32, "lengths")
         if block_table.is_cuda:
             _together("muxq_kv_compact", k_cache, v_cache, k_scale, v_scale, path, counts, starts, lengths, block_table)
