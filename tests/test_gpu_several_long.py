@@ -121,3 +121,33 @@ def test_a_dimension_that_is_infinite_everywhere(bits):
         best = min(best, a.elapsed_time(b))
     assert torch.equal(got.nan_to_num(7.0, 8.0, 9.0), want.nan_to_num(7.0, 8.0, 9.0))
     assert best < 150.0, f"{best:.0f} ms"
+
+
+def test_verification_of_more_rows_than_a_grid_holds():
+    """Greedy, where the rows of all nodes are looked at at once as long as a launch holds them."""
+    M = (1 << 22) + 5
+    say(f"[case] verify {M} rows")
+    target = torch.rand(M, 2, generator=gen(1), device=DEV)
+    tokens, parents = torch.zeros(M, dtype=torch.int32, device=DEV), torch.full((M,), -1, dtype=torch.int32, device=DEV)
+    parents[M - 2:] = ints([0, 1])
+    for V in (1, 2):
+        rows = target[:, :V]
+        tokens[M - 2:] = rows[M - 3:M - 1].argmax(1).int()          # what the target says after the node above
+        left = torch.full((M,), 7, dtype=torch.int32, device=DEV)
+        path, counts, said = B.muxq_verify_tree(rows, tokens, ints([3, 4, M - 3, M]), parents, 64, path=left)
+        assert counts.tolist() == [1, 0, 3] and said.tolist() == [int(rows[3].argmax()), -1, int(rows[M - 1].argmax())]
+        assert path[3] == 0 and (path[:3] == 7).all() and (path[4:M - 3] == -1).all() and path[M - 3:].tolist() == [0, 1, 2]
+
+
+def test_copies_of_more_pairs_than_a_launch_takes():
+    n = (1 << 22) + 9                     # 2^22 pairs of pages of two parts each are one launch
+    say(f"[case] copy {n} pairs")
+    k, v = (normal(gen(i), 12, 1, 8, 16) for i in (1, 2))
+    src, dst = (torch.full((n,), -1, dtype=torch.int32, device=DEV) for _ in range(2))
+    at = torch.tensor([0, (1 << 22) - 1, 1 << 22, n - 1], device=DEV)
+    src[at], dst[at] = ints([1, 2, 3, 4]), ints([5, 6, 7, 8])
+    want = [x.clone() for x in (k, v)]
+    for x in want:
+        x[5:9] = x[1:5]
+    B.muxq_kv_copy(src, dst, k, v)
+    assert torch.equal(k, want[0]) and torch.equal(v, want[1])
