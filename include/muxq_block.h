@@ -10,7 +10,8 @@
  * or synchronised; every call only enqueues kernels on `stream` and may be captured into a graph (the first
  * call on a device after muxq_init(), which loads the kernels);
  * the return value is a muxq_status, and on any status other than MUXQ_OK (MUXQ_ERR_HIP apart)
- * nothing has been enqueued.  Activations are fp16, rows contiguous, with row strides in elements
+ * nothing has been enqueued.  (MUXQ_ERR_HIP is also what a call gives that would take a launch of 2^32 threads or more, some
+ * 2^34 elements.)  Activations are fp16, rows contiguous, with row strides in elements
  * that are multiples of 8, from 16-byte aligned pointers.  Sums, maxima and softmax
  * statistics are binary32.  Results do not depend on the order in which workgroups run.
  * Index arrays (slots, positions, block tables, lengths, request starts, adapter numbers) are read

@@ -14,6 +14,7 @@ namespace muxq {
 // triple-chevron launch reports the runtime's sticky error word: a failure some earlier,
 // unrelated call of the process left there would be taken for a failed launch here.)
 // The arguments are converted to the kernel's exact parameter types first.
+// A launch has fewer than 2^32 threads in each dimension; HIP starts a larger one modulo that, without an error.
 template <typename... P, size_t... I>
 inline hipError_t launch_kernel_impl(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds_bytes,
                                      hipStream_t s, std::tuple<P...> &params, std::index_sequence<I...>)
@@ -26,6 +27,7 @@ inline hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, siz
                                 A &&...args)
 {
     static_assert(sizeof...(P) == sizeof...(A), "argument count differs from the kernel's parameter list");
+    if ((uint64_t)grid.x * block.x >> 32 || (uint64_t)grid.y * block.y >> 32 || (uint64_t)grid.z * block.z >> 32) return hipErrorInvalidConfiguration;
     std::tuple<P...> params{static_cast<P>(std::forward<A>(args))...};
     return launch_kernel_impl(kernel, grid, block, lds_bytes, s, params, std::index_sequence_for<P...>{});
 }

@@ -375,7 +375,7 @@ hipError_t launch_verify(const VerifyArgs &a, hipStream_t s)
 {
     const size_t lds = (size_t)((a.V + kBlock - 1) / kBlock) * sizeof(double);
     // Greedy: all rows at once and the walk after them, or the rows of a walk one after the other.
-    // (A launch has fewer than 2^32 threads; HIP drops the rest of a larger one without a word.)
+    // (A launch has fewer than 2^32 threads.)
     const bool known = !a.uniforms && (long long)a.M * a.V <= kAtOnce && (long long)a.M * kThreads < 1ll << 32;
     if (known) {
         const hipError_t e = launch_kernel(k_largest, dim3(a.M), dim3(kThreads), 0, s, a);
