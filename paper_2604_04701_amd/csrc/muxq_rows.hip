@@ -24,9 +24,9 @@
 // their sum are over a running power of two that the scales which a row sees do not pass.
 //
 // What bounds it and what it reaches:
-//   16384 tokens within a window of 4096, 32 heads of 128 over 8 of keys, fp16: 1.08 ms, 894 TFLOP/s of the 1190 that a large product reaches.
+//   16384 tokens within a window of 4096, 32 heads of 128 over 8 of keys, fp16: 1.09 ms, 885 TFLOP/s of the 1190 that a large product reaches.
 //     The matrix pipes are busy 46 % of the cycles that a CU works, at 1.7 GHz of the 2.4 nominal; LDS is active 48 % of them.
-//   13 prompts, 8192 tokens together, behind up to 1500, a window of 1024, in codes: 0.22 ms, 530 TFLOP/s: conversion and scales are as many vector
+//   13 prompts, 8192 tokens together, behind up to 1500, a window of 1024, in codes: 0.22 ms, 520 TFLOP/s: conversion and scales are as many vector
 //     instructions as the softmax is (14 for a product, 6 over fp16); the matrix pipes are busy 26 % of the cycles.
 //   64 trees of 32 nodes over up to 8192 tokens: 0.26 ms, 4.4 TB/s: loads on their way, 32 KB a workgroup and two workgroups a CU.
 //   1024 tokens, 12 heads of 64: 16.6 us with the join; 8 nodes behind 37
