@@ -151,3 +151,46 @@ def test_copies_of_more_pairs_than_a_launch_takes():
         x[5:9] = x[1:5]
     B.muxq_kv_copy(src, dst, k, v)
     assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
+@pytest.mark.parametrize("new", [1, 2])
+def test_as_many_sequences_as_there_may_be(new):
+    """65535 of them, a page each: attention, verification and compaction."""
+    S, d, page = 65535, 16, 8
+    say(f"[case] {S} sequences of {new} rows")
+    g = gen(new)
+    k, v = (normal(g, S, 1, page, d) for _ in "kv")
+    table = torch.randperm(S, generator=g, device=DEV).int().view(S, 1)
+    lengths = torch.randint(new, page + 1, (S,), generator=g, device=DEV).int()
+    starts = torch.arange(0, S * new + 1, new, device=DEV).int()
+    q = normal(g, S * new, 1, d)
+    parents = torch.arange(new, device=DEV).int().sub(1).repeat(S)
+    for tree in (False, True):
+        if tree:
+            got = B.muxq_tree_attention(q, k, v, table, starts, lengths, parents, new, page)
+        else:
+            got = B.muxq_window_attention(q, k, v, table, starts, lengths, new, page)
+        kk, vv = (x[table[:, 0].long(), 0].double() for x in (k, v))
+        score = (q.double().view(S, new, 1, d) * kk[:, None]).sum(3) / 4
+        last = lengths[:, None] - new + torch.arange(new, device=DEV)
+        score = score.masked_fill(torch.arange(page, device=DEV) > last[..., None], -math.inf)
+        p = torch.softmax(score, 2)
+        want, mass = ((p[..., None] * x[:, None]).sum(2) for x in (vv, vv.abs()))
+        # one rounding of the output, one of the weights, and of sums of 16 products of some 20 in all
+        tol = TINY16 + 2.0 ** -11 * (want.abs() + 1.01 * mass) + 3 * 2.0 ** -16 * mass
+        check(got.view(S, new, d), want, tol, "attention")
+    V = 5
+    target = torch.softmax(torch.randn(S * new, V, generator=g, device=DEV), 1)
+    tokens = torch.randint(0, V, (S * new,), generator=g, device=DEV).int()
+    path, counts, said = B.muxq_verify_tree(target, tokens, starts, parents, new)
+    best = target.argmax(1).view(S, new)
+    stands = (tokens.view(S, new)[:, -1] == best[:, 0]) & (new == 2)
+    assert torch.equal(counts, 1 + stands.int())
+    assert torch.equal(said, torch.where(stands, best[:, -1], best[:, 0]).int())
+    assert (path.view(S, new)[:, 0] == 0).all()
+    # the last node to the front
+    at = torch.full((S * new,), new - 1, dtype=torch.int32, device=DEV)
+    kept = [x[table[:, 0].long(), 0, lengths.long() - 1] for x in (k, v)]
+    B.muxq_kv_compact(at, torch.ones(S, dtype=torch.int32, device=DEV), starts, lengths, table, k, v, new)
+    for x, y in zip((k, v), kept):
+        assert torch.equal(x[table[:, 0].long(), 0, lengths.long() - new], y)
